@@ -10,7 +10,8 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 LIB = os.path.join(PKG, "libeden_hip.so")
 OBJ_DIR = os.path.join(ROOT, "_build")
-SOURCES = ["eden_tables.cpp", "eden_kernels.hip", "eden_kernels_small.hip", "eden_kernels_sparse.hip", "eden_kernels_wg.hip", "eden_kernels_wg_dec.hip", "eden_kernels_lo14.hip", "eden_kernels_lo15.hip", "eden_api.hip"]
+SOURCES = ["eden_tables.cpp", "eden_kernels.hip", "eden_kernels_small.hip", "eden_kernels_sparse.hip", "eden_kernels_wg.hip", "eden_kernels_wg_dec.hip", "eden_kernels_lo14.hip", "eden_kernels_lo15.hip", "eden_api.hip",
+           "eden_layers_tiles.hip", "eden_layers_elements.hip", "eden_layers_api.hip"]
 
 
 def hipcc_path() -> str:
@@ -34,7 +35,12 @@ def _stale(src: str, obj: str) -> bool:
     if not os.path.exists(obj):
         return True
     csrc = os.path.join(PKG, "csrc")
-    deps = [src, os.path.join(ROOT, "include", "eden.h")] + [os.path.join(csrc, f) for f in os.listdir(csrc) if f.endswith(".h")]
+    # the layer operators share no header with the rest but eden.h
+    layers = os.path.basename(src).startswith("eden_layers")
+    deps = [src, os.path.join(ROOT, "include", "eden.h")] + [os.path.join(csrc, f) for f in os.listdir(csrc)
+                                                             if f.endswith(".h") and f.startswith("eden_layers") == layers]
+    if layers:
+        deps.append(os.path.join(ROOT, "include", "eden_layers.h"))
     return any(os.path.getmtime(dep) > os.path.getmtime(obj) for dep in deps)
 
 

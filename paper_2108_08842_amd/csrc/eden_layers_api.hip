@@ -1,0 +1,164 @@
+// C ABI of the layer operators (see include/eden_layers.h for the contract of every call).  Host code only: argument checks, the
+// choice of a kernel, launches.
+#include "eden_layers_kernels.h"
+
+using namespace eden_layers;
+
+namespace {
+
+constexpr uint64_t kMostSize = 1ull << 30;
+constexpr uint64_t kMostGroups = 0x7FFFFFFFull;        // workgroups of a launch
+
+bool known_type(uint32_t dtype) { return dtype <= EDEN_BF16; }
+size_t bytes_of(uint32_t dtype) { return dtype == EDEN_F32 ? 4 : 2; }
+int status(hipError_t e) { return e == hipSuccess ? EDEN_OK : EDEN_ERR_HIP; }
+
+// A matrix that is read or written: absent only if it has no element; aligned to its elements, rows apart.
+bool matrix_ok(const void *p, uint64_t ld, uint64_t rows, uint64_t cols, size_t element) {
+    if (rows == 0 || cols == 0) return true;
+    return p != nullptr && reinterpret_cast<uintptr_t>(p) % element == 0 && (rows == 1 || (ld >= cols && ld <= (1ull << 40)));
+}
+bool checkpoint_ok(const void *p, uint64_t rows, uint64_t cols) {
+    return rows == 0 || cols == 0 || (p != nullptr && reinterpret_cast<uintptr_t>(p) % 16 == 0);
+}
+size_t codes_bytes(uint64_t rows, uint64_t cols) { return rows * blocks_of(cols) * kBlock; }
+
+// Element-wise launches: at least 1024 values a workgroup but for the ends of rows
+bool launchable(uint64_t rows, uint64_t cols) { return rows * (blocks_of(cols) / 64 + 1) <= kMostGroups; }
+
+uint64_t tile_count(uint64_t rows, uint64_t cols) { return (uint64_t)tiles_of((uint32_t)rows) * tiles_of((uint32_t)cols); }
+size_t partial_bytes(uint64_t rows, uint64_t cols, uint64_t splits) { return splits * rows * ((cols + 3) / 4 * 4 + 1) * sizeof(float); }
+
+// How many workgroups share a tile's sum.  The device holds two tiles per CU, 512 in all; a sum of less than 256 is not worth the join.
+uint64_t splits_of(uint64_t rows, uint64_t cols, uint64_t depth) {
+    if (rows == 0 || cols == 0) return 1;
+    const uint64_t tiles = tile_count(rows, cols);
+    if (tiles > 256) return 1;
+    uint64_t s = 512 / tiles;
+    if (s > depth / 256) s = depth / 256;
+    return s < 1 ? 1 : s > 64 ? 64 : s;
+}
+
+// Launches a product whose operands and end are set.
+int run(Op op, uint32_t dtype, Product &p, void *workspace, size_t workspace_bytes, void *stream) {
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    uint64_t splits = splits_of(p.rows, p.cols, p.depth);
+    if (reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return EDEN_ERR_INVALID_ARG;
+    if (workspace == nullptr) workspace_bytes = 0;
+    while (splits > 1 && partial_bytes(p.rows, p.cols, splits) > workspace_bytes) --splits;
+    const uint64_t each = ((p.depth + splits - 1) / splits + kSplitUnit - 1) / kSplitUnit * kSplitUnit;
+    splits = each ? (p.depth + each - 1) / each : 1;
+    p.splits = splits < 1 ? 1 : (uint32_t)splits;
+    p.split_depth = (uint32_t)each;
+    p.partial = static_cast<float *>(workspace);
+    p.partial_ld = (p.cols + 3) / 4 * 4;
+    if (tile_count(p.rows, p.cols) * p.splits > kMostGroups) return EDEN_ERR_INVALID_ARG;
+    hipError_t e = launch_tiles(op, dtype, p, st);
+    if (e == hipSuccess && p.splits > 1) e = launch_join(op, dtype, p, st);
+    return status(e);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t eden_checkpoint_bytes(uint64_t rows, uint64_t cols) {
+    if (rows > kMostSize || cols > kMostSize) return 0;
+    return rows * blocks_of(cols) * (kBlock + 1);
+}
+
+int eden_checkpoint_save(const void *x, uint64_t ldx, uint64_t rows, uint64_t cols, uint32_t dtype, void *checkpoint, size_t capacity, void *stream) {
+    if (!known_type(dtype) || rows > kMostSize || cols > kMostSize || !launchable(rows, cols)) return EDEN_ERR_INVALID_ARG;
+    if (!matrix_ok(x, ldx, rows, cols, bytes_of(dtype)) || !checkpoint_ok(checkpoint, rows, cols)) return EDEN_ERR_INVALID_ARG;
+    if (capacity < eden_checkpoint_bytes(rows, cols)) return EDEN_ERR_CAPACITY;
+    if (rows == 0 || cols == 0) return EDEN_OK;
+    uint8_t *codes = static_cast<uint8_t *>(checkpoint);
+    return status(launch_save(dtype, x, ldx, (uint32_t)rows, (uint32_t)cols, codes, codes + codes_bytes(rows, cols), static_cast<hipStream_t>(stream)));
+}
+
+int eden_checkpoint_restore(const void *checkpoint, uint64_t rows, uint64_t cols, uint32_t dtype, void *x, uint64_t ldx, void *stream) {
+    if (!known_type(dtype) || rows > kMostSize || cols > kMostSize || !launchable(rows, cols)) return EDEN_ERR_INVALID_ARG;
+    if (!matrix_ok(x, ldx, rows, cols, bytes_of(dtype)) || !checkpoint_ok(checkpoint, rows, cols)) return EDEN_ERR_INVALID_ARG;
+    if (rows == 0 || cols == 0) return EDEN_OK;
+    const uint8_t *codes = static_cast<const uint8_t *>(checkpoint);
+    return status(launch_restore(dtype, codes, codes + codes_bytes(rows, cols), (uint32_t)rows, (uint32_t)cols, x, ldx, static_cast<hipStream_t>(stream)));
+}
+
+size_t eden_layers_workspace_bytes(uint64_t rows, uint64_t cols, uint64_t depth, uint32_t dtype) {
+    if (!known_type(dtype) || rows > kMostSize || cols > kMostSize || depth > kMostSize) return 0;
+    const uint64_t splits = splits_of(rows, cols, depth);
+    return splits > 1 ? partial_bytes(rows, cols, splits) : 0;
+}
+
+int eden_linear(const void *x, uint64_t ldx, const void *w, uint64_t ldw, const void *bias, const void *residual, uint64_t ldr, void *y, uint64_t ldy,
+                void *z_checkpoint, size_t z_capacity, uint64_t m, uint64_t n, uint64_t k, uint32_t dtype, uint32_t activation, void *workspace,
+                size_t workspace_bytes, void *stream) {
+    if (!known_type(dtype) || activation > EDEN_ACT_SILU || m > kMostSize || n > kMostSize || k > kMostSize) return EDEN_ERR_INVALID_ARG;
+    const size_t e = bytes_of(dtype);
+    if (!matrix_ok(x, ldx, m, k, e) || !matrix_ok(w, ldw, n, k, e) || !matrix_ok(y, ldy, m, n, e)) return EDEN_ERR_INVALID_ARG;
+    if ((bias && !matrix_ok(bias, n, 1, n, e)) || (residual && !matrix_ok(residual, ldr, m, n, e)) || (z_checkpoint && !checkpoint_ok(z_checkpoint, m, n)))
+        return EDEN_ERR_INVALID_ARG;
+    if (z_checkpoint && z_capacity < eden_checkpoint_bytes(m, n)) return EDEN_ERR_CAPACITY;
+    if (m == 0 || n == 0) return EDEN_OK;
+    Product p = {};
+    p.a = x, p.lda = ldx, p.b = w, p.ldb = ldw;
+    p.rows = (uint32_t)m, p.cols = (uint32_t)n, p.depth = (uint32_t)k;
+    p.finish.bias = bias, p.finish.residual = residual, p.finish.ld_residual = ldr, p.finish.out = y, p.finish.ld_out = ldy;
+    p.finish.activation = activation, p.finish.blocks = (uint32_t)blocks_of(n);
+    if (z_checkpoint) {
+        p.finish.codes_out = static_cast<uint8_t *>(z_checkpoint);
+        p.finish.exps_out = p.finish.codes_out + codes_bytes(m, n);
+    }
+    return run(kForward, dtype, p, workspace, workspace_bytes, stream);
+}
+
+int eden_linear_weight_grad(const void *dy, uint64_t ldy, const void *x_checkpoint, float *dw, uint64_t ldw, float *bias_grad, uint64_t m, uint64_t n,
+                            uint64_t k, uint32_t dtype, int accumulate, void *workspace, size_t workspace_bytes, void *stream) {
+    if (!known_type(dtype) || m > kMostSize || n > kMostSize || k > kMostSize) return EDEN_ERR_INVALID_ARG;
+    if (!matrix_ok(dy, ldy, m, n, bytes_of(dtype)) || !checkpoint_ok(x_checkpoint, m, k) || !matrix_ok(dw, ldw, n, k, 4)) return EDEN_ERR_INVALID_ARG;
+    if (bias_grad && !matrix_ok(bias_grad, n, 1, n, 4)) return EDEN_ERR_INVALID_ARG;
+    if (n == 0 || (k == 0 && !bias_grad)) return EDEN_OK;
+    Product p = {};
+    p.a = dy, p.lda = ldy, p.b = x_checkpoint, p.ldb = blocks_of(k) * kBlock;
+    p.b_blocks = (uint32_t)blocks_of(k);
+    p.b_exps = static_cast<const uint8_t *>(x_checkpoint) + codes_bytes(m, k);
+    p.rows = (uint32_t)n, p.cols = (uint32_t)k, p.depth = (uint32_t)m;
+    p.finish.out = dw, p.finish.ld_out = ldw, p.finish.accumulate = accumulate != 0;
+    p.row_sums = bias_grad;
+    return run(kWeightGrad, dtype, p, workspace, workspace_bytes, stream);
+}
+
+int eden_linear_input_grad(const void *dz, uint64_t ldz, const void *w, uint64_t ldw, const void *z_checkpoint, uint32_t activation, const void *residual,
+                           uint64_t ldr, void *dx, uint64_t ldx, uint64_t m, uint64_t n, uint64_t k, uint32_t dtype, void *workspace,
+                           size_t workspace_bytes, void *stream) {
+    if (!known_type(dtype) || activation > EDEN_ACT_SILU || m > kMostSize || n > kMostSize || k > kMostSize) return EDEN_ERR_INVALID_ARG;
+    const size_t e = bytes_of(dtype);
+    if (!matrix_ok(dz, ldz, m, n, e) || !matrix_ok(w, ldw, n, k, e) || !matrix_ok(dx, ldx, m, k, e)) return EDEN_ERR_INVALID_ARG;
+    if (residual && !matrix_ok(residual, ldr, m, k, e)) return EDEN_ERR_INVALID_ARG;
+    const bool slopes = activation != EDEN_ACT_NONE;
+    if (slopes ? !checkpoint_ok(z_checkpoint, m, k) : z_checkpoint != nullptr) return EDEN_ERR_INVALID_ARG;
+    if (m == 0 || k == 0) return EDEN_OK;
+    Product p = {};
+    p.a = dz, p.lda = ldz, p.b = w, p.ldb = ldw;
+    p.rows = (uint32_t)m, p.cols = (uint32_t)k, p.depth = (uint32_t)n;
+    p.finish.residual = residual, p.finish.ld_residual = ldr, p.finish.out = dx, p.finish.ld_out = ldx;
+    p.finish.activation = activation, p.finish.blocks = (uint32_t)blocks_of(k);
+    if (slopes) {
+        p.finish.codes_in = static_cast<const uint8_t *>(z_checkpoint);
+        p.finish.exps_in = p.finish.codes_in + codes_bytes(m, k);
+    }
+    return run(kInputGrad, dtype, p, workspace, workspace_bytes, stream);
+}
+
+int eden_activation_grad(const void *dy, uint64_t ldy, const void *z_checkpoint, uint32_t activation, void *dz, uint64_t ldz, uint64_t rows,
+                         uint64_t cols, uint32_t dtype, void *stream) {
+    if (!known_type(dtype) || activation > EDEN_ACT_SILU || rows > kMostSize || cols > kMostSize || !launchable(rows, cols)) return EDEN_ERR_INVALID_ARG;
+    const size_t e = bytes_of(dtype);
+    if (!matrix_ok(dy, ldy, rows, cols, e) || !matrix_ok(dz, ldz, rows, cols, e) || !checkpoint_ok(z_checkpoint, rows, cols)) return EDEN_ERR_INVALID_ARG;
+    if (rows == 0 || cols == 0) return EDEN_OK;
+    const uint8_t *codes = static_cast<const uint8_t *>(z_checkpoint);
+    return status(launch_activation_grad(dtype, dy, ldy, codes, codes + codes_bytes(rows, cols), activation, dz, ldz, (uint32_t)rows, (uint32_t)cols,
+                                         static_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"

@@ -1,0 +1,208 @@
+// Device-side building blocks of the layer kernels (gfx950, wave64): operand types, the 8-bit checkpoint, activations, and the
+// end of a product (bias, activation, residual, slope, checkpoint).
+#ifndef EDEN_LAYERS_DEVICE_H
+#define EDEN_LAYERS_DEVICE_H
+
+#include <hip/hip_runtime.h>
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "eden_layers.h"
+
+namespace eden_layers {
+
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+
+constexpr int kBlock = 32;                  // columns of a checkpoint block
+
+__host__ __device__ inline size_t blocks_of(size_t cols) { return (cols + kBlock - 1) / kBlock; }
+
+// ---- elements
+
+template <uint32_t DTYPE> struct Elem;
+template <> struct Elem<EDEN_F32> {
+    using type = float;
+    static constexpr int kBytes = 4;
+};
+template <> struct Elem<EDEN_F16> {
+    using type = _Float16;
+    static constexpr int kBytes = 2;
+};
+template <> struct Elem<EDEN_BF16> {
+    using type = __bf16;
+    static constexpr int kBytes = 2;
+};
+
+// N consecutive elements from any address of their own alignment (the part reads and writes unaligned vectors); elements from
+// `valid` on are 0 / not written.
+template <class T, int N> struct Vec { T v[N]; };
+
+template <class T, int N> __device__ inline Vec<T, N> load_some(const T *p, int valid) {
+    Vec<T, N> r;
+    if (valid >= N) {
+        __builtin_memcpy(&r, p, sizeof(r));
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) r.v[i] = i < valid ? p[i] : (T)0.0f;
+    }
+    return r;
+}
+template <class T, int N> __device__ inline void store_some(T *p, const Vec<T, N> &r, int valid) {
+    if (valid >= N) {
+        __builtin_memcpy(p, &r, sizeof(r));
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < valid) p[i] = r.v[i];
+    }
+}
+
+// ---- 8-bit checkpoint
+
+// Exponent byte of a block from the bits of its largest |x| (as whole numbers: NaN above infinity above all else).
+__device__ inline uint32_t block_exponent(uint32_t largest_bits) {
+    const uint32_t e = largest_bits >> 23;
+    return e == 255u ? 255u : (uint32_t)max((int)e - 6, 1);
+}
+// 2^(127 - t), what the values of a block are multiplied by: exact.  A block that is not finite (t = 255) gets 0 and codes of its own.
+__device__ inline float block_inverse(uint32_t t) { return t == 255u ? 0.0f : __uint_as_float((254u - t) << 23); }
+// 2^(t - 127); NaN for t = 255.
+__device__ inline float block_unit(uint32_t t) { return t == 255u ? __uint_as_float(0x7FC00000u) : __uint_as_float(t << 23); }
+
+__device__ inline uint32_t code_of(float x, float inverse) {
+    // x * inverse is below 128 in size; where the block is not finite the product may be NaN, which the clip turns into a number
+    const float q = fminf(fmaxf(rintf(x * inverse), -127.0f), 127.0f);
+    return (uint32_t)(int)q & 0xFFu;
+}
+__device__ inline uint32_t codes4(const float (&x)[4], uint32_t t) {
+    const float inverse = block_inverse(t);
+    const uint32_t c = code_of(x[0], inverse) | code_of(x[1], inverse) << 8 | code_of(x[2], inverse) << 16 | code_of(x[3], inverse) << 24;
+    return t == 255u ? 0u : c;
+}
+// Four codes' values.  Exact: seven bits times a power of two.
+__device__ inline void values4(uint32_t codes, float unit, float (&x)[4]) {
+    x[0] = (float)(int8_t)(codes & 0xFFu) * unit;
+    x[1] = (float)(int8_t)((codes >> 8) & 0xFFu) * unit;
+    x[2] = (float)(int8_t)((codes >> 16) & 0xFFu) * unit;
+    x[3] = (float)(int8_t)(codes >> 24) * unit;
+}
+__device__ inline uint32_t magnitude_bits(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
+
+// ---- activations
+
+constexpr float kSqrtHalf = 0.70710678118654752f;
+constexpr float kInvSqrt2Pi = 0.39894228040143268f;
+constexpr float kSqrt2OverPi = 0.79788456080286536f;
+constexpr float kTanhCubic = 0.044715f;
+
+// exp and 1 / x: FULL (fp32 results) to an ulp or two; else (results with at most 11 bits) in one instruction each, off by |x| 2^-24 and 2^-23
+template <bool FULL> __device__ inline float exp_of(float x) { return FULL ? expf(x) : __expf(x); }
+template <bool FULL> __device__ inline float over(float a, float b) { return FULL ? a / b : a * __builtin_amdgcn_rcpf(b); }
+
+template <bool FULL> __device__ inline float activate(float z, uint32_t act) {
+    switch (act) {
+    case EDEN_ACT_RELU: return z > 0.0f ? z : (z != z ? z : 0.0f);
+    case EDEN_ACT_GELU: return 0.5f * z * (1.0f + erff(z * kSqrtHalf));
+    case EDEN_ACT_GELU_TANH:                                       // (1 + tanh u) / 2 = 1 / (1 + exp(-2u))
+        return over<FULL>(z, 1.0f + exp_of<FULL>(-2.0f * kSqrt2OverPi * (z + kTanhCubic * z * z * z)));
+    case EDEN_ACT_SILU: return over<FULL>(z, 1.0f + exp_of<FULL>(-z));
+    default: return z;
+    }
+}
+// Derivative at a checkpoint's value: finite, or NaN for NaN.
+template <bool FULL> __device__ inline float slope(float z, uint32_t act) {
+    switch (act) {
+    case EDEN_ACT_RELU: return z > 0.0f ? 1.0f : (z != z ? z : 0.0f);
+    case EDEN_ACT_GELU: return 0.5f * (1.0f + erff(z * kSqrtHalf)) + z * kInvSqrt2Pi * exp_of<FULL>(-0.5f * z * z);
+    case EDEN_ACT_GELU_TANH: {
+        const float c = fminf(fmaxf(z, -12.0f), 12.0f);            // the slope is 0 or 1 in fp32 from there on, and z^3 stays finite
+        const float p = over<FULL>(1.0f, 1.0f + exp_of<FULL>(-2.0f * kSqrt2OverPi * (c + kTanhCubic * c * c * c)));
+        const float s = p + c * p * (1.0f - p) * (2.0f * kSqrt2OverPi) * (1.0f + 3.0f * kTanhCubic * c * c);
+        return z != z ? z : s;
+    }
+    case EDEN_ACT_SILU: {
+        const float p = over<FULL>(1.0f, 1.0f + exp_of<FULL>(-z));
+        return p * (1.0f + z * (1.0f - p));
+    }
+    default: return 1.0f;
+    }
+}
+
+// ---- the end of a product: from fp32 sums to what the call returns
+
+struct Finish {
+    const void *bias;              // per column, dtype (eden_linear)
+    const void *residual;          // dtype
+    void *out;                     // dtype, or fp32 (eden_linear_weight_grad)
+    size_t ld_residual, ld_out;
+    uint8_t *codes_out, *exps_out; // checkpoint of z to be written (eden_linear)
+    const uint8_t *codes_in, *exps_in;  // checkpoint of z^ to be read (eden_linear_input_grad)
+    uint32_t blocks;               // of a row of either checkpoint
+    uint32_t activation;
+    uint32_t accumulate;           // eden_linear_weight_grad: add to what is there
+};
+
+enum Op : int { kForward = 0, kInputGrad = 1, kWeightGrad = 2 };
+
+// z of four consecutive columns, before the checkpoint is taken
+template <int OP, uint32_t DTYPE> __device__ inline void finish_bias(const Finish &f, uint32_t col, int valid, float (&v)[4]) {
+    using T = typename Elem<DTYPE>::type;
+    if constexpr (OP == kForward) {
+        if (f.bias) {
+            const auto b = load_some<T, 4>(static_cast<const T *>(f.bias) + col, valid);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] += (float)b.v[i];
+        }
+    }
+}
+// ... and what follows.  `valid`: columns of the four that the result has (the caller sees to it that there is one).
+template <int OP, uint32_t DTYPE>
+__device__ inline void finish_store(const Finish &f, uint32_t row, uint32_t col, int valid, float (&v)[4]) {
+    if constexpr (OP == kWeightGrad) {
+        float *out = static_cast<float *>(f.out) + (size_t)row * f.ld_out + col;
+        Vec<float, 4> r;
+        if (f.accumulate) {
+            r = load_some<float, 4>(out, valid);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r.v[i] += v[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r.v[i] = v[i];
+        }
+        store_some<float, 4>(out, r, valid);
+    } else {
+        using T = typename Elem<DTYPE>::type;
+        if constexpr (OP == kForward) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = activate<DTYPE == EDEN_F32>(v[i], f.activation);
+        } else if (f.codes_in) {
+            const uint32_t block = col / kBlock;
+            float z[4];
+            uint32_t codes;
+            __builtin_memcpy(&codes, f.codes_in + ((size_t)row * f.blocks + block) * kBlock + col % kBlock, 4);
+            values4(codes, block_unit(f.exps_in[(size_t)row * f.blocks + block]), z);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] *= slope<DTYPE == EDEN_F32>(z[i], f.activation);
+        }
+        if (f.residual) {
+            const auto a = load_some<T, 4>(static_cast<const T *>(f.residual) + (size_t)row * f.ld_residual + col, valid);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] += (float)a.v[i];
+        }
+        Vec<T, 4> r;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.v[i] = (T)v[i];
+        store_some<T, 4>(static_cast<T *>(f.out) + (size_t)row * f.ld_out + col, r, valid);
+    }
+}
+
+}  // namespace eden_layers
+
+#endif  // EDEN_LAYERS_DEVICE_H

@@ -1,0 +1,299 @@
+"""Layer operators (include/eden_layers.h): a linear layer that is trained from 8-bit activation checkpoints.
+
+    y, z = linear(x, w, bias, activation="gelu", residual=r, checkpoint=True)     # z: the activation's input in 8 bits
+    kept = save_checkpoint(x)                                                     # the layer's input in 8 bits
+    dz = activation_grad(dy, z, "gelu")
+    dw, db = linear_weight_grad(dz, kept, bias=True)                              # fp32: what Context.encode takes
+    dx = linear_input_grad(dz, w)       # or, through the activation in front of the layer, activation=, checkpoint=
+
+Tensors are torch CUDA(HIP) tensors of float32, float16 or bfloat16 with unit distance between the last dimension's elements; dimensions
+in front of it are rows.  Argument checks, allocation and marshalling only: every step runs in the HIP kernels, on the current
+stream or the one given.  What does not fit raises EdenError (ERR_INVALID_ARG) before anything is launched.
+"""
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from . import eden
+from .eden import EdenError
+
+F32, F16, BF16 = 0, 1, 2
+BLOCK = 32                                                        # columns of a checkpoint block
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+EXPORTS = ["eden_checkpoint_bytes", "eden_checkpoint_save", "eden_checkpoint_restore", "eden_layers_workspace_bytes", "eden_linear",
+           "eden_linear_weight_grad", "eden_linear_input_grad", "eden_activation_grad"]
+
+_DTYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
+_lib = None
+
+
+def lib():
+    """The built library with this header's entry points declared."""
+    global _lib
+    if _lib is not None:
+        return _lib
+    L = eden.lib()
+    vp, u64, u32, sz, ci = ctypes.c_void_p, ctypes.c_uint64, ctypes.c_uint32, ctypes.c_size_t, ctypes.c_int
+    L.eden_checkpoint_bytes.argtypes = [u64, u64]
+    L.eden_checkpoint_bytes.restype = sz
+    L.eden_layers_workspace_bytes.argtypes = [u64, u64, u64, u32]
+    L.eden_layers_workspace_bytes.restype = sz
+    for name, args in (("eden_checkpoint_save", [vp, u64, u64, u64, u32, vp, sz, vp]),
+                       ("eden_checkpoint_restore", [vp, u64, u64, u32, vp, u64, vp]),
+                       ("eden_linear", [vp, u64, vp, u64, vp, vp, u64, vp, u64, vp, sz, u64, u64, u64, u32, u32, vp, sz, vp]),
+                       ("eden_linear_weight_grad", [vp, u64, vp, vp, u64, vp, u64, u64, u64, u32, ci, vp, sz, vp]),
+                       ("eden_linear_input_grad", [vp, u64, vp, u64, vp, u32, vp, u64, vp, u64, u64, u64, u64, u32, vp, sz, vp]),
+                       ("eden_activation_grad", [vp, u64, vp, u32, vp, u64, u64, u64, u32, vp])):
+        f = getattr(L, name)
+        f.argtypes, f.restype = args, ci
+    _lib = L
+    return L
+
+
+def _refuse(what):
+    raise EdenError(eden.ERR_INVALID_ARG, what)
+
+
+def _check(rc, what):
+    if rc != eden.OK:
+        raise EdenError(rc, what)
+
+
+def _dtype(t, what):
+    code = _DTYPES.get(t.dtype)
+    if code is None or not t.is_cuda:
+        _refuse(f"{what}: a float32, float16 or bfloat16 tensor on the GPU is needed, got {t.dtype} on {t.device}")
+    return code
+
+
+def _rows(t, what):
+    """(address, distance between rows, rows, columns) of a tensor seen as a matrix of its last dimension."""
+    if t.dim() == 2:
+        rows, cols = t.shape
+        ld, unit = t.stride()
+    else:
+        if t.dim() == 0:
+            _refuse(f"{what}: at least one dimension is needed")
+        cols = t.shape[-1]
+        if t.numel() == 0:                                        # nothing is read or written: only the sizes count
+            rows = 1
+            for s in t.shape[:-1]:
+                rows *= s
+            return t.data_ptr(), cols, rows, cols
+        try:
+            m = t.view(-1, cols)
+        except RuntimeError:
+            _refuse(f"{what}: the dimensions in front of the last are not rows at one distance")
+        rows, (ld, unit) = m.shape[0], m.stride()
+    if rows and cols and ((cols > 1 and unit != 1) or (rows > 1 and ld < cols)):
+        _refuse(f"{what}: rows must not overlap and the last dimension's elements must be neighbours, strides {tuple(t.stride())}")
+    return t.data_ptr(), ld if rows > 1 else cols, rows, cols
+
+
+def _same(t, like, what):
+    if t.dtype is not like.dtype or t.device != like.device:
+        _refuse(f"{what}: {t.dtype} on {t.device}, expected {like.dtype} on {like.device}")
+
+
+def _output(out, shape, dtype, device, what):
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if tuple(out.shape) != tuple(shape) or out.dtype is not dtype or out.device != device:
+        _refuse(f"{what}: {tuple(out.shape)} of {out.dtype} on {out.device}, expected {tuple(shape)} of {dtype} on {device}")
+    return out
+
+
+def _act(name, what):
+    code = ACTIVATIONS.get(name)
+    if code is None:
+        _refuse(f"{what}: unknown activation {name!r}")
+    return code
+
+
+class _On:
+    """Makes the tensors' device current and, where a stream is given, has torch allocate on it, so that memory freed on
+    return is reused behind the call's kernels."""
+
+    __slots__ = ("stacked",)
+
+    def __init__(self, device, stream):
+        self.stacked = []
+        if stream is not None:
+            if stream.device != device:
+                _refuse(f"stream on {stream.device}, tensors on {device}")
+            self.stacked.append(torch.cuda.stream(stream))
+        elif torch.cuda.current_device() != device.index:
+            self.stacked.append(torch.cuda.device(device))
+
+    def __enter__(self):
+        for c in self.stacked:
+            c.__enter__()
+
+    def __exit__(self, *e):
+        for c in reversed(self.stacked):
+            c.__exit__(*e)
+
+
+def _workspace(L, rows, cols, depth, dtype, device):
+    size = L.eden_layers_workspace_bytes(rows, cols, depth, dtype)
+    if not size:
+        return None, None, 0
+    t = torch.empty(size, dtype=torch.uint8, device=device)
+    return t, t.data_ptr(), size
+
+
+def checkpoint_bytes(rows: int, cols: int) -> int:
+    return int(lib().eden_checkpoint_bytes(rows, cols))
+
+
+class Checkpoint:
+    """The 8-bit checkpoint of a rows x cols matrix in a buffer of checkpoint_bytes(rows, cols) bytes (33 for 32 values)."""
+
+    __slots__ = ("buffer", "rows", "cols")
+
+    def __init__(self, buffer, rows: int, cols: int):
+        need = rows * -(-cols // BLOCK) * (BLOCK + 1)
+        if buffer.dtype is not torch.uint8 or not buffer.is_cuda or not buffer.is_contiguous() or buffer.numel() < need:
+            _refuse(f"Checkpoint: a contiguous uint8 buffer of {need} bytes on the GPU is needed")
+        self.buffer, self.rows, self.cols = buffer, rows, cols
+
+    def restore(self, dtype=torch.bfloat16, out=None, stream=None):
+        """The values it stands for (exact in bfloat16 and float32)."""
+        if out is not None:
+            dtype = out.dtype
+        if dtype not in _DTYPES:
+            _refuse(f"restore: {dtype}")
+        with _On(self.buffer.device, stream):
+            out = _output(out, (self.rows, self.cols) if out is None else out.shape, dtype, self.buffer.device, "restore: out")
+            p, ld, rows, cols = _rows(out, "restore: out")
+            if (rows, cols) != (self.rows, self.cols):
+                _refuse(f"restore: out is {rows} x {cols}, the checkpoint {self.rows} x {self.cols}")
+            _check(lib().eden_checkpoint_restore(self.buffer.data_ptr(), rows, cols, _DTYPES[dtype], p, ld, eden._stream_ptr(stream)),
+                   "eden_checkpoint_restore")
+        return out
+
+
+def _new_checkpoint(into, rows, cols, device):
+    if into is None:
+        return Checkpoint(torch.empty(rows * -(-cols // BLOCK) * (BLOCK + 1), dtype=torch.uint8, device=device), rows, cols)
+    if (into.rows, into.cols) != (rows, cols) or into.buffer.device != device:
+        _refuse(f"checkpoint of {into.rows} x {into.cols} on {into.buffer.device}, expected {rows} x {cols} on {device}")
+    return into
+
+
+def _saved(c, rows, cols, device, what):
+    if (c.rows, c.cols) != (rows, cols) or c.buffer.device != device:
+        _refuse(f"{what}: checkpoint of {c.rows} x {c.cols} on {c.buffer.device}, expected {rows} x {cols} on {device}")
+    return c.buffer.data_ptr()
+
+
+def save_checkpoint(x, into=None, stream=None) -> Checkpoint:
+    """The 8-bit checkpoint of x; `into`: a Checkpoint of the same size that is overwritten."""
+    dtype = _dtype(x, "save_checkpoint: x")
+    p, ld, rows, cols = _rows(x, "save_checkpoint: x")
+    with _On(x.device, stream):
+        c = _new_checkpoint(into, rows, cols, x.device)
+        _check(lib().eden_checkpoint_save(p, ld, rows, cols, dtype, c.buffer.data_ptr(), c.buffer.numel(), eden._stream_ptr(stream)),
+               "eden_checkpoint_save")
+    return c
+
+
+def linear(x, w, bias=None, activation: str = "none", residual=None, checkpoint=False, out=None, stream=None):
+    """act(x w^T + bias) + residual.  `checkpoint`: True or a Checkpoint to be overwritten: returns (y, checkpoint of x w^T + bias)."""
+    L = lib()
+    dtype = _dtype(x, "linear: x")
+    act = _act(activation, "linear")
+    xp, ldx, m, k = _rows(x, "linear: x")
+    _same(w, x, "linear: w")
+    if w.dim() != 2 or w.shape[1] != k:
+        _refuse(f"linear: w is {tuple(w.shape)}, x has {k} columns")
+    wp, ldw, n, _ = _rows(w, "linear: w")
+    bp = rp = None
+    ldr = n
+    if bias is not None:
+        _same(bias, x, "linear: bias")
+        if tuple(bias.shape) != (n,) or (n > 1 and bias.stride(0) != 1):
+            _refuse(f"linear: bias is {tuple(bias.shape)} with stride {bias.stride()}, expected {n} neighbours")
+        bp = bias.data_ptr()
+    shape = x.shape[:-1] + (n,)
+    if residual is not None:
+        _same(residual, x, "linear: residual")
+        if residual.shape != shape:
+            _refuse(f"linear: residual is {tuple(residual.shape)}, expected {tuple(shape)}")
+        rp, ldr, _, _ = _rows(residual, "linear: residual")
+    with _On(x.device, stream):
+        y = _output(out, shape, x.dtype, x.device, "linear: out")
+        yp, ldy, _, _ = _rows(y, "linear: out")
+        c = None if checkpoint is False or checkpoint is None else _new_checkpoint(None if checkpoint is True else checkpoint, m, n, x.device)
+        ws, wsp, size = _workspace(L, m, n, k, dtype, x.device)
+        _check(L.eden_linear(xp, ldx, wp, ldw, bp, rp, ldr, yp, ldy, c.buffer.data_ptr() if c else None, c.buffer.numel() if c else 0, m, n, k,
+                             dtype, act, wsp, size, eden._stream_ptr(stream)), "eden_linear")
+    return (y, c) if c is not None else y
+
+
+def linear_weight_grad(dy, saved: Checkpoint, bias: bool = False, out=None, bias_out=None, accumulate: bool = False, stream=None):
+    """dy^T x (fp32) from the checkpoint of x; with `bias` (dw, sum of dy's rows).  `out`, `bias_out`: where to write them, for instance
+    parts of the vector that Context.encode takes; `accumulate`: add to what they hold."""
+    L = lib()
+    dtype = _dtype(dy, "linear_weight_grad: dy")
+    dp, ldy, m, n = _rows(dy, "linear_weight_grad: dy")
+    k = saved.cols
+    sp = _saved(saved, m, k, dy.device, "linear_weight_grad")
+    if accumulate and (out is None or (bias and bias_out is None)):
+        _refuse("linear_weight_grad: nothing to accumulate in")
+    with _On(dy.device, stream):
+        dw = _output(out, (n, k), torch.float32, dy.device, "linear_weight_grad: out")
+        wp, ldw, _, _ = _rows(dw, "linear_weight_grad: out")
+        db = None
+        if bias or bias_out is not None:
+            db = _output(bias_out, (n,), torch.float32, dy.device, "linear_weight_grad: bias_out")
+            if n > 1 and db.stride(0) != 1:
+                _refuse("linear_weight_grad: bias_out's elements must be neighbours")
+        ws, wsp, size = _workspace(L, n, k, m, dtype, dy.device)
+        _check(L.eden_linear_weight_grad(dp, ldy, sp, wp, ldw, db.data_ptr() if db is not None else None, m, n, k, dtype, 1 if accumulate else 0, wsp, size,
+                                         eden._stream_ptr(stream)), "eden_linear_weight_grad")
+    return (dw, db) if db is not None else dw
+
+
+def linear_input_grad(dz, w, activation: str = "none", checkpoint: Checkpoint = None, residual=None, out=None, stream=None):
+    """(dz w) * act'(z) + residual; z: the checkpoint of the input of the activation in front of the layer (none without one)."""
+    L = lib()
+    dtype = _dtype(dz, "linear_input_grad: dz")
+    act = _act(activation, "linear_input_grad")
+    dp, ldz, m, n = _rows(dz, "linear_input_grad: dz")
+    _same(w, dz, "linear_input_grad: w")
+    if w.dim() != 2 or w.shape[0] != n:
+        _refuse(f"linear_input_grad: w is {tuple(w.shape)}, dz has {n} columns")
+    wp, ldw, _, k = _rows(w, "linear_input_grad: w")
+    if (checkpoint is None) != (act == 0):
+        _refuse("linear_input_grad: an activation and the checkpoint of its input go together")
+    sp = None if checkpoint is None else _saved(checkpoint, m, k, dz.device, "linear_input_grad")
+    rp, ldr = None, k
+    shape = dz.shape[:-1] + (k,)
+    if residual is not None:
+        _same(residual, dz, "linear_input_grad: residual")
+        if residual.shape != shape:
+            _refuse(f"linear_input_grad: residual is {tuple(residual.shape)}, expected {tuple(shape)}")
+        rp, ldr, _, _ = _rows(residual, "linear_input_grad: residual")
+    with _On(dz.device, stream):
+        dx = _output(out, shape, dz.dtype, dz.device, "linear_input_grad: out")
+        xp, ldx, _, _ = _rows(dx, "linear_input_grad: out")
+        ws, wsp, size = _workspace(L, m, k, n, dtype, dz.device)
+        _check(L.eden_linear_input_grad(dp, ldz, wp, ldw, sp, act, rp, ldr, xp, ldx, m, n, k, dtype, wsp, size, eden._stream_ptr(stream)),
+               "eden_linear_input_grad")
+    return dx
+
+
+def activation_grad(dy, saved: Checkpoint, activation: str, out=None, stream=None):
+    """dy * act'(z), z from its checkpoint."""
+    dtype = _dtype(dy, "activation_grad: dy")
+    act = _act(activation, "activation_grad")
+    dp, ldy, rows, cols = _rows(dy, "activation_grad: dy")
+    sp = _saved(saved, rows, cols, dy.device, "activation_grad")
+    with _On(dy.device, stream):
+        dz = _output(out, dy.shape, dy.dtype, dy.device, "activation_grad: out")
+        zp, ldz, _, _ = _rows(dz, "activation_grad: out")
+        _check(lib().eden_activation_grad(dp, ldy, sp, act, zp, ldz, rows, cols, dtype, eden._stream_ptr(stream)), "eden_activation_grad")
+    return dz
