@@ -39,11 +39,28 @@ uint64_t splits_of(uint64_t rows, uint64_t cols, uint64_t depth) {
     return s < 1 ? 1 : s > 64 ? 64 : s;
 }
 
+// Rows that start at, and hold, whole 16-byte pieces, and offsets inside a tile that 31 bits hold
+bool whole_pieces(const void *p, uint64_t ld, uint64_t inner) {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0 && inner % 8 == 0 && ld < (1u << 21);
+}
+// Whether the kernel of 256 x 256 tiles takes a product.
+bool is_large(Op op, uint32_t dtype, const Product &p) {
+    if (dtype == EDEN_F32 || (op == kWeightGrad && dtype == EDEN_F16) || p.depth == 0 || p.cols == 0) return false;
+    const uint64_t tiles = (uint64_t)((p.rows + kLargeTile - 1) / kLargeTile) * ((p.cols + kLargeTile - 1) / kLargeTile);
+    if (tiles < 192 || tiles > kMostGroups) return false;
+    if (!whole_pieces(p.a, p.lda, op == kWeightGrad ? p.rows : p.depth)) return false;
+    return op == kWeightGrad ? p.ldb < (1u << 24) : whole_pieces(p.b, p.ldb, op == kForward ? p.depth : p.cols);
+}
+
 // Launches a product whose operands and end are set.
 int run(Op op, uint32_t dtype, Product &p, void *workspace, size_t workspace_bytes, void *stream) {
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    uint64_t splits = splits_of(p.rows, p.cols, p.depth);
     if (reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return EDEN_ERR_INVALID_ARG;
+    if (is_large(op, dtype, p)) {
+        p.splits = 1, p.split_depth = p.depth;
+        return status(launch_large(op, dtype, p, st));
+    }
+    uint64_t splits = splits_of(p.rows, p.cols, p.depth);
     if (workspace == nullptr) workspace_bytes = 0;
     while (splits > 1 && partial_bytes(p.rows, p.cols, splits) > workspace_bytes) --splits;
     const uint64_t each = ((p.depth + splits - 1) / splits + kSplitUnit - 1) / kSplitUnit * kSplitUnit;

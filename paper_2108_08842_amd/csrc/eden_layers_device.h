@@ -8,6 +8,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "eden_layers.h"
 
 namespace eden_layers {
@@ -16,6 +18,7 @@ typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
@@ -106,33 +109,65 @@ constexpr float kTanhCubic = 0.044715f;
 template <bool FULL> __device__ inline float exp_of(float x) { return FULL ? expf(x) : __expf(x); }
 template <bool FULL> __device__ inline float over(float a, float b) { return FULL ? a / b : a * __builtin_amdgcn_rcpf(b); }
 
-template <bool FULL> __device__ inline float activate(float z, uint32_t act) {
-    switch (act) {
-    case EDEN_ACT_RELU: return z > 0.0f ? z : (z != z ? z : 0.0f);
-    case EDEN_ACT_GELU: return 0.5f * z * (1.0f + erff(z * kSqrtHalf));
-    case EDEN_ACT_GELU_TANH:                                       // (1 + tanh u) / 2 = 1 / (1 + exp(-2u))
+template <uint32_t ACT, bool FULL> __device__ inline float activate_as(float z) {
+    if constexpr (ACT == EDEN_ACT_RELU) return z > 0.0f ? z : (z != z ? z : 0.0f);
+    else if constexpr (ACT == EDEN_ACT_GELU) return 0.5f * z * (1.0f + erff(z * kSqrtHalf));
+    else if constexpr (ACT == EDEN_ACT_GELU_TANH)                  // (1 + tanh u) / 2 = 1 / (1 + exp(-2u))
         return over<FULL>(z, 1.0f + exp_of<FULL>(-2.0f * kSqrt2OverPi * (z + kTanhCubic * z * z * z)));
-    case EDEN_ACT_SILU: return over<FULL>(z, 1.0f + exp_of<FULL>(-z));
-    default: return z;
-    }
+    else if constexpr (ACT == EDEN_ACT_SILU) return over<FULL>(z, 1.0f + exp_of<FULL>(-z));
+    else return z;
 }
 // Derivative at a checkpoint's value: finite, or NaN for NaN.
-template <bool FULL> __device__ inline float slope(float z, uint32_t act) {
-    switch (act) {
-    case EDEN_ACT_RELU: return z > 0.0f ? 1.0f : (z != z ? z : 0.0f);
-    case EDEN_ACT_GELU: return 0.5f * (1.0f + erff(z * kSqrtHalf)) + z * kInvSqrt2Pi * exp_of<FULL>(-0.5f * z * z);
-    case EDEN_ACT_GELU_TANH: {
+template <uint32_t ACT, bool FULL> __device__ inline float slope_as(float z) {
+    if constexpr (ACT == EDEN_ACT_RELU) return z > 0.0f ? 1.0f : (z != z ? z : 0.0f);
+    else if constexpr (ACT == EDEN_ACT_GELU) return 0.5f * (1.0f + erff(z * kSqrtHalf)) + z * kInvSqrt2Pi * exp_of<FULL>(-0.5f * z * z);
+    else if constexpr (ACT == EDEN_ACT_GELU_TANH) {
         const float c = fminf(fmaxf(z, -12.0f), 12.0f);            // the slope is 0 or 1 in fp32 from there on, and z^3 stays finite
         const float p = over<FULL>(1.0f, 1.0f + exp_of<FULL>(-2.0f * kSqrt2OverPi * (c + kTanhCubic * c * c * c)));
         const float s = p + c * p * (1.0f - p) * (2.0f * kSqrt2OverPi) * (1.0f + 3.0f * kTanhCubic * c * c);
         return z != z ? z : s;
-    }
-    case EDEN_ACT_SILU: {
+    } else if constexpr (ACT == EDEN_ACT_SILU) {
         const float p = over<FULL>(1.0f, 1.0f + exp_of<FULL>(-z));
         return p * (1.0f + z * (1.0f - p));
+    } else return 1.0f;
+}
+
+// f(std::integral_constant<uint32_t, ACT>()) for the activation `act`: one branch for all values of a thread
+template <class F> __device__ inline void for_activation(uint32_t act, F f) {
+    switch (act) {
+    case EDEN_ACT_RELU: f(std::integral_constant<uint32_t, EDEN_ACT_RELU>()); break;
+    case EDEN_ACT_GELU: f(std::integral_constant<uint32_t, EDEN_ACT_GELU>()); break;
+    case EDEN_ACT_GELU_TANH: f(std::integral_constant<uint32_t, EDEN_ACT_GELU_TANH>()); break;
+    case EDEN_ACT_SILU: f(std::integral_constant<uint32_t, EDEN_ACT_SILU>()); break;
+    default: break;
     }
-    default: return 1.0f;
-    }
+}
+template <bool FULL, int R, int C> __device__ inline void activate_all(float (&v)[R][C], uint32_t act) {
+    for_activation(act, [&](auto a) {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int c = 0; c < C; ++c) v[r][c] = activate_as<decltype(a)::value, FULL>(v[r][c]);
+    });
+}
+template <bool FULL, int R, int C> __device__ inline void multiply_slopes(float (&v)[R][C], const float (&z)[R][C], uint32_t act) {
+    for_activation(act, [&](auto a) {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int c = 0; c < C; ++c) v[r][c] *= slope_as<decltype(a)::value, FULL>(z[r][c]);
+    });
+}
+template <bool FULL> __device__ inline float activate(float z, uint32_t act) {
+    float v[1][1] = {{z}};
+    activate_all<FULL>(v, act);
+    return v[0][0];
+}
+template <bool FULL> __device__ inline float slope(float z, uint32_t act) {
+    float v[1][1] = {{1.0f}};
+    const float at[1][1] = {{z}};
+    multiply_slopes<FULL>(v, at, act);
+    return v[0][0];
 }
 
 // ---- the end of a product: from fp32 sums to what the call returns
@@ -200,6 +235,133 @@ __device__ inline void finish_store(const Finish &f, uint32_t row, uint32_t col,
 #pragma unroll
         for (int i = 0; i < 4; ++i) r.v[i] = (T)v[i];
         store_some<T, 4>(static_cast<T *>(f.out) + (size_t)row * f.ld_out + col, r, valid);
+    }
+}
+
+// The same for eight neighbouring columns at once where the result has them all: whole 16-byte pieces.
+template <int OP, uint32_t DTYPE>
+__device__ inline void finish_store8(const Finish &f, uint32_t row, uint32_t col, int valid, float (&lo)[4], float (&hi)[4]) {
+    if (OP == kWeightGrad || valid < 8) {
+        if (valid > 0) finish_store<OP, DTYPE>(f, row, col, min(valid, 4), lo);
+        if (valid > 4) finish_store<OP, DTYPE>(f, row, col + 4, valid - 4, hi);
+        return;
+    }
+    using T = typename Elem<DTYPE>::type;
+    if constexpr (OP == kForward) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            lo[i] = activate<DTYPE == EDEN_F32>(lo[i], f.activation);
+            hi[i] = activate<DTYPE == EDEN_F32>(hi[i], f.activation);
+        }
+    } else if (f.codes_in) {
+        const size_t block = (size_t)row * f.blocks + col / kBlock;
+        const u32x2 c = *reinterpret_cast<const u32x2 *>(f.codes_in + block * kBlock + col % kBlock);
+        const float unit = block_unit(f.exps_in[block]);
+        float z0[4], z1[4];
+        values4(c[0], unit, z0);
+        values4(c[1], unit, z1);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            lo[i] *= slope<DTYPE == EDEN_F32>(z0[i], f.activation);
+            hi[i] *= slope<DTYPE == EDEN_F32>(z1[i], f.activation);
+        }
+    }
+    if (f.residual) {
+        const auto a = load_some<T, 8>(static_cast<const T *>(f.residual) + (size_t)row * f.ld_residual + col, 8);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            lo[i] += (float)a.v[i];
+            hi[i] += (float)a.v[4 + i];
+        }
+    }
+    Vec<T, 8> r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        r.v[i] = (T)lo[i];
+        r.v[4 + i] = (T)hi[i];
+    }
+    store_some<T, 8>(static_cast<T *>(f.out) + (size_t)row * f.ld_out + col, r, 8);
+}
+
+// The whole end of eight neighbouring columns from `col` on of ROWS rows STEP apart, all inside the result; four lanes side by side have a checkpoint's
+// block.  The rows go through it side by side, so that their reads and exponentials overlap.
+template <int OP, uint32_t DTYPE, int ROWS, int STEP> __device__ inline void finish_inside(const Finish &f, uint32_t row, uint32_t col, float (&v)[ROWS][8]) {
+    if constexpr (OP == kWeightGrad) {
+        float *out = static_cast<float *>(f.out) + (size_t)row * f.ld_out + col;
+        if (f.accumulate) {
+            Vec<float, 8> held[ROWS];
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) held[r] = load_some<float, 8>(out + (size_t)(r * STEP) * f.ld_out, 8);
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[r][i] += held[r].v[i];
+        }
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            Vec<float, 8> to;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) to.v[i] = v[r][i];
+            store_some<float, 8>(out + (size_t)(r * STEP) * f.ld_out, to, 8);
+        }
+    } else {
+        using T = typename Elem<DTYPE>::type;
+        constexpr bool FULL = DTYPE == EDEN_F32;
+        const size_t block = (size_t)row * f.blocks + col / kBlock;
+        Vec<T, 8> added[ROWS];
+        if (f.residual) {
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) added[r] = load_some<T, 8>(static_cast<const T *>(f.residual) + (size_t)(row + r * STEP) * f.ld_residual + col, 8);
+        }
+        if constexpr (OP == kForward) {
+            if (f.bias) {
+                const auto b = load_some<T, 8>(static_cast<const T *>(f.bias) + col, 8);
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[r][i] += (float)b.v[i];
+            }
+            if (f.codes_out) {
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r) {
+                    float lo[4], hi[4];
+                    uint32_t largest = 0;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        lo[i] = v[r][i], hi[i] = v[r][4 + i];
+                        largest = max(largest, max(magnitude_bits(lo[i]), magnitude_bits(hi[i])));
+                    }
+                    largest = max(largest, (uint32_t)__shfl_xor((int)largest, 1));
+                    largest = max(largest, (uint32_t)__shfl_xor((int)largest, 2));
+                    const uint32_t t = block_exponent(largest);
+                    const size_t at = block + (size_t)(r * STEP) * f.blocks;
+                    *reinterpret_cast<u32x2 *>(f.codes_out + at * kBlock + col % kBlock) = u32x2{codes4(lo, t), codes4(hi, t)};
+                    if (col % kBlock == 0) f.exps_out[at] = (uint8_t)t;
+                }
+            }
+            activate_all<FULL>(v, f.activation);
+        } else if (f.codes_in) {
+            float z[ROWS][8];
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                const size_t at = block + (size_t)(r * STEP) * f.blocks;
+                const u32x2 c = *reinterpret_cast<const u32x2 *>(f.codes_in + at * kBlock + col % kBlock);
+                const float unit = block_unit(f.exps_in[at]);
+                float lo[4], hi[4];
+                values4(c[0], unit, lo);
+                values4(c[1], unit, hi);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) z[r][i] = lo[i], z[r][4 + i] = hi[i];
+            }
+            multiply_slopes<FULL>(v, z, f.activation);
+        }
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            Vec<T, 8> to;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) to.v[i] = (T)(f.residual ? v[r][i] + (float)added[r].v[i] : v[r][i]);
+            store_some<T, 8>(static_cast<T *>(f.out) + (size_t)(row + r * STEP) * f.ld_out + col, to, 8);
+        }
     }
 }
 

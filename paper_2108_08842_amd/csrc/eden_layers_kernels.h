@@ -24,11 +24,13 @@ struct Product {
 };
 
 constexpr uint32_t kTile = 128;       // rows and columns of the general kernel's tiles
+constexpr uint32_t kLargeTile = 256;  // of the kernel for large results
 constexpr uint32_t kSplitUnit = 64;   // the depth is split at multiples of this
 // (a result without columns still has row sums: one tile)
 __host__ __device__ inline uint32_t tiles_of(uint32_t n) { return n ? (n + kTile - 1) / kTile : 1; }
 
 hipError_t launch_tiles(Op op, uint32_t dtype, const Product &p, hipStream_t st);
+hipError_t launch_large(Op op, uint32_t dtype, const Product &p, hipStream_t st);
 hipError_t launch_join(Op op, uint32_t dtype, const Product &p, hipStream_t st);
 
 hipError_t launch_save(uint32_t dtype, const void *x, size_t ldx, uint32_t rows, uint32_t cols, uint8_t *codes, uint8_t *exps, hipStream_t st);

@@ -1,0 +1,348 @@
+// Matrix products of the layer operators where the result fills the device and rows are whole 16-byte pieces: fp16 and bf16.
+//
+// A workgroup has a tile of 256 x 256, a wave 128 x 128 of it: 256 accumulation registers, and of every byte that
+// goes from the LDS to the matrix cores 128 products, twice as many as in the general kernel.  A CU holds one such workgroup, a SIMD one wave, so the
+// wave itself keeps the matrix core fed.  It takes one product in 32 cycles, the wave issues an instruction in four, and one that its unit does not
+// accept at once holds up the products behind it: everything else goes between the products, a little at a time.
+//   memory -> LDS      an operand's tile is fetched 64 deep (whole 128-byte lines of its rows), straight into the LDS, which holds five such tiles: the two in
+//                      use, the following two, and the first of the two after that.  A tile's eight loads a wave are spread over 32 products.
+//   LDS -> registers   the operands of the next 16 deep are read while those of the last are multiplied
+//   barriers           one in 64 deep, between the last reads of two tiles and their last products
+// 16-byte pieces of a row are swapped on the way into the LDS (each lane fetches the piece that belongs to its place).  A checkpoint's codes cannot go
+// straight into the LDS: they are read into registers 64 deep ahead, turned into bf16 numbers and stored while the products run.
+#include "eden_layers_product.h"
+
+#include <utility>
+
+namespace eden_layers {
+namespace {
+
+constexpr int kThreads = 256, kSide = (int)kLargeTile, kDeep = 64, kSlots = 5;
+constexpr int kOperand = kSide * kDeep * 2;        // bytes of an operand's tile, a slot of the LDS
+constexpr int kLoads = kOperand / 16 / kThreads;   // 16-byte pieces per thread
+constexpr uint32_t kMostBytes = 0x7FFFFF00u;       // reach of a descriptor; offsets from kNowhere on lie beyond it (and below 2^32)
+constexpr uint32_t kNowhere = 0x7FFFFFF0u;
+
+using rsrc_t = __amdgpu_buffer_rsrc_t;
+typedef __attribute__((address_space(3))) char lds_char;
+
+// A barrier behind which every wave finds what all waves' loads, but for a wave's last LATER, have written into the LDS, and behind which no wave has LDS
+// reads or writes on their way.  (__syncthreads() would wait for all loads, or for none.)
+template <int LATER> __device__ inline void meet() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LATER) : "memory");
+}
+
+template <int... I, class F> __device__ inline void each_of(std::integer_sequence<int, I...>, F f) { (f(std::integral_constant<int, I>()), ...); }
+template <int N, class F> __device__ inline void each(F f) { each_of(std::make_integer_sequence<int, N>(), f); }
+
+// A descriptor in scalar registers
+__device__ inline u32x4 descriptor(const char *base, uint64_t reach) {
+    const uint64_t at = reinterpret_cast<uint64_t>(base);
+    const uint32_t bytes = reach < kMostBytes ? (uint32_t)reach : kMostBytes;
+    return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)at), (uint32_t)__builtin_amdgcn_readfirstlane((int)(at >> 32) & 0xFFFF),
+                 (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), 0x00020000u};
+}
+
+// Where a thread's pieces of an operand come from: byte offsets from the tile's first element.
+template <bool STRIDED> struct Source {
+    const char *base;
+    size_t step;               // bytes from one tile to the next
+    uint64_t reach;            // bytes from `base` to the end of what may be read
+    uint32_t offset, stride;   // of piece i: offset + i * stride
+    uint32_t depth;            // !STRIDED: depth of this lane's pieces inside a tile
+    u32x4 now;                 // of the tile that is being fetched: descriptor, this lane's first offset
+    uint32_t at;
+
+    __device__ Source(const void *p, size_t ld, uint32_t first, uint32_t count, uint32_t begin, uint32_t end, uint32_t whole, int wave, int lane) {
+        if constexpr (STRIDED) {
+            base = static_cast<const char *>(p) + ((size_t)begin * ld + first) * 2;
+            step = (size_t)kDeep * ld * 2;
+            reach = ((uint64_t)(end - begin - 1) * ld + (count - first)) * 2;
+            const uint32_t d = wave * 2 + (lane >> 5), piece = (lane & 31) ^ (4 * (d & 3));
+            offset = (uint32_t)(d * ld * 2) + piece * 16;
+            stride = (uint32_t)(8 * ld * 2);
+            depth = 0;
+        } else {
+            const uint32_t rows = min((uint32_t)kSide, count - first);
+            base = static_cast<const char *>(p) + ((size_t)first * ld + begin) * 2;
+            step = kDeep * 2;
+            reach = ((uint64_t)(rows - 1) * ld + (whole - begin)) * 2;
+            const uint32_t row = wave * 8 + (lane >> 3), piece = (lane & 7) ^ ((row >> 1) & 7);
+            offset = (uint32_t)(row * ld * 2) + piece * 16;
+            stride = (uint32_t)(32 * ld * 2);
+            depth = piece * 8;
+        }
+    }
+    // The next tile is `left` deep.  What lies beyond is read as zeros.
+    __device__ void start(uint32_t left) {
+        now = descriptor(base, reach);
+        at = (STRIDED ? 0u < left : depth < left) ? offset : kNowhere;      // (and further on)
+        base += step;
+        reach = reach > step ? reach - step : 0;
+    }
+    // Load i of the tile, into the LDS at `slot`.  (Written out: the compiler would have every LDS read wait for the loads into any other part of the LDS.
+    // It has no result in registers; meet() waits for it.)
+    __device__ void fetch(uint32_t slot, int wave, int i) const {
+        const uint32_t to = (uint32_t)__builtin_amdgcn_readfirstlane((int)(slot + (i * 4 + wave) * 1024));
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(at + i * stride), "s"(now) : "memory", "m0");
+    }
+};
+
+// A checkpoint's codes: 32 neighbouring lanes have the 32 pieces of one depth (8 codes each), a thread eight depths of a tile.  What lies
+// beyond the depths of the split is read as zeros (codes 0, unit 0).
+struct Codes {
+    const uint8_t *codes, *exps;
+    uint64_t codes_reach, exps_reach;
+    size_t ld;
+    uint32_t blocks, at, exp_at;
+    rsrc_t codes_now, exps_now;
+    u32x2 q[kLoads];
+    uint32_t t[kLoads];
+
+    __device__ Codes(const Product &p, uint32_t col0, uint32_t begin, uint32_t end, int tid)
+        : codes(static_cast<const uint8_t *>(p.b) + (size_t)begin * p.ldb + col0), exps(p.b_exps + (size_t)begin * p.b_blocks + col0 / kBlock),
+          codes_reach((uint64_t)(end - begin) * p.ldb - col0), exps_reach((uint64_t)(end - begin) * p.b_blocks - col0 / kBlock), ld(p.ldb), blocks(p.b_blocks),
+          at((tid / 32) * (uint32_t)p.ldb + tid % 32 * 8), exp_at((tid / 32) * p.b_blocks + tid % 32 / 4) {}
+    __device__ void start() {
+        codes_now = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(codes), 0, (int)(codes_reach < kMostBytes ? (uint32_t)codes_reach : kMostBytes), 0x00020000);
+        exps_now = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(exps), 0, (int)(exps_reach < kMostBytes ? (uint32_t)exps_reach : kMostBytes), 0x00020000);
+        codes += kDeep * ld;
+        exps += (size_t)kDeep * blocks;
+        codes_reach = codes_reach > kDeep * ld ? codes_reach - kDeep * ld : 0;
+        exps_reach = exps_reach > (uint64_t)kDeep * blocks ? exps_reach - (uint64_t)kDeep * blocks : 0;
+    }
+    __device__ void load(int i) {
+        q[i] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(codes_now, (int)(at + i * 8 * (uint32_t)ld), 0, 0));
+        t[i] = __builtin_amdgcn_raw_buffer_load_b8(exps_now, (int)(exp_at + i * 8 * blocks), 0, 0);
+    }
+    // Values 2 h and 2 h + 1 of piece i; the whole piece into the LDS
+    __device__ uint32_t two(int i, int h) const {
+        const float unit = block_unit(t[i]);
+        const uint32_t c = q[i][h >> 1] >> (16 * (h & 1));
+        return upper_halves((float)(int8_t)(c & 0xFFu) * unit, (float)(int8_t)((c >> 8) & 0xFFu) * unit);
+    }
+    __device__ void store(char *tile, int tid, int i, u32x4 words) const {
+        *reinterpret_cast<u32x4 *>(tile + piece_of_depth<kSide>(i * 8 + tid / 32, tid % 32)) = words;
+    }
+};
+
+// Where a lane reads an operand's tile in the LDS.  The swaps leave four different places; tiles of 32 (whole rows apart) or steps of 16 deep (whole
+// depths apart) are constant distances from them.
+template <bool STRIDED> struct Reader {
+    uint32_t at[4];
+
+    __device__ Reader(int base, int lane, int swap = 0) {          // STRIDED: tile i is number i ^ swap from `base` on
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (STRIDED) {                               // of tile i
+                const int col = base + (i ^ swap) * 32 + (lane & 16) + (lane & 3) * 4;
+                at[i] = piece_of_depth<kSide>((lane >> 5) * 8 + ((lane & 15) >> 2), col >> 3) + (col & 7) * 2;
+            } else {                                               // of step i
+                at[i] = piece_of_row<kDeep>(base + (lane & 31), 2 * i + (lane >> 5));
+            }
+        }
+    }
+    __device__ u32x4 read(const char *slot, int tile, int step) const {
+        if constexpr (STRIDED) {
+            const char *from = slot + at[tile] + step * (16 * kSide * 2);
+            union { s16x4 h[2]; u32x4 w; } r;
+            r.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)from);
+            r.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(from + 4 * kSide * 2));
+            return r.w;
+        } else {
+            return *reinterpret_cast<const u32x4 *>(slot + at[step] + tile * (32 * kDeep * 2));
+        }
+    }
+};
+
+// Orders a wave's own accesses to the LDS.
+__device__ inline void wave_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// The end of 32 x 128 sums that a wave has left in the LDS: eight columns a lane, so that four lanes have a checkpoint's block and a row's
+// results leave in pieces of 16 bytes side by side; four rows at a time.
+constexpr int kRowFloats = 128 + 4;                                // the four: neighbouring rows begin in different banks
+template <int OP, uint32_t DTYPE>
+__device__ inline void finish_rows(const Product &p, const float *sums, uint32_t row0, uint32_t col0, int lane, uint32_t split) {
+    const uint32_t col = col0 + (lane & 15) * 8;
+    if (p.splits == 1 && row0 + 32 <= p.rows && col0 + 128 <= p.cols) {
+        for (int r = lane >> 4; r < 32; r += 16) {
+            float v[4][8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                *reinterpret_cast<f32x4 *>(v[i]) = *reinterpret_cast<const f32x4 *>(sums + (r + 4 * i) * kRowFloats + (lane & 15) * 8);
+                *reinterpret_cast<f32x4 *>(v[i] + 4) = *reinterpret_cast<const f32x4 *>(sums + (r + 4 * i) * kRowFloats + (lane & 15) * 8 + 4);
+            }
+            finish_inside<OP, DTYPE, 4, 4>(p.finish, row0 + r, col, v);
+        }
+        return;
+    }
+    const int valid = col < p.cols ? (int)min(8u, p.cols - col) : 0;
+    for (int r = lane >> 4; r < 32; r += 4) {
+        const uint32_t row = row0 + r;
+        if (row >= p.rows) break;
+        float lo[4], hi[4];
+        *reinterpret_cast<f32x4 *>(lo) = *reinterpret_cast<const f32x4 *>(sums + r * kRowFloats + (lane & 15) * 8);
+        *reinterpret_cast<f32x4 *>(hi) = *reinterpret_cast<const f32x4 *>(sums + r * kRowFloats + (lane & 15) * 8 + 4);
+        finish8<OP, DTYPE>(p, row, col, valid, split, lo, hi);
+    }
+}
+
+template <int OP, uint32_t DTYPE> __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, 1))) void k_large(const Product p) {
+    constexpr bool kStridedA = OP == kWeightGrad, kStridedB = OP != kForward, kHalf = DTYPE == EDEN_F16, kCodes = OP == kWeightGrad;
+    static_assert(!(kCodes && kHalf), "fp16 next to a checkpoint has two terms");
+    __shared__ __attribute__((aligned(1024))) char lds[kSlots * kOperand];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wave_row = wave >> 1, wave_col = wave & 1;
+    const uint32_t row_tiles = (p.rows + kSide - 1) / kSide, col_tiles = (p.cols + kSide - 1) / kSide;
+    uint32_t split, row_tile, col_tile;
+    place_of(blockIdx.x, gridDim.x, row_tiles, col_tiles, split, row_tile, col_tile);
+    const uint32_t row0 = row_tile * kSide, col0 = col_tile * kSide;
+    const uint32_t begin = split * p.split_depth, end = min(p.depth, begin + p.split_depth);
+    const uint32_t steps = (end - begin + kDeep - 1) / kDeep;      // begin < end: launched for depths above 0 only
+
+    Source<kStridedA> a(p.a, p.lda, row0, p.rows, begin, end, p.depth, wave, lane);
+    Source<kStridedB> b(p.b, kCodes ? 0 : p.ldb, col0, kCodes ? col0 + 1 : p.cols, begin, end, p.depth, wave, lane);
+    const int swap = kCodes ? wave_col * 2 : 0;
+    const Reader<kStridedA> reader_a(wave_row * 128, lane, swap);
+    const Reader<kStridedB> reader_b(wave_col * 128, lane);
+    Codes codes(p, col0, begin, end, tid);
+
+    f32x16 acc[4][4] = {};
+    float sums[2] = {0.0f, 0.0f};                                  // row sums of this lane's depths, of the tiles i = 0, 1: the two waves of a row
+                                                                   // of waves begin with different ones
+    const bool with_sums = kCodes && p.row_sums && col_tile == 0;
+    u32x4 fa[2][4], fb[2][4];
+
+    const uint32_t lds0 = (uint32_t)(size_t)(lds_char *)lds;
+    auto depth_left = [&](uint32_t step) { return end - begin > step * kDeep ? end - begin - step * kDeep : 0u; };
+    auto read = [&](const char *slot_a, const char *slot_b, int s, int set, int i) {              // one operand of eight
+        if (i < 4) fb[set][i] = reader_b.read(slot_b, i, s);
+        else fa[set][i - 4] = reader_a.read(slot_a, i - 4, s);
+    };
+    // Sixteen products 16 deep: S = 0 .. 3 of a tile's 64.  The operands of the following ones are read, for S = 3 those of the next tiles, behind a
+    // barrier since when nobody needs the present ones.  Into their places go the second operand's tile after the next (S = 3 and the next 0)
+    // and the first operand's after that (the next S = 1, 2).
+    auto deep16 = [&](auto step16, const char *slot_a, const char *slot_b, uint32_t fetch_to, char *codes_to) {
+        constexpr int S = decltype(step16)::value, set = S & 1;
+        u32x4 words;
+        each<16>([&](auto number) {
+            constexpr int j = decltype(number)::value;
+            acc[j >> 2][j & 3] = multiply<kHalf>(fb[set][j & 3], fa[set][j >> 2], acc[j >> 2][j & 3]);
+            if constexpr (S == 3 && j == 0) meet<kCodes ? 3 * kLoads : kLoads>();     // (later: the first operand's tile after the next; codes)
+            if constexpr (j & 1) read(slot_a, slot_b, (S + 1) & 3, set ^ 1, j >> 1);
+            if constexpr (j % 4 == 2) {                            // eight loads in two runs of sixteen
+                if constexpr (S == 1 || S == 2) a.fetch(fetch_to, wave, (S - 1) * 4 + j / 4);
+                else if constexpr (!kCodes) b.fetch(fetch_to, wave, (S == 3 ? 0 : 4) + j / 4);
+            }
+            if constexpr (kCodes) {
+                constexpr int w = j >> 1, i = ((S + 1) & 3) * 2 + w / 4;                // two pieces of eight, from S = 3 on
+                if constexpr (!(j & 1)) words[w % 4] = codes.two(i, w % 4);
+                if constexpr (!(j & 1) && w % 4 == 3) codes.store(codes_to, tid, i, words);
+                if constexpr ((j & 1) && w % 4 == 3) codes.load(i);
+                // row sums: two additions an instruction, cheaper for all than a branch
+                const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+                if constexpr (j & 1) {
+                    const uint32_t pair = fa[set][j >> 3][(j >> 1) & 3];                // (a cast of the vector's element itself would take its first)
+                    sums[j >> 3] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), ones, sums[j >> 3], false);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    };
+    // Tile number c (first operand of step s: 2 s, second: 2 s + 1) goes to slot c mod 5.
+    auto on = [](uint32_t slot, uint32_t tiles) {
+        const uint32_t to = slot + tiles * kOperand;
+        return to >= (uint32_t)(kSlots * kOperand) ? to - kSlots * kOperand : to;
+    };
+    uint32_t slot = 0;                                             // of the first operand of the present step
+    if constexpr (kCodes) {
+        codes.start();
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) codes.load(i);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) codes.store(lds + kOperand, tid, i, u32x4{codes.two(i, 0), codes.two(i, 1), codes.two(i, 2), codes.two(i, 3)});
+        codes.start();
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) codes.load(i);
+        codes.start();
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {                              // what S = 3 does
+            codes.store(lds + 3 * kOperand, tid, i, u32x4{codes.two(i, 0), codes.two(i, 1), codes.two(i, 2), codes.two(i, 3)});
+            codes.load(i);
+        }
+    }
+    a.start(depth_left(0));
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) a.fetch(lds0, wave, i);
+    if constexpr (!kCodes) {
+        b.start(depth_left(0));
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) b.fetch(lds0 + kOperand, wave, i);
+    }
+    a.start(depth_left(1));
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) a.fetch(lds0 + 2 * kOperand, wave, i);
+    if constexpr (!kCodes) {
+        b.start(depth_left(1));
+#pragma unroll
+        for (int i = 0; i < kLoads / 2; ++i) b.fetch(lds0 + 3 * kOperand, wave, i);
+    }
+    meet<0>();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) read(lds, lds + kOperand, 0, 0, i);
+    for (uint32_t step = 0; step < steps; ++step) {
+        const uint32_t slot_b = on(slot, 1), next_a = on(slot, 2), next_b = on(slot, 3), after_a = on(slot, 4);
+        deep16(std::integral_constant<int, 0>(), lds + slot, lds + slot_b, lds0 + next_b, lds + next_b);
+        a.start(depth_left(step + 2));
+        deep16(std::integral_constant<int, 1>(), lds + slot, lds + slot_b, lds0 + after_a, lds + next_b);
+        deep16(std::integral_constant<int, 2>(), lds + slot, lds + slot_b, lds0 + after_a, lds + next_b);
+        if constexpr (kCodes) codes.start();
+        else b.start(depth_left(step + 2));
+        deep16(std::integral_constant<int, 3>(), lds + next_a, lds + next_b, lds0 + slot, lds + slot);
+        slot = next_a;
+    }
+
+    if constexpr (kCodes) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            sums[i] += __shfl_xor(sums[i], 32);
+            if (with_sums && lane < 32) finish_row_sum(p, sums[i], row0 + wave_row * 128 + (i ^ swap) * 32 + lane, split);
+        }
+    }
+    meet<0>();                                                     // nothing is read or fetched any more: the LDS takes the sums, 32 rows of each wave at a time
+    float *mine = reinterpret_cast<float *>(lds) + wave * 32 * kRowFloats;
+    for (int i = 0; i < 4; ++i) {
+        wave_fence();
+        auto put = [&](const f32x16 (&from)[4]) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    *reinterpret_cast<f32x4 *>(mine + (lane & 31) * kRowFloats + j * 32 + 8 * g + 4 * (lane >> 5)) =
+                        f32x4{from[j][4 * g], from[j][4 * g + 1], from[j][4 * g + 2], from[j][4 * g + 3]};
+        };
+        if (i == 0) put(acc[0]);
+        else if (i == 1) put(acc[1]);
+        else if (i == 2) put(acc[2]);
+        else put(acc[3]);
+        wave_fence();
+        finish_rows<OP, DTYPE>(p, mine, row0 + wave_row * 128 + (i ^ swap) * 32, col0 + wave_col * 128, lane, split);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_large(Op op, uint32_t dtype, const Product &p, hipStream_t st) {
+    const uint32_t grid = ((p.rows + kSide - 1) / kSide) * ((p.cols + kSide - 1) / kSide) * p.splits;
+    if (op == kWeightGrad) k_large<kWeightGrad, EDEN_BF16><<<grid, kThreads, 0, st>>>(p);
+    else if (op == kForward && dtype == EDEN_F16) k_large<kForward, EDEN_F16><<<grid, kThreads, 0, st>>>(p);
+    else if (op == kForward) k_large<kForward, EDEN_BF16><<<grid, kThreads, 0, st>>>(p);
+    else if (dtype == EDEN_F16) k_large<kInputGrad, EDEN_F16><<<grid, kThreads, 0, st>>>(p);
+    else k_large<kInputGrad, EDEN_BF16><<<grid, kThreads, 0, st>>>(p);
+    return hipGetLastError();
+}
+
+}  // namespace eden_layers

@@ -1,0 +1,163 @@
+// What the matrix-core kernels of the layer operators share: bf16 terms, places in the LDS, operands of a 32 x 32 x 16 product, the workgroup's
+// place in the result, and the end of a 32 x 32 tile.
+#ifndef EDEN_LAYERS_PRODUCT_H
+#define EDEN_LAYERS_PRODUCT_H
+
+#include "eden_layers_kernels.h"
+
+namespace eden_layers {
+
+// Byte offset of a 16-byte piece.  Rows of the depth: 16 neighbouring rows at one depth lie in different banks.
+template <int DEPTH> __device__ inline int piece_of_row(int row, int piece) {
+    return row * (DEPTH * 2) + ((DEPTH == 64 ? piece ^ ((row >> 1) & 7) : piece ^ ((row >> 2) & 3)) << 4);
+}
+// Rows of columns: 32 columns at four neighbouring depths do.
+template <int WIDTH> __device__ inline int piece_of_depth(int depth, int piece) { return depth * (WIDTH * 2) + ((piece ^ (4 * (depth & 3))) << 4); }
+
+// x = term + rest, term = the upper 16 bits (exact; an infinity leaves nothing, a NaN a NaN)
+__device__ inline float take_term(float &x) {
+    const float term = __uint_as_float(__float_as_uint(x) & 0xFFFF0000u);
+    const float rest = x - term;
+    x = __builtin_isinf(x) ? 0.0f : rest;
+    return term;
+}
+__device__ inline uint32_t upper_halves(float lo, float hi) { return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u); }
+
+__device__ inline u32x4 code_values(uint32_t c0, uint32_t c1, float unit) {
+    float a[4], b[4];
+    values4(c0, unit, a);
+    values4(c1, unit, b);
+    return u32x4{upper_halves(a[0], a[1]), upper_halves(a[2], a[3]), upper_halves(b[0], b[1]), upper_halves(b[2], b[3])};
+}
+
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+// Operand of a 32 x 32 x 16 product: lane l holds index base + l % 32 and depths 8 (l / 32) .. + 7 of the 16 from `depth` on.
+template <bool STRIDED, int DEPTH, int WIDTH> __device__ inline u32x4 fragment(const char *plane, int base, int depth, int lane) {
+    if constexpr (!STRIDED) {
+        const int row = base + (lane & 31), piece = (depth >> 3) + (lane >> 5);
+        return *reinterpret_cast<const u32x4 *>(plane + piece_of_row<DEPTH>(row, piece));
+    } else {
+        // transposing reads: 16 lanes read four depths of 16 columns and get four depths of one column each
+        const int col = base + (lane & 16) + (lane & 3) * 4, d = depth + (lane >> 5) * 8 + ((lane & 15) >> 2);
+        const char *p = plane + piece_of_depth<WIDTH>(d, col >> 3) + (col & 7) * 2;
+        const char *q = plane + piece_of_depth<WIDTH>(d + 4, col >> 3) + (col & 7) * 2;
+        union { s16x4 h[2]; u32x4 w; } r;
+        r.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p);
+        r.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)q);
+        return r.w;
+    }
+}
+
+template <bool HALF> __device__ inline f32x16 multiply(u32x4 a, u32x4 b, f32x16 c) {
+    if constexpr (HALF) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// Workgroup -> tile: workgroups go round the eight XCDs in turn; each XCD gets a run of neighbouring tiles, eight row tiles at a time, so that its L2
+// serves their operands.
+__device__ inline void place_of(uint32_t id, uint32_t total, uint32_t row_tiles, uint32_t col_tiles, uint32_t &split, uint32_t &row_tile, uint32_t &col_tile) {
+    const uint32_t xcd = id & 7u, each = total >> 3, more = total & 7u;
+    const uint32_t t = xcd * each + min(xcd, more) + (id >> 3);
+    const uint32_t tiles = row_tiles * col_tiles;
+    split = t / tiles;
+    const uint32_t tile = t - split * tiles, group = tile / (8 * col_tiles), first = group * 8, height = min(8u, row_tiles - first);
+    const uint32_t within = tile - group * 8 * col_tiles;
+    row_tile = first + within % height;
+    col_tile = within / height;
+}
+
+// The end of 32 x 32 sums: a lane has row lane % 32 and columns 8 g + 4 (lane / 32) .. + 3 of the tile's, g = 0 .. 3.
+template <int OP, uint32_t DTYPE>
+__device__ inline void finish_tile(const Product &p, const f32x16 &acc, uint32_t row, uint32_t block_col, int lane, uint32_t split) {
+    if (block_col >= p.cols) return;
+    float v[4][4];
+    int valid[4];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        const uint32_t col = block_col + 8 * g + 4 * (lane >> 5);
+        valid[g] = row < p.rows && col < p.cols ? (int)min(4u, p.cols - col) : 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[g][e] = acc[4 * g + e];
+    }
+    if (p.splits > 1) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            if (!valid[g]) continue;
+            float *out = p.partial + ((size_t)split * p.rows + row) * p.partial_ld + block_col + 8 * g + 4 * (lane >> 5);
+            *reinterpret_cast<f32x4 *>(out) = f32x4{v[g][0], v[g][1], v[g][2], v[g][3]};      // partial_ld is a multiple of 4
+        }
+        return;
+    }
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+        if (valid[g]) finish_bias<OP, DTYPE>(p.finish, block_col + 8 * g + 4 * (lane >> 5), valid[g], v[g]);
+    if constexpr (OP == kForward)
+        if (p.finish.codes_out) {
+            uint32_t largest = 0;
+            float z[4][4];
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    z[g][e] = e < valid[g] ? v[g][e] : 0.0f;
+                    largest = max(largest, magnitude_bits(z[g][e]));
+                }
+            largest = max(largest, (uint32_t)__shfl_xor((int)largest, 32));
+            const uint32_t t = block_exponent(largest);
+            if (row < p.rows) {
+                const size_t block = (size_t)row * p.finish.blocks + block_col / kBlock;
+                if (lane < 32) p.finish.exps_out[block] = (uint8_t)t;
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    *reinterpret_cast<uint32_t *>(p.finish.codes_out + block * kBlock + 8 * g + 4 * (lane >> 5)) = codes4(z[g], t);
+            }
+        }
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+        if (valid[g]) finish_store<OP, DTYPE>(p.finish, row, block_col + 8 * g + 4 * (lane >> 5), valid[g], v[g]);
+}
+// The end of eight neighbouring sums of a row, `valid` of which the result has (0: the lane takes part in a block's largest value only).  Four lanes side
+// by side have a block of 32.
+template <int OP, uint32_t DTYPE>
+__device__ inline void finish8(const Product &p, uint32_t row, uint32_t col, int valid, uint32_t split, float (&lo)[4], float (&hi)[4]) {
+    const int valid_lo = min(valid, 4), valid_hi = max(valid - 4, 0);
+    if (p.splits > 1) {
+        float *out = p.partial + ((size_t)split * p.rows + row) * p.partial_ld + col;                 // partial_ld is a multiple of 4
+        if (valid_lo) *reinterpret_cast<f32x4 *>(out) = f32x4{lo[0], lo[1], lo[2], lo[3]};
+        if (valid_hi) *reinterpret_cast<f32x4 *>(out + 4) = f32x4{hi[0], hi[1], hi[2], hi[3]};
+        return;
+    }
+    if (valid_lo) finish_bias<OP, DTYPE>(p.finish, col, valid_lo, lo);
+    if (valid_hi) finish_bias<OP, DTYPE>(p.finish, col + 4, valid_hi, hi);
+    if constexpr (OP == kForward)
+        if (p.finish.codes_out) {
+            uint32_t largest = 0;
+            float z[2][4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                z[0][e] = e < valid ? lo[e] : 0.0f;
+                z[1][e] = e + 4 < valid ? hi[e] : 0.0f;
+                largest = max(largest, max(magnitude_bits(z[0][e]), magnitude_bits(z[1][e])));
+            }
+            largest = max(largest, (uint32_t)__shfl_xor((int)largest, 1));
+            largest = max(largest, (uint32_t)__shfl_xor((int)largest, 2));
+            const uint32_t t = block_exponent(largest);
+            if (col < p.finish.blocks * kBlock) {
+                const size_t block = (size_t)row * p.finish.blocks + col / kBlock;
+                *reinterpret_cast<u32x2 *>(p.finish.codes_out + block * kBlock + col % kBlock) = u32x2{codes4(z[0], t), codes4(z[1], t)};
+                if (col % kBlock == 0) p.finish.exps_out[block] = (uint8_t)t;
+            }
+        }
+    finish_store8<OP, DTYPE>(p.finish, row, col, valid, lo, hi);
+}
+// Row sums (sums: the product with ones, any of its rows) of row `row`, for one lane of each.
+__device__ inline void finish_row_sum(const Product &p, float sum, uint32_t row, uint32_t split) {
+    if (row >= p.rows) return;
+    if (p.splits > 1) p.partial[(size_t)p.splits * p.rows * p.partial_ld + (size_t)split * p.rows + row] = sum;
+    else p.row_sums[row] = p.finish.accumulate ? p.row_sums[row] + sum : sum;
+}
+
+}  // namespace eden_layers
+
+#endif  // EDEN_LAYERS_PRODUCT_H

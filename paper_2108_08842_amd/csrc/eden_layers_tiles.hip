@@ -9,7 +9,7 @@
 // input gradient), which the transposing reads of the LDS turn by the way.  16-byte pieces of a row are swapped so that neither kind of
 // read meets its own bank.  The operand of the columns goes first into the products, so that a lane ends up with one row and runs of four
 // columns of the result: the end of the product works on vectors, and a checkpoint's block of 32 columns is 16 values in each of two lanes.
-#include "eden_layers_kernels.h"
+#include "eden_layers_product.h"
 
 namespace eden_layers {
 namespace {
@@ -30,25 +30,9 @@ template <int OP, uint32_t DTYPE> struct Plan {
     static constexpr int kPieces = (int)kTile * kDepth / 8 / kThreads;         // pieces of 8 elements per thread and operand
 };
 
-// Byte offset of a 16-byte piece.  Rows of the depth: 16 neighbouring rows at one depth lie in different banks.
-template <int DEPTH> __device__ inline int piece_of_row(int row, int piece) {
-    return row * (DEPTH * 2) + ((DEPTH == 64 ? piece ^ ((row >> 1) & 7) : piece ^ ((row >> 2) & 3)) << 4);
-}
-// Rows of columns: 32 columns at four neighbouring depths do.
-__device__ inline int piece_of_depth(int depth, int piece) { return depth * ((int)kTile * 2) + ((piece ^ (4 * (depth & 3))) << 4); }
-
 // Eight elements of an operand on their way from memory to the LDS.
 template <uint32_t DTYPE> struct Piece { Vec<typename Elem<DTYPE>::type, 8> v; };
 struct CodePiece { u32x4 codes; uint32_t exponent; };              // 16 codes
-
-// x = term + rest, term = the upper 16 bits (exact; an infinity leaves nothing, a NaN a NaN)
-__device__ inline float take_term(float &x) {
-    const float term = __uint_as_float(__float_as_uint(x) & 0xFFFF0000u);
-    const float rest = x - term;
-    x = __builtin_isinf(x) ? 0.0f : rest;
-    return term;
-}
-__device__ inline uint32_t upper_halves(float lo, float hi) { return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u); }
 
 template <uint32_t DTYPE, int TERMS> __device__ inline void store_piece(char *lds, int plane, const Piece<DTYPE> &p) {
     if constexpr (TERMS == 1) {
@@ -69,50 +53,6 @@ template <uint32_t DTYPE, int TERMS> __device__ inline void store_piece(char *ld
             *reinterpret_cast<u32x4 *>(lds + t * plane) = w;
         }
     }
-}
-
-__device__ inline u32x4 code_values(uint32_t c0, uint32_t c1, float unit) {
-    float a[4], b[4];
-    values4(c0, unit, a);
-    values4(c1, unit, b);
-    return u32x4{upper_halves(a[0], a[1]), upper_halves(a[2], a[3]), upper_halves(b[0], b[1]), upper_halves(b[2], b[3])};
-}
-
-typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-
-// Operand of a 32 x 32 x 16 product: lane l holds index base + l % 32 and depths 8 (l / 32) .. + 7 of the 16 from `depth` on.
-template <bool STRIDED, int DEPTH> __device__ inline u32x4 fragment(const char *plane, int base, int depth, int lane) {
-    if constexpr (!STRIDED) {
-        const int row = base + (lane & 31), piece = (depth >> 3) + (lane >> 5);
-        return *reinterpret_cast<const u32x4 *>(plane + piece_of_row<DEPTH>(row, piece));
-    } else {
-        // transposing reads: 16 lanes read four depths of 16 columns and get four depths of one column each
-        const int col = base + (lane & 16) + (lane & 3) * 4, d = depth + (lane >> 5) * 8 + ((lane & 15) >> 2);
-        const char *p = plane + piece_of_depth(d, col >> 3) + (col & 7) * 2;
-        const char *q = plane + piece_of_depth(d + 4, col >> 3) + (col & 7) * 2;
-        union { s16x4 h[2]; u32x4 w; } r;
-        r.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p);
-        r.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)q);
-        return r.w;
-    }
-}
-
-template <bool HALF> __device__ inline f32x16 multiply(u32x4 a, u32x4 b, f32x16 c) {
-    if constexpr (HALF) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-    else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-
-// Workgroup -> tile: workgroups go round the eight XCDs in turn; each XCD gets a run of neighbouring tiles, eight row tiles at a time, so that its L2
-// serves their operands.
-__device__ inline void place_of(uint32_t id, uint32_t total, uint32_t row_tiles, uint32_t col_tiles, uint32_t &split, uint32_t &row_tile, uint32_t &col_tile) {
-    const uint32_t xcd = id & 7u, each = total >> 3, more = total & 7u;
-    const uint32_t t = xcd * each + min(xcd, more) + (id >> 3);
-    const uint32_t tiles = row_tiles * col_tiles;
-    split = t / tiles;
-    const uint32_t tile = t - split * tiles, group = tile / (8 * col_tiles), first = group * 8, height = min(8u, row_tiles - first);
-    const uint32_t within = tile - group * 8 * col_tiles;
-    row_tile = first + within % height;
-    col_tile = within / height;
 }
 
 template <int OP, uint32_t DTYPE> __global__ __launch_bounds__(kThreads, 2) void k_tiles(const Product p) {
@@ -168,22 +108,22 @@ template <int OP, uint32_t DTYPE> __global__ __launch_bounds__(kThreads, 2) void
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int c = i * kThreads + tid;
-            store_piece<DTYPE, P::kTermsA>(stage + (P::kStridedA ? piece_of_depth(c / 16, c % 16) : piece_of_row<D>(c / (D / 8), c % (D / 8))), P::kPlane, a[i]);
+            store_piece<DTYPE, P::kTermsA>(stage + (P::kStridedA ? piece_of_depth<kTile>(c / 16, c % 16) : piece_of_row<D>(c / (D / 8), c % (D / 8))), P::kPlane, a[i]);
         }
         char *second = stage + P::kTermsA * P::kPlane;
         if constexpr (OP != kWeightGrad) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const int c = i * kThreads + tid;
-                store_piece<DTYPE, P::kTermsB>(second + (P::kStridedB ? piece_of_depth(c / 16, c % 16) : piece_of_row<D>(c / (D / 8), c % (D / 8))), P::kPlane, b[i]);
+                store_piece<DTYPE, P::kTermsB>(second + (P::kStridedB ? piece_of_depth<kTile>(c / 16, c % 16) : piece_of_row<D>(c / (D / 8), c % (D / 8))), P::kPlane, b[i]);
             }
         } else {
 #pragma unroll
             for (int i = 0; i < N / 2; ++i) {
                 const int c = i * kThreads + tid;
                 const float unit = block_unit(codes[i].exponent);
-                *reinterpret_cast<u32x4 *>(second + piece_of_depth(c / 8, c % 8 * 2)) = code_values(codes[i].codes[0], codes[i].codes[1], unit);
-                *reinterpret_cast<u32x4 *>(second + piece_of_depth(c / 8, c % 8 * 2 + 1)) = code_values(codes[i].codes[2], codes[i].codes[3], unit);
+                *reinterpret_cast<u32x4 *>(second + piece_of_depth<kTile>(c / 8, c % 8 * 2)) = code_values(codes[i].codes[0], codes[i].codes[1], unit);
+                *reinterpret_cast<u32x4 *>(second + piece_of_depth<kTile>(c / 8, c % 8 * 2 + 1)) = code_values(codes[i].codes[2], codes[i].codes[3], unit);
             }
         }
     };
@@ -201,11 +141,11 @@ template <int OP, uint32_t DTYPE> __global__ __launch_bounds__(kThreads, 2) void
 #pragma unroll
             for (int t = 0; t < P::kTermsA; ++t)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) fa[t][i] = fragment<P::kStridedA, D>(stage + t * P::kPlane, wave_row * 64 + i * 32, d, lane);
+                for (int i = 0; i < 2; ++i) fa[t][i] = fragment<P::kStridedA, D, kTile>(stage + t * P::kPlane, wave_row * 64 + i * 32, d, lane);
 #pragma unroll
             for (int t = 0; t < P::kTermsB; ++t)
 #pragma unroll
-                for (int j = 0; j < 2; ++j) fb[t][j] = fragment<P::kStridedB, D>(second + t * P::kPlane, wave_col * 64 + j * 32, d, lane);
+                for (int j = 0; j < 2; ++j) fb[t][j] = fragment<P::kStridedB, D, kTile>(second + t * P::kPlane, wave_col * 64 + j * 32, d, lane);
 #pragma unroll
             for (int ta = P::kTermsA - 1; ta >= 0; --ta)           // small products first
 #pragma unroll
@@ -241,65 +181,12 @@ template <int OP, uint32_t DTYPE> __global__ __launch_bounds__(kThreads, 2) void
     }
 
     if constexpr (OP == kWeightGrad)
-        if (with_sums && lane < 32) {
-            const uint32_t row = row0 + wave_row * 64 + wave_col * 32 + lane;
-            if (row < p.rows) {
-                if (p.splits > 1) p.partial[(size_t)p.splits * p.rows * p.partial_ld + (size_t)split * p.rows + row] = sums[0];
-                else p.row_sums[row] = p.finish.accumulate ? p.row_sums[row] + sums[0] : sums[0];
-            }
-        }
+        if (with_sums && lane < 32) finish_row_sum(p, sums[0], row0 + wave_row * 64 + wave_col * 32 + lane, split);
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const uint32_t row = row0 + wave_row * 64 + i * 32 + (lane & 31), block_col = col0 + wave_col * 64 + j * 32;
-            if (block_col >= p.cols) continue;
-            float v[4][4];
-            int valid[4];
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const uint32_t col = block_col + 8 * g + 4 * (lane >> 5);
-                valid[g] = row < p.rows && col < p.cols ? (int)min(4u, p.cols - col) : 0;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[g][e] = acc[i][j][4 * g + e];
-            }
-            if (p.splits > 1) {
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    if (!valid[g]) continue;
-                    float *out = p.partial + ((size_t)split * p.rows + row) * p.partial_ld + block_col + 8 * g + 4 * (lane >> 5);
-                    *reinterpret_cast<f32x4 *>(out) = f32x4{v[g][0], v[g][1], v[g][2], v[g][3]};      // partial_ld is a multiple of 4
-                }
-                continue;
-            }
-#pragma unroll
-            for (int g = 0; g < 4; ++g)
-                if (valid[g]) finish_bias<OP, DTYPE>(p.finish, block_col + 8 * g + 4 * (lane >> 5), valid[g], v[g]);
-            if constexpr (OP == kForward)
-                if (p.finish.codes_out) {
-                    uint32_t largest = 0;
-                    float z[4][4];
-#pragma unroll
-                    for (int g = 0; g < 4; ++g)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            z[g][e] = e < valid[g] ? v[g][e] : 0.0f;
-                            largest = max(largest, magnitude_bits(z[g][e]));
-                        }
-                    largest = max(largest, (uint32_t)__shfl_xor((int)largest, 32));
-                    const uint32_t t = block_exponent(largest);
-                    if (row < p.rows) {
-                        const size_t block = (size_t)row * p.finish.blocks + block_col / kBlock;
-                        if (lane < 32) p.finish.exps_out[block] = (uint8_t)t;
-#pragma unroll
-                        for (int g = 0; g < 4; ++g)
-                            *reinterpret_cast<uint32_t *>(p.finish.codes_out + block * kBlock + 8 * g + 4 * (lane >> 5)) = codes4(z[g], t);
-                    }
-                }
-#pragma unroll
-            for (int g = 0; g < 4; ++g)
-                if (valid[g]) finish_store<OP, DTYPE>(p.finish, row, block_col + 8 * g + 4 * (lane >> 5), valid[g], v[g]);
-        }
+        for (int j = 0; j < 2; ++j)
+            finish_tile<OP, DTYPE>(p, acc[i][j], row0 + wave_row * 64 + i * 32 + (lane & 31), col0 + wave_col * 64 + j * 32, lane, split);
 }
 
 // Sums of the splits, in their order, and the end of the product.  A thread has four columns, eight threads a block of a checkpoint.

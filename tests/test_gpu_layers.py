@@ -279,6 +279,83 @@ def test_gradients_against_differences(layers, act):
         assert bool(((got.cpu().double() - want).abs() <= 1e-5 * (1.0 + want.abs()) * 4).all())
 
 
+# ---- results that fill the device: another kernel (rows of whole 16-byte pieces, two-byte types), ragged tiles, depths around its steps of 64
+
+def wide(seed, rows, cols, dtype, pad=0, scale=1.0):
+    """A matrix whose rows are `pad` elements further apart than they are long, NaN between them and behind the last."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.full((rows * (cols + pad) + 64,), float("nan"), dtype=dtype, device="cuda")
+    m = x[:rows * (cols + pad)].view(rows, cols + pad)[:, :cols]
+    m.copy_(torch.randn(rows, cols, generator=g, device="cuda") * scale)
+    return m
+
+
+@pytest.mark.parametrize("depth,pad", [(8, 0), (56, 8), (64, 0), (72, 0), (200, 24), (1000, 0)])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_large_linear(layers, dtype, depth, pad):
+    t, m, n = TYPES[dtype], 3337, 3592
+    x, w, bias, r = wide(1, m, depth, t, pad), wide(2, n, depth, t, pad, depth ** -0.5), wide(3, 1, n, t)[0], wide(4, m, n, t, pad)
+    out = torch.full((m, n + pad), 5.0, dtype=t, device="cuda")
+    y, c = layers.linear(x, w, bias, activation="gelu", residual=r, checkpoint=True, out=out[:, :n])
+    z = x.double() @ w.double().t().contiguous() + bias.double()
+    want = ref.act(z, "gelu") + r.double()
+    dz = ref.product_bound(x.double(), w.double(), depth) + 4 * ref.EPS * z.abs()
+    near = 1.13 * dz + 2.0 ** -20 * (1.0 + z.abs() + want.abs()) + ref.ROUND[t] * want.abs()
+    assert bool(((y.double() - want).abs() <= near).all()) and bool((out[:, n:] == 5.0).all())
+    assert ref.rel(y, want) <= 1.5 * ref.norm_bound(depth, t) + 2.0 ** -20
+    codes, exps = ref.unpack(c.buffer, m, n)
+    unit = torch.from_numpy(np.repeat(np.exp2(exps.astype(np.float64) - 127), 32, axis=1)[:, :n])
+    got = torch.from_numpy(ref.decode(codes, exps, n))
+    assert bool(((got - z.cpu()).abs() <= unit * torch.where(got.abs() == 127 * unit, 1.0, 0.5) + dz.cpu()).all()) and not codes[:, n:].any()
+
+
+@pytest.mark.parametrize("depth,pad", [(8, 8), (64, 0), (72, 24), (328, 0)])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_large_input_grad(layers, dtype, depth, pad):
+    t, m, k = TYPES[dtype], 3337, 3592
+    dz, w, r = wide(1, m, depth, t, pad), wide(2, depth, k, t, pad, depth ** -0.5), wide(4, m, k, t, pad)
+    saved_z = layers.save_checkpoint(wide(5, m, k, t, 0, 2.0))
+    s = ref.slope(saved_z.restore(torch.float32).double(), "silu")
+    product = dz.double() @ w.double()
+    want = product * s + r.double()
+    dx = layers.linear_input_grad(dz, w, activation="silu", checkpoint=saved_z, residual=r)
+    near = 1.13 * ref.product_bound(dz.double(), w.double().t().contiguous(), depth) + 2.0 ** -19 * product.abs() + (4 * ref.EPS + ref.ROUND[t]) * want.abs() + ref.TINY[t]
+    assert bool(((dx.double() - want).abs() <= near).all())
+    assert ref.rel(dx, want) <= 1.5 * ref.norm_bound(depth, t) + 2.0 ** -19
+
+
+@pytest.mark.parametrize("depth,pad", [(1, 0), (63, 8), (64, 0), (65, 0), (333, 24), (1000, 0)])
+def test_large_weight_grad(layers, depth, pad):
+    n, k = 3592, 3589
+    dy = wide(1, depth, n, torch.bfloat16, pad)
+    c = layers.save_checkpoint(wide(2, depth, k, torch.bfloat16, 0, 10.0))
+    X, Y = c.restore(torch.float32).double(), dy.double()
+    flat = torch.full((3 + n * k + n + 2,), 4.0, device="cuda")
+    out, bias_out = flat[3:3 + n * k].view(n, k), flat[3 + n * k:-2]
+    layers.linear_weight_grad(dy, c, out=out, bias_out=bias_out)
+    want, want_b = Y.t().contiguous() @ X, Y.sum(0)
+    near = ref.product_bound(Y.t().contiguous(), X.t().contiguous(), depth) + 2.0 ** -24 * want.abs()
+    assert bool(((out.double() - want).abs() <= near).all()) and ref.rel(out, want) <= ref.norm_bound(depth, torch.float32)
+    assert bool(((bias_out.double() - want_b).abs() <= (depth + 8) * 2.0 ** -23 * Y.abs().sum(0)).all())
+    first, first_b = out.clone(), bias_out.clone()
+    layers.linear_weight_grad(dy, c, out=out, bias_out=bias_out, accumulate=True)
+    assert torch.equal(out, first + first) and torch.equal(bias_out, first_b + first_b)
+    assert bool((flat[:3] == 4.0).all()) and bool((flat[-2:] == 4.0).all())
+
+
+def test_large_products_give_the_same_bits_every_time(layers):
+    # loads into the LDS, barriers and stages: a missing wait would show as results that come and go
+    x, w, dy = wide(1, 4096, 2048, torch.bfloat16), wide(2, 4096, 2048, torch.bfloat16), wide(3, 4096, 4096, torch.bfloat16)
+    c = layers.save_checkpoint(x)
+    calls = [lambda: layers.linear(x, w), lambda: layers.linear_input_grad(dy, w), lambda: layers.linear_weight_grad(dy, c)]
+    first = [f() for f in calls]
+    for _ in range(20):
+        for f, want in zip(calls, first):
+            assert torch.equal(f(), want)
+    assert ref.rel(first[0], x.double() @ w.double().t().contiguous()) <= ref.norm_bound(2048, torch.bfloat16)
+    assert ref.rel(first[1], dy.double() @ w.double()) <= ref.norm_bound(4096, torch.bfloat16)
+
+
 # ---- values that are not finite
 
 @pytest.mark.parametrize("dtype", TYPES)
