@@ -43,22 +43,30 @@ uint64_t splits_of(uint64_t rows, uint64_t cols, uint64_t depth) {
 bool whole_pieces(const void *p, uint64_t ld, uint64_t inner) {
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0 && inner % 8 == 0 && ld < (1u << 21);
 }
-// Whether the kernel of 256 x 256 tiles takes a product.
-bool is_large(Op op, uint32_t dtype, const Product &p) {
+// Whether the kernel whose loads go straight into the LDS takes a product.
+bool is_direct(Op op, uint32_t dtype, const Product &p) {
     if (dtype == EDEN_F32 || (op == kWeightGrad && dtype == EDEN_F16) || p.depth == 0 || p.cols == 0) return false;
-    const uint64_t tiles = (uint64_t)((p.rows + kLargeTile - 1) / kLargeTile) * ((p.cols + kLargeTile - 1) / kLargeTile);
-    if (tiles < 192 || tiles > kMostGroups) return false;
     if (!whole_pieces(p.a, p.lda, op == kWeightGrad ? p.rows : p.depth)) return false;
     return op == kWeightGrad ? p.ldb < (1u << 24) : whole_pieces(p.b, p.ldb, op == kForward ? p.depth : p.cols);
+}
+// ... and whether its tiles of 256 x 256 give every CU work
+bool fills_device(const Product &p) {
+    return (uint64_t)((p.rows + kLargeTile - 1) / kLargeTile) * ((p.cols + kLargeTile - 1) / kLargeTile) >= 192;
 }
 
 // Launches a product whose operands and end are set.
 int run(Op op, uint32_t dtype, Product &p, void *workspace, size_t workspace_bytes, void *stream) {
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return EDEN_ERR_INVALID_ARG;
-    if (is_large(op, dtype, p)) {
+    if (op == kForward && p.rows <= kFewRows) {
+        // 32 columns a workgroup spare reads of x; 16 where that would leave CUs idle
+        return status(launch_rows(dtype, p, p.finish.codes_out != nullptr || p.cols > 32 * 512, st));
+    }
+    const bool direct = is_direct(op, dtype, p);
+    if (tile_count(p.rows, p.cols) > kMostGroups / 64) return EDEN_ERR_INVALID_ARG;
+    if (direct && fills_device(p)) {
         p.splits = 1, p.split_depth = p.depth;
-        return status(launch_large(op, dtype, p, st));
+        return status(launch_direct(op, dtype, p, kLargeTile, st));
     }
     uint64_t splits = splits_of(p.rows, p.cols, p.depth);
     if (workspace == nullptr) workspace_bytes = 0;
@@ -69,8 +77,7 @@ int run(Op op, uint32_t dtype, Product &p, void *workspace, size_t workspace_byt
     p.split_depth = (uint32_t)each;
     p.partial = static_cast<float *>(workspace);
     p.partial_ld = (p.cols + 3) / 4 * 4;
-    if (tile_count(p.rows, p.cols) * p.splits > kMostGroups) return EDEN_ERR_INVALID_ARG;
-    hipError_t e = launch_tiles(op, dtype, p, st);
+    hipError_t e = direct ? launch_direct(op, dtype, p, kTile, st) : launch_tiles(op, dtype, p, st);
     if (e == hipSuccess && p.splits > 1) e = launch_join(op, dtype, p, st);
     return status(e);
 }

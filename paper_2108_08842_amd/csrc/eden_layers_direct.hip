@@ -17,9 +17,14 @@
 namespace eden_layers {
 namespace {
 
-constexpr int kThreads = 256, kSide = (int)kLargeTile, kDeep = 64, kSlots = 5;
-constexpr int kOperand = kSide * kDeep * 2;        // bytes of an operand's tile, a slot of the LDS
-constexpr int kLoads = kOperand / 16 / kThreads;   // 16-byte pieces per thread
+constexpr int kThreads = 256, kDeep = 64, kSlots = 5;
+// T: a wave has T x T products of 32 x 32
+template <int T> struct Tile {
+    static constexpr int kSide = 64 * T;
+    static constexpr int kOperand = kSide * kDeep * 2;             // bytes of an operand's tile, a slot of the LDS
+    static constexpr int kLoads = kOperand / 16 / kThreads;        // 16-byte pieces per thread
+    static constexpr int kPieces = kSide / 8;                      // of a row of columns
+};
 constexpr uint32_t kMostBytes = 0x7FFFFF00u;       // reach of a descriptor; offsets from kNowhere on lie beyond it (and below 2^32)
 constexpr uint32_t kNowhere = 0x7FFFFFF0u;
 
@@ -44,7 +49,8 @@ __device__ inline u32x4 descriptor(const char *base, uint64_t reach) {
 }
 
 // Where a thread's pieces of an operand come from: byte offsets from the tile's first element.
-template <bool STRIDED> struct Source {
+template <int T, bool STRIDED> struct Source {
+    static constexpr int kSide = Tile<T>::kSide, kPieces = Tile<T>::kPieces;
     const char *base;
     size_t step;               // bytes from one tile to the next
     uint64_t reach;            // bytes from `base` to the end of what may be read
@@ -58,9 +64,9 @@ template <bool STRIDED> struct Source {
             base = static_cast<const char *>(p) + ((size_t)begin * ld + first) * 2;
             step = (size_t)kDeep * ld * 2;
             reach = ((uint64_t)(end - begin - 1) * ld + (count - first)) * 2;
-            const uint32_t d = wave * 2 + (lane >> 5), piece = (lane & 31) ^ (4 * (d & 3));
+            const uint32_t d = (wave * 64 + lane) / kPieces, piece = (lane % kPieces) ^ (4 * (d & 3));
             offset = (uint32_t)(d * ld * 2) + piece * 16;
-            stride = (uint32_t)(8 * ld * 2);
+            stride = (uint32_t)(kThreads / kPieces * ld * 2);
             depth = 0;
         } else {
             const uint32_t rows = min((uint32_t)kSide, count - first);
@@ -88,9 +94,10 @@ template <bool STRIDED> struct Source {
     }
 };
 
-// A checkpoint's codes: 32 neighbouring lanes have the 32 pieces of one depth (8 codes each), a thread eight depths of a tile.  What lies
+// A checkpoint's codes: neighbouring lanes have the pieces of one depth (8 codes each), a thread kLoads depths of a tile.  What lies
 // beyond the depths of the split is read as zeros (codes 0, unit 0).
-struct Codes {
+template <int T> struct Codes {
+    static constexpr int kSide = Tile<T>::kSide, kLoads = Tile<T>::kLoads, kPieces = Tile<T>::kPieces, kDepths = kThreads / kPieces;
     const uint8_t *codes, *exps;
     uint64_t codes_reach, exps_reach;
     size_t ld;
@@ -102,7 +109,7 @@ struct Codes {
     __device__ Codes(const Product &p, uint32_t col0, uint32_t begin, uint32_t end, int tid)
         : codes(static_cast<const uint8_t *>(p.b) + (size_t)begin * p.ldb + col0), exps(p.b_exps + (size_t)begin * p.b_blocks + col0 / kBlock),
           codes_reach((uint64_t)(end - begin) * p.ldb - col0), exps_reach((uint64_t)(end - begin) * p.b_blocks - col0 / kBlock), ld(p.ldb), blocks(p.b_blocks),
-          at((tid / 32) * (uint32_t)p.ldb + tid % 32 * 8), exp_at((tid / 32) * p.b_blocks + tid % 32 / 4) {}
+          at((tid / kPieces) * (uint32_t)p.ldb + tid % kPieces * 8), exp_at((tid / kPieces) * p.b_blocks + tid % kPieces / 4) {}
     __device__ void start() {
         codes_now = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(codes), 0, (int)(codes_reach < kMostBytes ? (uint32_t)codes_reach : kMostBytes), 0x00020000);
         exps_now = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(exps), 0, (int)(exps_reach < kMostBytes ? (uint32_t)exps_reach : kMostBytes), 0x00020000);
@@ -112,8 +119,8 @@ struct Codes {
         exps_reach = exps_reach > (uint64_t)kDeep * blocks ? exps_reach - (uint64_t)kDeep * blocks : 0;
     }
     __device__ void load(int i) {
-        q[i] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(codes_now, (int)(at + i * 8 * (uint32_t)ld), 0, 0));
-        t[i] = __builtin_amdgcn_raw_buffer_load_b8(exps_now, (int)(exp_at + i * 8 * blocks), 0, 0);
+        q[i] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(codes_now, (int)(at + i * kDepths * (uint32_t)ld), 0, 0));
+        t[i] = __builtin_amdgcn_raw_buffer_load_b8(exps_now, (int)(exp_at + i * kDepths * blocks), 0, 0);
     }
     // Values 2 h and 2 h + 1 of piece i; the whole piece into the LDS
     __device__ uint32_t two(int i, int h) const {
@@ -122,18 +129,19 @@ struct Codes {
         return upper_halves((float)(int8_t)(c & 0xFFu) * unit, (float)(int8_t)((c >> 8) & 0xFFu) * unit);
     }
     __device__ void store(char *tile, int tid, int i, u32x4 words) const {
-        *reinterpret_cast<u32x4 *>(tile + piece_of_depth<kSide>(i * 8 + tid / 32, tid % 32)) = words;
+        *reinterpret_cast<u32x4 *>(tile + piece_of_depth<kSide>(i * kDepths + tid / kPieces, tid % kPieces)) = words;
     }
 };
 
 // Where a lane reads an operand's tile in the LDS.  The swaps leave four different places; tiles of 32 (whole rows apart) or steps of 16 deep (whole
 // depths apart) are constant distances from them.
-template <bool STRIDED> struct Reader {
-    uint32_t at[4];
+template <int T, bool STRIDED> struct Reader {
+    static constexpr int kSide = Tile<T>::kSide;
+    uint32_t at[STRIDED ? T : 4];
 
     __device__ Reader(int base, int lane, int swap = 0) {          // STRIDED: tile i is number i ^ swap from `base` on
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < (STRIDED ? T : 4); ++i) {
             if constexpr (STRIDED) {                               // of tile i
                 const int col = base + (i ^ swap) * 32 + (lane & 16) + (lane & 3) * 4;
                 at[i] = piece_of_depth<kSide>((lane >> 5) * 8 + ((lane & 15) >> 2), col >> 3) + (col & 7) * 2;
@@ -161,36 +169,47 @@ __device__ inline void wave_fence() {
     __builtin_amdgcn_wave_barrier();
 }
 
-// The end of 32 x 128 sums that a wave has left in the LDS: eight columns a lane, so that four lanes have a checkpoint's block and a row's
+// The end of 32 x 32 T sums that a wave has left in the LDS: eight columns a lane, so that four lanes have a checkpoint's block and a row's
 // results leave in pieces of 16 bytes side by side; four rows at a time.
-constexpr int kRowFloats = 128 + 4;                                // the four: neighbouring rows begin in different banks
-template <int OP, uint32_t DTYPE>
+template <int T> constexpr int kRowFloats = 32 * T + 4;            // the four: neighbouring rows begin in different banks
+template <int OP, uint32_t DTYPE, int T>
 __device__ inline void finish_rows(const Product &p, const float *sums, uint32_t row0, uint32_t col0, int lane, uint32_t split) {
-    const uint32_t col = col0 + (lane & 15) * 8;
-    if (p.splits == 1 && row0 + 32 <= p.rows && col0 + 128 <= p.cols) {
-        for (int r = lane >> 4; r < 32; r += 16) {
+    constexpr int kLanes = 4 * T, kStep = 64 / kLanes;             // lanes of a row; rows side by side
+    const uint32_t first = lane / kLanes, within = lane % kLanes * 8, col = col0 + within;
+    if (row0 + 32 <= p.rows && col0 + 32 * T <= p.cols) {
+        for (uint32_t r = first; r < 32; r += 4 * kStep) {
             float v[4][8];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                *reinterpret_cast<f32x4 *>(v[i]) = *reinterpret_cast<const f32x4 *>(sums + (r + 4 * i) * kRowFloats + (lane & 15) * 8);
-                *reinterpret_cast<f32x4 *>(v[i] + 4) = *reinterpret_cast<const f32x4 *>(sums + (r + 4 * i) * kRowFloats + (lane & 15) * 8 + 4);
+                *reinterpret_cast<f32x4 *>(v[i]) = *reinterpret_cast<const f32x4 *>(sums + (r + kStep * i) * kRowFloats<T> + within);
+                *reinterpret_cast<f32x4 *>(v[i] + 4) = *reinterpret_cast<const f32x4 *>(sums + (r + kStep * i) * kRowFloats<T> + within + 4);
             }
-            finish_inside<OP, DTYPE, 4, 4>(p.finish, row0 + r, col, v);
+            if (p.splits > 1) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float *out = p.partial + ((size_t)split * p.rows + row0 + r + kStep * i) * p.partial_ld + col;
+                    *reinterpret_cast<f32x4 *>(out) = *reinterpret_cast<f32x4 *>(v[i]);
+                    *reinterpret_cast<f32x4 *>(out + 4) = *reinterpret_cast<f32x4 *>(v[i] + 4);
+                }
+            } else {
+                finish_inside<OP, DTYPE, 4, kStep>(p.finish, row0 + r, col, v);
+            }
         }
         return;
     }
     const int valid = col < p.cols ? (int)min(8u, p.cols - col) : 0;
-    for (int r = lane >> 4; r < 32; r += 4) {
+    for (uint32_t r = first; r < 32; r += kStep) {
         const uint32_t row = row0 + r;
         if (row >= p.rows) break;
         float lo[4], hi[4];
-        *reinterpret_cast<f32x4 *>(lo) = *reinterpret_cast<const f32x4 *>(sums + r * kRowFloats + (lane & 15) * 8);
-        *reinterpret_cast<f32x4 *>(hi) = *reinterpret_cast<const f32x4 *>(sums + r * kRowFloats + (lane & 15) * 8 + 4);
+        *reinterpret_cast<f32x4 *>(lo) = *reinterpret_cast<const f32x4 *>(sums + r * kRowFloats<T> + within);
+        *reinterpret_cast<f32x4 *>(hi) = *reinterpret_cast<const f32x4 *>(sums + r * kRowFloats<T> + within + 4);
         finish8<OP, DTYPE>(p, row, col, valid, split, lo, hi);
     }
 }
 
-template <int OP, uint32_t DTYPE> __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, 1))) void k_large(const Product p) {
+template <int OP, uint32_t DTYPE, int T> __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(T == 4 ? 1 : 2, T == 4 ? 1 : 2))) void k_direct(const Product p) {
+    constexpr int kSide = Tile<T>::kSide, kOperand = Tile<T>::kOperand, kLoads = Tile<T>::kLoads, N = T * T;
     constexpr bool kStridedA = OP == kWeightGrad, kStridedB = OP != kForward, kHalf = DTYPE == EDEN_F16, kCodes = OP == kWeightGrad;
     static_assert(!(kCodes && kHalf), "fp16 next to a checkpoint has two terms");
     __shared__ __attribute__((aligned(1024))) char lds[kSlots * kOperand];
@@ -203,50 +222,57 @@ template <int OP, uint32_t DTYPE> __global__ __launch_bounds__(kThreads) __attri
     const uint32_t begin = split * p.split_depth, end = min(p.depth, begin + p.split_depth);
     const uint32_t steps = (end - begin + kDeep - 1) / kDeep;      // begin < end: launched for depths above 0 only
 
-    Source<kStridedA> a(p.a, p.lda, row0, p.rows, begin, end, p.depth, wave, lane);
-    Source<kStridedB> b(p.b, kCodes ? 0 : p.ldb, col0, kCodes ? col0 + 1 : p.cols, begin, end, p.depth, wave, lane);
-    const int swap = kCodes ? wave_col * 2 : 0;
-    const Reader<kStridedA> reader_a(wave_row * 128, lane, swap);
-    const Reader<kStridedB> reader_b(wave_col * 128, lane);
-    Codes codes(p, col0, begin, end, tid);
+    Source<T, kStridedA> a(p.a, p.lda, row0, p.rows, begin, end, p.depth, wave, lane);
+    Source<T, kStridedB> b(p.b, kCodes ? 0 : p.ldb, col0, kCodes ? col0 + 1 : p.cols, begin, end, p.depth, wave, lane);
+    const int swap = kCodes ? wave_col * (T / 2) : 0;
+    const Reader<T, kStridedA> reader_a(wave_row * (kSide / 2), lane, swap);
+    const Reader<T, kStridedB> reader_b(wave_col * (kSide / 2), lane);
+    Codes<T> codes(p, col0, begin, end, tid);
 
-    f32x16 acc[4][4] = {};
-    float sums[2] = {0.0f, 0.0f};                                  // row sums of this lane's depths, of the tiles i = 0, 1: the two waves of a row
-                                                                   // of waves begin with different ones
+    f32x16 acc[T][T] = {};
+    float sums[T / 2] = {};                                        // row sums of this lane's depths, of the first half of the tiles: the two waves
+                                                                   // of a row of waves begin with different halves
     const bool with_sums = kCodes && p.row_sums && col_tile == 0;
-    u32x4 fa[2][4], fb[2][4];
+    u32x4 fa[2][T], fb[2][T];
 
     const uint32_t lds0 = (uint32_t)(size_t)(lds_char *)lds;
     auto depth_left = [&](uint32_t step) { return end - begin > step * kDeep ? end - begin - step * kDeep : 0u; };
-    auto read = [&](const char *slot_a, const char *slot_b, int s, int set, int i) {              // one operand of eight
-        if (i < 4) fb[set][i] = reader_b.read(slot_b, i, s);
-        else fa[set][i - 4] = reader_a.read(slot_a, i - 4, s);
+    auto read = [&](const char *slot_a, const char *slot_b, int s, int set, int i) {              // one operand of 2 T
+        if (i < T) fb[set][i] = reader_b.read(slot_b, i, s);
+        else fa[set][i - T] = reader_a.read(slot_a, i - T, s);
     };
-    // Sixteen products 16 deep: S = 0 .. 3 of a tile's 64.  The operands of the following ones are read, for S = 3 those of the next tiles, behind a
+    // T x T products 16 deep: S = 0 .. 3 of a tile's 64.  The operands of the following ones are read, for S = 3 those of the next tiles, behind a
     // barrier since when nobody needs the present ones.  Into their places go the second operand's tile after the next (S = 3 and the next 0)
     // and the first operand's after that (the next S = 1, 2).
     auto deep16 = [&](auto step16, const char *slot_a, const char *slot_b, uint32_t fetch_to, char *codes_to) {
-        constexpr int S = decltype(step16)::value, set = S & 1;
+        constexpr int S = decltype(step16)::value, set = S & 1, kReads = 2 * T, kHalf2 = kLoads / 2;
         u32x4 words;
-        each<16>([&](auto number) {
-            constexpr int j = decltype(number)::value;
-            acc[j >> 2][j & 3] = multiply<kHalf>(fb[set][j & 3], fa[set][j >> 2], acc[j >> 2][j & 3]);
+        each<N>([&](auto number) {
+            constexpr int j = decltype(number)::value, i = j / T;
+            acc[i][j % T] = multiply<kHalf>(fb[set][j % T], fa[set][i], acc[i][j % T]);
             if constexpr (S == 3 && j == 0) meet<kCodes ? 3 * kLoads : kLoads>();     // (later: the first operand's tile after the next; codes)
-            if constexpr (j & 1) read(slot_a, slot_b, (S + 1) & 3, set ^ 1, j >> 1);
-            if constexpr (j % 4 == 2) {                            // eight loads in two runs of sixteen
-                if constexpr (S == 1 || S == 2) a.fetch(fetch_to, wave, (S - 1) * 4 + j / 4);
-                else if constexpr (!kCodes) b.fetch(fetch_to, wave, (S == 3 ? 0 : 4) + j / 4);
+            // 2 T reads, kLoads / 2 loads, kLoads / 4 pieces of codes in N = T T products: T = 4: every second, fourth, eighth; T = 2: one each, two, four
+            if constexpr ((j + 1) * kReads / N != j * kReads / N) read(slot_a, slot_b, (S + 1) & 3, set ^ 1, j * kReads / N);
+            if constexpr (((2 * j + 1) * kHalf2 / N) % 2 == 1 && ((2 * j - 1) * kHalf2 / N) % 2 == 0) {
+                constexpr int load = j * kHalf2 / N;
+                if constexpr (S == 1 || S == 2) a.fetch(fetch_to, wave, (S - 1) * kHalf2 + load);
+                else if constexpr (!kCodes) b.fetch(fetch_to, wave, (S == 3 ? 0 : kHalf2) + load);
             }
             if constexpr (kCodes) {
-                constexpr int w = j >> 1, i = ((S + 1) & 3) * 2 + w / 4;                // two pieces of eight, from S = 3 on
-                if constexpr (!(j & 1)) words[w % 4] = codes.two(i, w % 4);
-                if constexpr (!(j & 1) && w % 4 == 3) codes.store(codes_to, tid, i, words);
-                if constexpr ((j & 1) && w % 4 == 3) codes.load(i);
+                constexpr int words_each = kLoads, w = j * words_each / N, piece = ((S + 1) & 3) * (kLoads / 4) + w / 4;         // from S = 3 on
+                if constexpr (j == 0 || (j - 1) * words_each / N != w) {
+                    words[w % 4] = codes.two(piece, w % 4);
+                    if constexpr (w % 4 == 3) {
+                        codes.store(codes_to, tid, piece, words);
+                        codes.load(piece);
+                    }
+                }
                 // row sums: two additions an instruction, cheaper for all than a branch
-                const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
-                if constexpr (j & 1) {
-                    const uint32_t pair = fa[set][j >> 3][(j >> 1) & 3];                // (a cast of the vector's element itself would take its first)
-                    sums[j >> 3] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), ones, sums[j >> 3], false);
+                constexpr int pairs = T / 2 * 4, q = j * pairs / N;
+                if constexpr (j == 0 || (j - 1) * pairs / N != q) {
+                    const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+                    const uint32_t pair = fa[set][q / 4][q % 4];                        // (a cast of the vector's element itself would take its first)
+                    sums[q / 4] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), ones, sums[q / 4], false);
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
@@ -269,7 +295,7 @@ template <int OP, uint32_t DTYPE> __global__ __launch_bounds__(kThreads) __attri
         for (int i = 0; i < kLoads; ++i) codes.load(i);
         codes.start();
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {                              // what S = 3 does
+        for (int i = 0; i < kLoads / 4; ++i) {                     // what S = 3 does
             codes.store(lds + 3 * kOperand, tid, i, u32x4{codes.two(i, 0), codes.two(i, 1), codes.two(i, 2), codes.two(i, 3)});
             codes.load(i);
         }
@@ -292,7 +318,7 @@ template <int OP, uint32_t DTYPE> __global__ __launch_bounds__(kThreads) __attri
     }
     meet<0>();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) read(lds, lds + kOperand, 0, 0, i);
+    for (int i = 0; i < 2 * T; ++i) read(lds, lds + kOperand, 0, 0, i);
     for (uint32_t step = 0; step < steps; ++step) {
         const uint32_t slot_b = on(slot, 1), next_a = on(slot, 2), next_b = on(slot, 3), after_a = on(slot, 4);
         deep16(std::integral_constant<int, 0>(), lds + slot, lds + slot_b, lds0 + next_b, lds + next_b);
@@ -307,41 +333,46 @@ template <int OP, uint32_t DTYPE> __global__ __launch_bounds__(kThreads) __attri
 
     if constexpr (kCodes) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < T / 2; ++i) {
             sums[i] += __shfl_xor(sums[i], 32);
-            if (with_sums && lane < 32) finish_row_sum(p, sums[i], row0 + wave_row * 128 + (i ^ swap) * 32 + lane, split);
+            if (with_sums && lane < 32) finish_row_sum(p, sums[i], row0 + wave_row * (kSide / 2) + (i ^ swap) * 32 + lane, split);
         }
     }
     meet<0>();                                                     // nothing is read or fetched any more: the LDS takes the sums, 32 rows of each wave at a time
-    float *mine = reinterpret_cast<float *>(lds) + wave * 32 * kRowFloats;
-    for (int i = 0; i < 4; ++i) {
+    float *mine = reinterpret_cast<float *>(lds) + wave * 32 * kRowFloats<T>;
+    for (int i = 0; i < T; ++i) {
         wave_fence();
-        auto put = [&](const f32x16 (&from)[4]) {
+        auto put = [&](const f32x16 (&from)[T]) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < T; ++j)
 #pragma unroll
                 for (int g = 0; g < 4; ++g)
-                    *reinterpret_cast<f32x4 *>(mine + (lane & 31) * kRowFloats + j * 32 + 8 * g + 4 * (lane >> 5)) =
+                    *reinterpret_cast<f32x4 *>(mine + (lane & 31) * kRowFloats<T> + j * 32 + 8 * g + 4 * (lane >> 5)) =
                         f32x4{from[j][4 * g], from[j][4 * g + 1], from[j][4 * g + 2], from[j][4 * g + 3]};
         };
         if (i == 0) put(acc[0]);
-        else if (i == 1) put(acc[1]);
-        else if (i == 2) put(acc[2]);
-        else put(acc[3]);
+        else if (T == 2 || i == 1) put(acc[1]);
+        else if (i == 2) put(acc[T / 2]);
+        else put(acc[T - 1]);
         wave_fence();
-        finish_rows<OP, DTYPE>(p, mine, row0 + wave_row * 128 + (i ^ swap) * 32, col0 + wave_col * 128, lane, split);
+        finish_rows<OP, DTYPE, T>(p, mine, row0 + wave_row * (kSide / 2) + (i ^ swap) * 32, col0 + wave_col * (kSide / 2), lane, split);
     }
 }
 
 }  // namespace
 
-hipError_t launch_large(Op op, uint32_t dtype, const Product &p, hipStream_t st) {
-    const uint32_t grid = ((p.rows + kSide - 1) / kSide) * ((p.cols + kSide - 1) / kSide) * p.splits;
-    if (op == kWeightGrad) k_large<kWeightGrad, EDEN_BF16><<<grid, kThreads, 0, st>>>(p);
-    else if (op == kForward && dtype == EDEN_F16) k_large<kForward, EDEN_F16><<<grid, kThreads, 0, st>>>(p);
-    else if (op == kForward) k_large<kForward, EDEN_BF16><<<grid, kThreads, 0, st>>>(p);
-    else if (dtype == EDEN_F16) k_large<kInputGrad, EDEN_F16><<<grid, kThreads, 0, st>>>(p);
-    else k_large<kInputGrad, EDEN_BF16><<<grid, kThreads, 0, st>>>(p);
+hipError_t launch_direct(Op op, uint32_t dtype, const Product &p, uint32_t side, hipStream_t st) {
+    const uint32_t grid = ((p.rows + side - 1) / side) * ((p.cols + side - 1) / side) * p.splits;
+    auto typed = [&](auto t) {
+        constexpr int T = decltype(t)::value;
+        if (op == kWeightGrad) k_direct<kWeightGrad, EDEN_BF16, T><<<grid, kThreads, 0, st>>>(p);
+        else if (op == kForward && dtype == EDEN_F16) k_direct<kForward, EDEN_F16, T><<<grid, kThreads, 0, st>>>(p);
+        else if (op == kForward) k_direct<kForward, EDEN_BF16, T><<<grid, kThreads, 0, st>>>(p);
+        else if (dtype == EDEN_F16) k_direct<kInputGrad, EDEN_F16, T><<<grid, kThreads, 0, st>>>(p);
+        else k_direct<kInputGrad, EDEN_BF16, T><<<grid, kThreads, 0, st>>>(p);
+    };
+    if (side == 256) typed(std::integral_constant<int, 4>());
+    else typed(std::integral_constant<int, 2>());
     return hipGetLastError();
 }
 
