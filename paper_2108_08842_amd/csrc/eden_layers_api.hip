@@ -58,10 +58,7 @@ bool fills_device(const Product &p) {
 int run(Op op, uint32_t dtype, Product &p, void *workspace, size_t workspace_bytes, void *stream) {
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return EDEN_ERR_INVALID_ARG;
-    if (op == kForward && p.rows <= kFewRows) {
-        // 32 columns a workgroup spare reads of x; 16 where that would leave CUs idle
-        return status(launch_rows(dtype, p, p.finish.codes_out != nullptr || p.cols > 32 * 512, st));
-    }
+    if (op == kForward && p.rows <= kFewRows) return status(launch_rows(dtype, p, st));
     const bool direct = is_direct(op, dtype, p);
     if (tile_count(p.rows, p.cols) > kMostGroups / 64) return EDEN_ERR_INVALID_ARG;
     if (direct && fills_device(p)) {

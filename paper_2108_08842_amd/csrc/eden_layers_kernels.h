@@ -32,9 +32,8 @@ __host__ __device__ inline uint32_t tiles_of(uint32_t n) { return n ? (n + kTile
 hipError_t launch_tiles(Op op, uint32_t dtype, const Product &p, hipStream_t st);
 // side: 128 or 256
 hipError_t launch_direct(Op op, uint32_t dtype, const Product &p, uint32_t side, hipStream_t st);
-constexpr uint32_t kFewRows = 64;
-// wide: 32 columns a workgroup (a checkpoint needs them), else 16
-hipError_t launch_rows(uint32_t dtype, const Product &p, bool wide, hipStream_t st);
+constexpr uint32_t kFewRows = 16;
+hipError_t launch_rows(uint32_t dtype, const Product &p, hipStream_t st);
 hipError_t launch_join(Op op, uint32_t dtype, const Product &p, hipStream_t st);
 
 hipError_t launch_save(uint32_t dtype, const void *x, size_t ldx, uint32_t rows, uint32_t cols, uint8_t *codes, uint8_t *exps, hipStream_t st);

@@ -1,6 +1,8 @@
-// eden_linear for up to 64 rows (single tokens, a few tokens at a time): the weights are read once and everything else is small.
+// eden_linear for up to 16 rows (single tokens, a few tokens at a time): the weights are read once and everything else is small.  Bound by memory: w's bytes.
 //
-// Bound by memory: w's bytes.  A workgroup has 16 or 32 columns of the result and all rows; its eight waves go through the depth in turn, 256 bytes of
+// k_dots, up to 8 rows: x lies in the LDS, a wave has one, two or four rows of w and reads a kilobyte of one at a time; every lane multiplies
+// its 16 bytes with those of x two elements an instruction, the lanes' sums are added at the end.
+// k_rows, up to 16 rows: a workgroup has 16 or 32 columns of the result and all rows; its eight waves go through the depth in turn, 256 bytes of
 // each of w's rows at a time, from memory to the matrix cores' registers without the LDS (lane l holds row l % 16 of w and 16 bytes of the
 // depth, so a load takes 64 bytes of 16 rows; the next chunk is on its way while one is multiplied).  16 x 16 products; fp32 operands
 // are multiplied in fp32.  The waves' sums meet in the LDS, in the order of the waves.
@@ -26,31 +28,51 @@ template <uint32_t DTYPE> __device__ inline f32x4 multiply16(u32x4 a, u32x4 b, f
     }
 }
 
-// COLS: sixteens of columns; ROWS: sixteens of rows
-template <uint32_t DTYPE, int COLS, int ROWS> __global__ __launch_bounds__(kWaves * 64) void k_rows(const Product p) {
+// The end of four neighbouring columns; BLOCK: eight lanes side by side have the 32 columns from col0 on.
+template <bool BLOCK, uint32_t DTYPE> __device__ inline void finish_quad(const Product &p, uint32_t row, uint32_t col0, uint32_t col, int valid, float (&v)[4]) {
+    if (valid) finish_bias<kForward, DTYPE>(p.finish, col, valid, v);
+    if constexpr (BLOCK)
+        if (p.finish.codes_out) {
+            uint32_t largest = 0;
+            float z[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                z[e] = e < valid ? v[e] : 0.0f;
+                largest = max(largest, magnitude_bits(z[e]));
+            }
+#pragma unroll
+            for (int step = 1; step < 8; step *= 2) largest = max(largest, (uint32_t)__shfl_xor((int)largest, step));
+            const uint32_t t = block_exponent(largest);
+            if (row < p.rows) {                                    // (the workgroup has a column: its block exists)
+                const size_t block = (size_t)row * p.finish.blocks + col0 / kBlock;
+                if (col == col0) p.finish.exps_out[block] = (uint8_t)t;
+                *reinterpret_cast<uint32_t *>(p.finish.codes_out + block * kBlock + (col - col0)) = codes4(z, t);
+            }
+        }
+    if (valid) finish_store<kForward, DTYPE>(p.finish, row, col, valid, v);
+}
+
+// COLS: sixteens of columns
+template <uint32_t DTYPE, int COLS> __global__ __launch_bounds__(kWaves * 64) void k_rows(const Product p) {
     using T = typename Elem<DTYPE>::type;
     constexpr int kPiece = 16 / Elem<DTYPE>::kBytes, kStep = 4 * kPiece, kChunk = kSteps * kStep;
-    __shared__ f32x4 sums[kWaves][COLS][ROWS][64];
+    __shared__ f32x4 sums[kWaves][COLS][64];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t col0 = blockIdx.x * (16 * COLS);
-    const T *w[COLS], *x[ROWS];
-    bool has_w[COLS], has_x[ROWS];
+    const T *w[COLS];
+    bool has_w[COLS];
 #pragma unroll
     for (int c = 0; c < COLS; ++c) {
         const uint32_t col = col0 + c * 16 + (lane & 15);
         has_w[c] = col < p.cols;
         w[c] = static_cast<const T *>(p.b) + (size_t)(has_w[c] ? col : 0) * p.ldb + (lane >> 4) * kPiece;
     }
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-        const uint32_t row = r * 16 + (lane & 15);
-        has_x[r] = row < p.rows;
-        x[r] = static_cast<const T *>(p.a) + (size_t)(has_x[r] ? row : 0) * p.lda + (lane >> 4) * kPiece;
-    }
+    const bool has_x = (lane & 15u) < p.rows;
+    const T *x = static_cast<const T *>(p.a) + (has_x ? (lane & 15) : 0) * p.lda + (lane >> 4) * kPiece;
 
-    f32x4 acc[COLS][ROWS] = {};
-    struct Chunk { Vec<T, kPiece> w[kSteps][COLS], x[kSteps][ROWS]; };
+    f32x4 acc[COLS] = {};
+    struct Chunk { Vec<T, kPiece> w[kSteps][COLS], x[kSteps]; };
     auto load = [&](Chunk &to, uint32_t k) {                       // what is outside the operands is 0
         const bool full = k + kChunk <= p.depth;
 #pragma unroll
@@ -59,8 +81,7 @@ template <uint32_t DTYPE, int COLS, int ROWS> __global__ __launch_bounds__(kWave
             const int valid = full ? kPiece : piece < p.depth ? (int)min((uint32_t)kPiece, p.depth - piece) : 0;
 #pragma unroll
             for (int c = 0; c < COLS; ++c) to.w[s][c] = load_some<T, kPiece>(w[c] + at, has_w[c] ? valid : 0);
-#pragma unroll
-            for (int r = 0; r < ROWS; ++r) to.x[s][r] = load_some<T, kPiece>(x[r] + at, has_x[r] ? valid : 0);
+            to.x[s] = load_some<T, kPiece>(x + at, has_x ? valid : 0);
         }
     };
     auto multiply = [&](const Chunk &from) {
@@ -68,9 +89,7 @@ template <uint32_t DTYPE, int COLS, int ROWS> __global__ __launch_bounds__(kWave
         for (int s = 0; s < kSteps; ++s)
 #pragma unroll
             for (int c = 0; c < COLS; ++c)
-#pragma unroll
-                for (int r = 0; r < ROWS; ++r)
-                    acc[c][r] = multiply16<DTYPE>(__builtin_bit_cast(u32x4, from.w[s][c]), __builtin_bit_cast(u32x4, from.x[s][r]), acc[c][r]);
+                acc[c] = multiply16<DTYPE>(__builtin_bit_cast(u32x4, from.w[s][c]), __builtin_bit_cast(u32x4, from.x[s]), acc[c]);
     };
     constexpr uint32_t kStride = kWaves * kChunk;
     Chunk even, odd;
@@ -88,58 +107,168 @@ template <uint32_t DTYPE, int COLS, int ROWS> __global__ __launch_bounds__(kWave
         }
     }
 #pragma unroll
-    for (int c = 0; c < COLS; ++c)
-#pragma unroll
-        for (int r = 0; r < ROWS; ++r) sums[wave][c][r][lane] = acc[c][r];
+    for (int c = 0; c < COLS; ++c) sums[wave][c][lane] = acc[c];
     __syncthreads();
 
     // thread -> row and four columns; 4 COLS threads side by side have a row (COLS = 2: a block of a checkpoint)
     constexpr int kQuads = 4 * COLS;
-    for (int t = tid; t < 16 * ROWS * kQuads; t += kWaves * 64) {
-        const int row = t / kQuads, quad = t % kQuads;
-        f32x4 sum = sums[0][quad >> 2][row >> 4][(quad & 3) * 16 + (row & 15)];
+    if (tid < 16 * kQuads) {
+        const int row = tid / kQuads, quad = tid % kQuads;
+        f32x4 sum = sums[0][quad >> 2][(quad & 3) * 16 + row];
 #pragma unroll
-        for (int i = 1; i < kWaves; ++i) sum += sums[i][quad >> 2][row >> 4][(quad & 3) * 16 + (row & 15)];
+        for (int i = 1; i < kWaves; ++i) sum += sums[i][quad >> 2][(quad & 3) * 16 + row];
         const uint32_t col = col0 + quad * 4;
         const int valid = (uint32_t)row < p.rows && col < p.cols ? (int)min(4u, p.cols - col) : 0;
         float v[4] = {sum[0], sum[1], sum[2], sum[3]};
-        if (valid) finish_bias<kForward, DTYPE>(p.finish, col, valid, v);
-        if constexpr (COLS == 2)
-            if (p.finish.codes_out) {
-                uint32_t largest = 0;
-                float z[4];
+        finish_quad<COLS == 2, DTYPE>(p, row, col0, col, valid, v);
+    }
+}
+
+// c + a . b for the eight (fp32: four) elements of two pieces, the fp32 sums in the order of the elements
+template <uint32_t DTYPE> __device__ inline float dot_piece(u32x4 a, u32x4 b, float c) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    z[e] = e < valid ? v[e] : 0.0f;
-                    largest = max(largest, magnitude_bits(z[e]));
-                }
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t x = a[i], y = b[i];
+        if constexpr (DTYPE == EDEN_F32) c = __builtin_fmaf(__uint_as_float(x), __uint_as_float(y), c);
+        else if constexpr (DTYPE == EDEN_F16) c = __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, x), __builtin_bit_cast(f16x2, y), c, false);
+        else c = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, x), __builtin_bit_cast(bf16x2, y), c, false);
+    }
+    return c;
+}
+
+// The sums over the wave's lanes of N values a lane (N a power of two up to 64): value i ends up in the lanes whose upper log2 N bits are i.  Half of the
+// values change sides at a time, so that N values take N + 5 exchanges and not 6 N.
+template <int N, int DISTANCE = 32> __device__ inline float sum_lanes(const float (&v)[N], int lane) {
+    if constexpr (N > 1) {
+        const bool upper = lane & DISTANCE;
+        float half[N / 2];
 #pragma unroll
-                for (int step = 1; step < 8; step *= 2) largest = max(largest, (uint32_t)__shfl_xor((int)largest, step));
-                const uint32_t exponent = block_exponent(largest);
-                if ((uint32_t)row < p.rows) {                      // (the workgroup has a column: its block exists)
-                    const size_t block = (size_t)row * p.finish.blocks + col0 / kBlock;
-                    if (quad == 0) p.finish.exps_out[block] = (uint8_t)exponent;
-                    *reinterpret_cast<uint32_t *>(p.finish.codes_out + block * kBlock + quad * 4) = codes4(z, exponent);
-                }
+        for (int i = 0; i < N / 2; ++i) half[i] = (upper ? v[i + N / 2] : v[i]) + __shfl_xor(upper ? v[i] : v[i + N / 2], DISTANCE);
+        return sum_lanes<N / 2, DISTANCE / 2>(half, lane);
+    } else {
+        float sum = v[0];
+#pragma unroll
+        for (int d = DISTANCE; d >= 1; d /= 2) sum += __shfl_xor(sum, d);
+        return sum;
+    }
+}
+
+constexpr size_t kMostShared = 61440;              // bytes of x in the LDS: two workgroups a CU at least
+template <uint32_t DTYPE> size_t shared_bytes(uint32_t depth, int rows) {
+    constexpr uint32_t kRun = 1024 / Elem<DTYPE>::kBytes;          // elements of a wave's load
+    return (size_t)((depth + kRun - 1) / kRun) * 1024 * rows;
+}
+
+// EACH: rows of w a wave has; ROWS: rows of x (a power of two, those beyond p.rows are zeros)
+template <uint32_t DTYPE, int EACH, int ROWS> __global__ __launch_bounds__(kWaves * 64) void k_dots(const Product p) {
+    using T = typename Elem<DTYPE>::type;
+    constexpr int kPiece = 16 / Elem<DTYPE>::kBytes, kRun = 8 / EACH, kCols = kWaves * EACH;      // pieces of a row on their way at once
+    extern __shared__ u32x4 shared[];                              // x: row r, piece i at r * pieces + i; then the sums
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t pieces = (p.depth + kPiece * 64 - 1) / (kPiece * 64) * 64;                     // a lane has one of every 64
+    const uint32_t col0 = blockIdx.x * kCols, first = col0 + wave * EACH;
+    const T *w[EACH];
+    bool has[EACH];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+        has[e] = first + e < p.cols;
+        w[e] = static_cast<const T *>(p.b) + (size_t)(has[e] ? first + e : 0) * p.ldb + lane * kPiece;
+    }
+    struct Run { u32x4 q[kRun][EACH]; };
+    auto load = [&](Run &to, uint32_t piece) {                     // what is outside w is 0
+        const bool full = (piece + kRun * 64) * kPiece <= p.depth;
+#pragma unroll
+        for (int i = 0; i < kRun; ++i) {
+            const uint32_t at = (piece + i * 64) * kPiece, mine = at + lane * kPiece;
+            const int valid = full ? kPiece : mine < p.depth ? (int)min((uint32_t)kPiece, p.depth - mine) : 0;
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) to.q[i][e] = __builtin_bit_cast(u32x4, load_some<T, kPiece>(w[e] + at, has[e] ? valid : 0));
+        }
+    };
+    Run even, odd;
+    load(even, 0);                                                 // w is on its way while x is fetched
+    for (uint32_t i = tid; i < ROWS * pieces; i += kWaves * 64) {
+        const uint32_t row = i / pieces, k = (i - row * pieces) * kPiece;
+        const int valid = row < p.rows && k < p.depth ? (int)min((uint32_t)kPiece, p.depth - k) : 0;
+        shared[i] = __builtin_bit_cast(u32x4, load_some<T, kPiece>(static_cast<const T *>(p.a) + (row < p.rows ? row * p.lda + k : 0), valid));
+    }
+    __syncthreads();
+
+    float sums[EACH * ROWS] = {};
+    auto multiply = [&](const Run &from, uint32_t piece) {
+#pragma unroll
+        for (int i = 0; i < kRun; ++i) {
+            if (piece + i * 64 >= pieces) break;
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                const u32x4 x = shared[r * pieces + piece + i * 64 + lane];
+#pragma unroll
+                for (int e = 0; e < EACH; ++e) sums[e * ROWS + r] = dot_piece<DTYPE>(from.q[i][e], x, sums[e * ROWS + r]);
             }
-        if (valid) finish_store<kForward, DTYPE>(p.finish, row, col, valid, v);
+        }
+    };
+    for (uint32_t piece = 0; piece < pieces;) {
+        if (piece + kRun * 64 < pieces) load(odd, piece + kRun * 64);
+        multiply(even, piece);
+        piece += kRun * 64;
+        if (piece >= pieces) break;
+        if (piece + kRun * 64 < pieces) load(even, piece + kRun * 64);
+        multiply(odd, piece);
+        piece += kRun * 64;
+    }
+    float *out = reinterpret_cast<float *>(shared + ROWS * pieces);                               // [ROWS][kCols]
+    const float sum = sum_lanes<EACH * ROWS>(sums, lane);
+    constexpr int kSame = 64 / (EACH * ROWS);                                                     // lanes with the same sum
+    if (lane % kSame == 0) out[lane / kSame % ROWS * kCols + wave * EACH + lane / kSame / ROWS] = sum;
+    __syncthreads();
+
+    constexpr int kQuads = kCols / 4;                              // EACH = 4: a block of a checkpoint
+    if (tid < ROWS * kQuads) {
+        const int row = tid / kQuads, quad = tid % kQuads;
+        const uint32_t col = col0 + quad * 4;
+        const int valid = (uint32_t)row < p.rows && col < p.cols ? (int)min(4u, p.cols - col) : 0;
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = out[row * kCols + quad * 4 + i];
+        finish_quad<kCols == kBlock, DTYPE>(p, row, col0, col, valid, v);
     }
 }
 
 template <uint32_t DTYPE, int COLS> void launch(const Product &p, hipStream_t st) {
-    const uint32_t grid = (p.cols + 16 * COLS - 1) / (16 * COLS);
-    if (p.rows <= 16) k_rows<DTYPE, COLS, 1><<<grid, kWaves * 64, 0, st>>>(p);
-    else if (p.rows <= 32) k_rows<DTYPE, COLS, 2><<<grid, kWaves * 64, 0, st>>>(p);
-    else k_rows<DTYPE, COLS, 4><<<grid, kWaves * 64, 0, st>>>(p);
+    k_rows<DTYPE, COLS><<<(p.cols + 16 * COLS - 1) / (16 * COLS), kWaves * 64, 0, st>>>(p);
+}
+template <uint32_t DTYPE, int EACH> void launch_dots(const Product &p, hipStream_t st) {
+    const uint32_t grid = (p.cols + kWaves * EACH - 1) / (kWaves * EACH);
+    auto with_rows = [&](auto rows) {
+        constexpr int ROWS = decltype(rows)::value;
+        k_dots<DTYPE, EACH, ROWS><<<grid, kWaves * 64, shared_bytes<DTYPE>(p.depth, ROWS) + ROWS * kWaves * EACH * sizeof(float), st>>>(p);
+    };
+    if (p.rows == 1) with_rows(std::integral_constant<int, 1>());
+    else if (p.rows == 2) with_rows(std::integral_constant<int, 2>());
+    else if (p.rows <= 4) with_rows(std::integral_constant<int, 4>());
+    else with_rows(std::integral_constant<int, 8>());
+}
+template <uint32_t DTYPE> hipError_t launch_type(const Product &p, hipStream_t st) {
+    const bool keeps = p.finish.codes_out != nullptr;              // a checkpoint's block is 32 columns
+    const int rows = p.rows == 1 ? 1 : p.rows == 2 ? 2 : p.rows <= 4 ? 4 : 8;
+    if (p.rows <= 8 && shared_bytes<DTYPE>(p.depth, rows) <= kMostShared) {
+        // several rows of w a wave read x less often; fewer leave no CU idle
+        if (keeps || p.cols >= 512 * 32) launch_dots<DTYPE, 4>(p, st);
+        else if (p.cols >= 512 * 16) launch_dots<DTYPE, 2>(p, st);
+        else launch_dots<DTYPE, 1>(p, st);
+    } else {
+        if (keeps) launch<DTYPE, 2>(p, st);
+        else launch<DTYPE, 1>(p, st);
+    }
+    return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_rows(uint32_t dtype, const Product &p, bool wide, hipStream_t st) {
-    if (dtype == EDEN_F32) wide ? launch<EDEN_F32, 2>(p, st) : launch<EDEN_F32, 1>(p, st);
-    else if (dtype == EDEN_F16) wide ? launch<EDEN_F16, 2>(p, st) : launch<EDEN_F16, 1>(p, st);
-    else wide ? launch<EDEN_BF16, 2>(p, st) : launch<EDEN_BF16, 1>(p, st);
-    return hipGetLastError();
+hipError_t launch_rows(uint32_t dtype, const Product &p, hipStream_t st) {
+    if (dtype == EDEN_F32) return launch_type<EDEN_F32>(p, st);
+    if (dtype == EDEN_F16) return launch_type<EDEN_F16>(p, st);
+    return launch_type<EDEN_BF16>(p, st);
 }
 
 }  // namespace eden_layers
