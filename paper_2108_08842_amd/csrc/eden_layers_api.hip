@@ -2,6 +2,8 @@
 // choice of a kernel, launches.
 #include "eden_layers_kernels.h"
 
+#include <algorithm>
+
 using namespace eden_layers;
 
 namespace {
@@ -26,17 +28,27 @@ size_t codes_bytes(uint64_t rows, uint64_t cols) { return rows * blocks_of(cols)
 // Element-wise launches: at least 1024 values a workgroup but for the ends of rows
 bool launchable(uint64_t rows, uint64_t cols) { return rows * (blocks_of(cols) / 64 + 1) <= kMostGroups; }
 
-uint64_t tile_count(uint64_t rows, uint64_t cols) { return (uint64_t)tiles_of((uint32_t)rows) * tiles_of((uint32_t)cols); }
+uint64_t tile_count(uint64_t rows, uint64_t cols, uint32_t side) { return (uint64_t)tiles_of((uint32_t)rows, side) * tiles_of((uint32_t)cols, side); }
 size_t partial_bytes(uint64_t rows, uint64_t cols, uint64_t splits) { return splits * rows * ((cols + 3) / 4 * 4 + 1) * sizeof(float); }
 
-// How many workgroups share a tile's sum.  The device holds two tiles per CU, 512 in all; a sum of less than 256 is not worth the join.
-uint64_t splits_of(uint64_t rows, uint64_t cols, uint64_t depth) {
-    if (rows == 0 || cols == 0) return 1;
-    const uint64_t tiles = tile_count(rows, cols);
-    if (tiles > 256) return 1;
-    uint64_t s = 512 / tiles;
-    if (s > depth / 256) s = depth / 256;
+// How many workgroups share a tile's sum: `slots` of them fit the device together, and one has at least `least` of the depth.
+uint64_t splits_of(uint64_t tiles, uint64_t depth, uint64_t slots, uint64_t least) {
+    const uint64_t s = std::min(slots / tiles, depth / least);
     return s < 1 ? 1 : s > 64 ? 64 : s;
+}
+struct Shape {
+    uint32_t side;
+    uint64_t splits;
+};
+// Loads straight into the LDS: 256 x 256 tiles where those give every CU work, else 128 x 128, two to a CU.
+Shape direct_shape(uint64_t rows, uint64_t cols, uint64_t depth) {
+    if (tile_count(rows, cols, 256) >= 192) return {256, 1};
+    return {128, splits_of(tile_count(rows, cols, 128), depth, 512, 256)};
+}
+// Through registers: 128 x 128 where those fill the device, else 64 x 64, three or more to a CU.
+Shape tiles_shape(uint64_t rows, uint64_t cols, uint64_t depth) {
+    if (tile_count(rows, cols, 128) >= 256) return {128, 1};
+    return {64, splits_of(tile_count(rows, cols, 64), depth, 768, 128)};
 }
 
 // Rows that start at, and hold, whole 16-byte pieces, and offsets inside a tile that 31 bits hold
@@ -49,23 +61,15 @@ bool is_direct(Op op, uint32_t dtype, const Product &p) {
     if (!whole_pieces(p.a, p.lda, op == kWeightGrad ? p.rows : p.depth)) return false;
     return op == kWeightGrad ? p.ldb < (1u << 24) : whole_pieces(p.b, p.ldb, op == kForward ? p.depth : p.cols);
 }
-// ... and whether its tiles of 256 x 256 give every CU work
-bool fills_device(const Product &p) {
-    return (uint64_t)((p.rows + kLargeTile - 1) / kLargeTile) * ((p.cols + kLargeTile - 1) / kLargeTile) >= 192;
-}
-
 // Launches a product whose operands and end are set.
 int run(Op op, uint32_t dtype, Product &p, void *workspace, size_t workspace_bytes, void *stream) {
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return EDEN_ERR_INVALID_ARG;
     if (op == kForward && p.rows <= kFewRows) return status(launch_rows(dtype, p, st));
     const bool direct = is_direct(op, dtype, p);
-    if (tile_count(p.rows, p.cols) > kMostGroups / 64) return EDEN_ERR_INVALID_ARG;
-    if (direct && fills_device(p)) {
-        p.splits = 1, p.split_depth = p.depth;
-        return status(launch_direct(op, dtype, p, kLargeTile, st));
-    }
-    uint64_t splits = splits_of(p.rows, p.cols, p.depth);
+    const Shape shape = direct ? direct_shape(p.rows, p.cols, p.depth) : tiles_shape(p.rows, p.cols, p.depth);
+    if (tile_count(p.rows, p.cols, shape.side) > kMostGroups / 64) return EDEN_ERR_INVALID_ARG;
+    uint64_t splits = shape.splits;
     if (workspace == nullptr) workspace_bytes = 0;
     while (splits > 1 && partial_bytes(p.rows, p.cols, splits) > workspace_bytes) --splits;
     const uint64_t each = ((p.depth + splits - 1) / splits + kSplitUnit - 1) / kSplitUnit * kSplitUnit;
@@ -74,7 +78,7 @@ int run(Op op, uint32_t dtype, Product &p, void *workspace, size_t workspace_byt
     p.split_depth = (uint32_t)each;
     p.partial = static_cast<float *>(workspace);
     p.partial_ld = (p.cols + 3) / 4 * 4;
-    hipError_t e = direct ? launch_direct(op, dtype, p, kTile, st) : launch_tiles(op, dtype, p, st);
+    hipError_t e = direct ? launch_direct(op, dtype, p, shape.side, st) : launch_tiles(op, dtype, p, shape.side, st);
     if (e == hipSuccess && p.splits > 1) e = launch_join(op, dtype, p, st);
     return status(e);
 }
@@ -107,7 +111,8 @@ int eden_checkpoint_restore(const void *checkpoint, uint64_t rows, uint64_t cols
 
 size_t eden_layers_workspace_bytes(uint64_t rows, uint64_t cols, uint64_t depth, uint32_t dtype) {
     if (!known_type(dtype) || rows > kMostSize || cols > kMostSize || depth > kMostSize) return 0;
-    const uint64_t splits = splits_of(rows, cols, depth);
+    if (rows == 0 || cols == 0) return 0;
+    const uint64_t splits = std::max(direct_shape(rows, cols, depth).splits, tiles_shape(rows, cols, depth).splits);
     return splits > 1 ? partial_bytes(rows, cols, splits) : 0;
 }
 

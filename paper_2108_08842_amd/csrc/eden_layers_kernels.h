@@ -23,13 +23,12 @@ struct Product {
     uint32_t splits, split_depth;  // of a split, a multiple of kSplitUnit
 };
 
-constexpr uint32_t kTile = 128;       // rows and columns of the general kernel's tiles
-constexpr uint32_t kLargeTile = 256;  // of the kernel for large results
 constexpr uint32_t kSplitUnit = 64;   // the depth is split at multiples of this
 // (a result without columns still has row sums: one tile)
-__host__ __device__ inline uint32_t tiles_of(uint32_t n) { return n ? (n + kTile - 1) / kTile : 1; }
+__host__ __device__ inline uint32_t tiles_of(uint32_t n, uint32_t side) { return n ? (n + side - 1) / side : 1; }
 
-hipError_t launch_tiles(Op op, uint32_t dtype, const Product &p, hipStream_t st);
+// side: of the tiles, 64 or 128
+hipError_t launch_tiles(Op op, uint32_t dtype, const Product &p, uint32_t side, hipStream_t st);
 // side: 128 or 256
 hipError_t launch_direct(Op op, uint32_t dtype, const Product &p, uint32_t side, hipStream_t st);
 constexpr uint32_t kFewRows = 16;

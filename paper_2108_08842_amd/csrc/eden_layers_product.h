@@ -12,7 +12,9 @@ template <int DEPTH> __device__ inline int piece_of_row(int row, int piece) {
     return row * (DEPTH * 2) + ((DEPTH == 64 ? piece ^ ((row >> 1) & 7) : piece ^ ((row >> 2) & 3)) << 4);
 }
 // Rows of columns: 32 columns at four neighbouring depths do.
-template <int WIDTH> __device__ inline int piece_of_depth(int depth, int piece) { return depth * (WIDTH * 2) + ((piece ^ (4 * (depth & 3))) << 4); }
+template <int WIDTH> __device__ inline int piece_of_depth(int depth, int piece) {
+    return depth * (WIDTH * 2) + ((WIDTH == 64 ? piece ^ (2 * (depth & 2)) : piece ^ (4 * (depth & 3))) << 4);
+}
 
 // x = term + rest, term = the upper 16 bits (exact; an infinity leaves nothing, a NaN a NaN)
 __device__ inline float take_term(float &x) {

@@ -1,7 +1,8 @@
 // Matrix products of the layer operators for any size, distance, alignment and type.
 //
 // out[r][c] = sum_d A(r, d) B(c, d) on the matrix cores, 32 x 32 x 16 products of bf16 (fp16 where both operands are fp16) summed in fp32.
-// A workgroup of four waves has a tile of 128 x 128, a wave 64 x 64 of it.  Operands go through registers into the LDS, where
+// A workgroup of four waves has a tile of 128 x 128, a wave 64 x 64 of it; where such tiles would leave most of the device idle and each step
+// of a few workgroups would be waited for, 64 x 64 and 32 x 32.  Operands go through registers into the LDS, where
 // those that the matrix cores cannot take are turned into bf16 terms that add up to them exactly:
 //   fp32                three terms of 8 bits; fp16 next to a checkpoint: two.  With three on both sides the products below 2^-24 are left out.
 //   8-bit checkpoint    q 2^(t - 127) itself: seven bits.
@@ -16,23 +17,39 @@ namespace {
 
 constexpr int kThreads = 256;
 
-template <int OP, uint32_t DTYPE> struct Plan {
+// W: a wave has W x W products of 32 x 32, a workgroup 64 W x 64 W
+template <int OP, uint32_t DTYPE, int W> struct Plan {
     static constexpr bool kTwoBytes = DTYPE != EDEN_F32;
     static constexpr int kTermsA = DTYPE == EDEN_F32 ? 3 : (OP == kWeightGrad && DTYPE == EDEN_F16) ? 2 : 1;
     static constexpr int kTermsB = OP == kWeightGrad ? 1 : DTYPE == EDEN_F32 ? 3 : 1;
     static constexpr bool kHalf = DTYPE == EDEN_F16 && OP != kWeightGrad;      // fp16 products
     static constexpr bool kStridedA = OP == kWeightGrad, kStridedB = OP != kForward;
-    // one term: 64 deep, two stages (64 KiB, two workgroups per CU); more: 32 deep, one stage (up to 48 KiB)
-    static constexpr int kDepth = kTermsA * kTermsB == 1 ? 64 : 32;
+    static constexpr int kSide = 64 * W;
+    // tiles of 128, one term: 64 deep, two stages (64 KiB, two workgroups per CU); more terms: 32 deep, one stage (up to 48 KiB).  Tiles of 64: 64 deep.
+    static constexpr int kDepth = W == 1 || kTermsA * kTermsB == 1 ? 64 : 32;
     static constexpr int kStages = kTermsA * kTermsB == 1 ? 2 : 1;
-    static constexpr int kPlane = (int)kTile * kDepth * 2;                     // bytes of one term of an operand's tile
+    static constexpr int kPlane = kSide * kDepth * 2;                          // bytes of one term of an operand's tile
     static constexpr int kStageBytes = (kTermsA + kTermsB) * kPlane;
-    static constexpr int kPieces = (int)kTile * kDepth / 8 / kThreads;         // pieces of 8 elements per thread and operand
+    static constexpr int kPieces = kSide * kDepth / 8 / kThreads;              // pieces of 8 elements per thread and operand
 };
 
 // Eight elements of an operand on their way from memory to the LDS.
 template <uint32_t DTYPE> struct Piece { Vec<typename Elem<DTYPE>::type, 8> v; };
 struct CodePiece { u32x4 codes; uint32_t exponent; };              // 16 codes
+
+// Eight neighbouring elements of an operand, those from `valid` on as zeros.  Read as one vector wherever that ends before the operand
+// does (`end`); what it takes from the next row is dropped.
+template <class T> __device__ inline Vec<T, 8> load_row_piece(const T *at, const T *end, int valid) {
+    Vec<T, 8> r;
+    if (valid > 0 && at + 8 <= end) {
+        r = load_some<T, 8>(at, 8);
+#pragma unroll
+        for (int i = 1; i < 8; ++i) r.v[i] = i < valid ? r.v[i] : (T)0.0f;
+    } else {
+        r = load_some<T, 8>(at, min(valid, 7));
+    }
+    return r;
+}
 
 template <uint32_t DTYPE, int TERMS> __device__ inline void store_piece(char *lds, int plane, const Piece<DTYPE> &p) {
     if constexpr (TERMS == 1) {
@@ -55,138 +72,145 @@ template <uint32_t DTYPE, int TERMS> __device__ inline void store_piece(char *ld
     }
 }
 
-template <int OP, uint32_t DTYPE> __global__ __launch_bounds__(kThreads, 2) void k_tiles(const Product p) {
-    using P = Plan<OP, DTYPE>;
+template <int OP, uint32_t DTYPE, int W> __global__ __launch_bounds__(kThreads, W == 1 ? 3 : 2) void k_tiles(const Product p) {
+    using P = Plan<OP, DTYPE, W>;
     using T = typename Elem<DTYPE>::type;
     constexpr int D = P::kDepth, N = P::kPieces;
+    constexpr uint32_t kSide = P::kSide, kAcross = kSide / 8;         // pieces of a row of columns
     __shared__ __attribute__((aligned(16))) char lds[P::kStages * P::kStageBytes];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wave_row = wave >> 1, wave_col = wave & 1;
-    const uint32_t row_tiles = tiles_of(p.rows), col_tiles = tiles_of(p.cols);
+    const uint32_t row_tiles = tiles_of(p.rows, kSide), col_tiles = tiles_of(p.cols, kSide);
     uint32_t split, row_tile, col_tile;
     place_of(blockIdx.x, gridDim.x, row_tiles, col_tiles, split, row_tile, col_tile);
-    const uint32_t row0 = row_tile * kTile, col0 = col_tile * kTile;
+    const uint32_t row0 = row_tile * kSide, col0 = col_tile * kSide;
     const uint32_t begin = split * p.split_depth, end = min(p.depth, begin + p.split_depth);
-    const bool inside = row0 + kTile <= p.rows && col0 + kTile <= p.cols;      // of the codes: up to the row's last whole block
+    const bool inside = row0 + kSide <= p.rows && col0 + kSide <= p.cols;      // of the codes: up to the row's last whole block
 
-    Piece<DTYPE> a[N], b[OP == kWeightGrad ? 1 : N];
-    CodePiece codes[OP == kWeightGrad ? N / 2 : 1];
+    struct Set {
+        Piece<DTYPE> a[N], b[OP == kWeightGrad ? 1 : N];
+        CodePiece codes[OP == kWeightGrad ? N / 2 : 1];
+    };
+    // behind the last element of an operand
+    const T *end_a = static_cast<const T *>(p.a) + (size_t)((P::kStridedA ? p.depth : p.rows) - 1) * p.lda + (P::kStridedA ? p.rows : p.depth);
+    const T *end_b = OP == kWeightGrad ? nullptr : static_cast<const T *>(p.b) + (size_t)((P::kStridedB ? p.depth : p.cols) - 1) * p.ldb + (P::kStridedB ? p.cols : p.depth);
 
     // pieces of a tile at one depth: piece i of this thread is number i * kThreads + tid, along the rows of memory
-    auto load_operand = [&](Piece<DTYPE> (&r)[N], const T *base, size_t ld, bool strided, uint32_t first, uint32_t count, uint32_t k, bool full) {
+    auto load_operand = [&](Piece<DTYPE> (&r)[N], const T *base, const T *base_end, size_t ld, bool strided, uint32_t first, uint32_t count, uint32_t k, bool full) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const uint32_t c = (uint32_t)(i * kThreads + tid), per_row = strided ? kTile / 8 : D / 8;
+            const uint32_t c = (uint32_t)(i * kThreads + tid), per_row = strided ? kAcross : D / 8;
             const uint32_t outer = c / per_row, inner = c % per_row * 8;
             const uint32_t row = strided ? k + outer : first + outer, col = strided ? first + inner : k + inner;
             const uint32_t rows = strided ? end : count, cols = strided ? count : end;
             const T *at = base + (size_t)row * ld + col;
             if (full) r[i].v = load_some<T, 8>(at, 8);
-            else r[i].v = load_some<T, 8>(at, row < rows ? (int)min(8u, cols > col ? cols - col : 0u) : 0);
+            else r[i].v = load_row_piece(at, base_end, row < rows ? (int)min(8u, cols > col ? cols - col : 0u) : 0);
         }
     };
-    auto load = [&](uint32_t k) {
+    auto load = [&](Set &to, uint32_t k) {
         const bool full = inside && k + D <= end;
-        load_operand(a, static_cast<const T *>(p.a), p.lda, P::kStridedA, row0, p.rows, k, full);
+        load_operand(to.a, static_cast<const T *>(p.a), end_a, p.lda, P::kStridedA, row0, p.rows, k, full);
         if constexpr (OP != kWeightGrad) {
-            load_operand(b, static_cast<const T *>(p.b), p.ldb, P::kStridedB, col0, p.cols, k, full);
+            load_operand(to.b, static_cast<const T *>(p.b), end_b, p.ldb, P::kStridedB, col0, p.cols, k, full);
         } else {
 #pragma unroll
             for (int i = 0; i < N / 2; ++i) {
-                const uint32_t c = (uint32_t)(i * kThreads + tid), row = k + c / 8, col = col0 + c % 8 * 16;
+                const uint32_t c = (uint32_t)(i * kThreads + tid), row = k + c / (kAcross / 2), col = col0 + c % (kAcross / 2) * 16;
                 if (row < end && col < p.b_blocks * kBlock) {
-                    codes[i].codes = *reinterpret_cast<const u32x4 *>(static_cast<const uint8_t *>(p.b) + (size_t)row * p.ldb + col);
-                    codes[i].exponent = p.b_exps[(size_t)row * p.b_blocks + col / kBlock];
+                    to.codes[i].codes = *reinterpret_cast<const u32x4 *>(static_cast<const uint8_t *>(p.b) + (size_t)row * p.ldb + col);
+                    to.codes[i].exponent = p.b_exps[(size_t)row * p.b_blocks + col / kBlock];
                 } else {
-                    codes[i].codes = u32x4{0, 0, 0, 0};
-                    codes[i].exponent = 1;
+                    to.codes[i].codes = u32x4{0, 0, 0, 0};
+                    to.codes[i].exponent = 1;
                 }
             }
         }
     };
-    auto store = [&](char *stage) {
+    auto store = [&](char *stage, const Set &from) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int c = i * kThreads + tid;
-            store_piece<DTYPE, P::kTermsA>(stage + (P::kStridedA ? piece_of_depth<kTile>(c / 16, c % 16) : piece_of_row<D>(c / (D / 8), c % (D / 8))), P::kPlane, a[i]);
+            store_piece<DTYPE, P::kTermsA>(stage + (P::kStridedA ? piece_of_depth<P::kSide>(c / kAcross, c % kAcross) : piece_of_row<D>(c / (D / 8), c % (D / 8))), P::kPlane, from.a[i]);
         }
         char *second = stage + P::kTermsA * P::kPlane;
         if constexpr (OP != kWeightGrad) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const int c = i * kThreads + tid;
-                store_piece<DTYPE, P::kTermsB>(second + (P::kStridedB ? piece_of_depth<kTile>(c / 16, c % 16) : piece_of_row<D>(c / (D / 8), c % (D / 8))), P::kPlane, b[i]);
+                store_piece<DTYPE, P::kTermsB>(second + (P::kStridedB ? piece_of_depth<P::kSide>(c / kAcross, c % kAcross) : piece_of_row<D>(c / (D / 8), c % (D / 8))), P::kPlane, from.b[i]);
             }
         } else {
 #pragma unroll
             for (int i = 0; i < N / 2; ++i) {
                 const int c = i * kThreads + tid;
-                const float unit = block_unit(codes[i].exponent);
-                *reinterpret_cast<u32x4 *>(second + piece_of_depth<kTile>(c / 8, c % 8 * 2)) = code_values(codes[i].codes[0], codes[i].codes[1], unit);
-                *reinterpret_cast<u32x4 *>(second + piece_of_depth<kTile>(c / 8, c % 8 * 2 + 1)) = code_values(codes[i].codes[2], codes[i].codes[3], unit);
+                const float unit = block_unit(from.codes[i].exponent);
+                *reinterpret_cast<u32x4 *>(second + piece_of_depth<P::kSide>(c / (kAcross / 2), c % (kAcross / 2) * 2)) = code_values(from.codes[i].codes[0], from.codes[i].codes[1], unit);
+                *reinterpret_cast<u32x4 *>(second + piece_of_depth<P::kSide>(c / (kAcross / 2), c % (kAcross / 2) * 2 + 1)) = code_values(from.codes[i].codes[2], from.codes[i].codes[3], unit);
             }
         }
     };
 
-    f32x16 acc[2][2] = {};
-    f32x16 sums = {};                                              // row sums: the product with ones, 32 rows per wave
-    const bool with_sums = OP == kWeightGrad && p.row_sums && col_tile == 0;
+    f32x16 acc[W][W] = {};
+    f32x16 sums = {};                                              // row sums: the product with ones, 32 rows per wave (W = 1: of the first wave of a row)
+    const bool with_sums = OP == kWeightGrad && p.row_sums && col_tile == 0 && wave_col < W;
     const u32x4 ones = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
 
     auto compute = [&](const char *stage) {
         const char *second = stage + P::kTermsA * P::kPlane;
 #pragma unroll
         for (int d = 0; d < D; d += 16) {
-            u32x4 fa[P::kTermsA][2], fb[P::kTermsB][2];
+            u32x4 fa[P::kTermsA][W], fb[P::kTermsB][W];
 #pragma unroll
             for (int t = 0; t < P::kTermsA; ++t)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) fa[t][i] = fragment<P::kStridedA, D, kTile>(stage + t * P::kPlane, wave_row * 64 + i * 32, d, lane);
+                for (int i = 0; i < W; ++i) fa[t][i] = fragment<P::kStridedA, D, P::kSide>(stage + t * P::kPlane, wave_row * (32 * W) + i * 32, d, lane);
 #pragma unroll
             for (int t = 0; t < P::kTermsB; ++t)
 #pragma unroll
-                for (int j = 0; j < 2; ++j) fb[t][j] = fragment<P::kStridedB, D, kTile>(second + t * P::kPlane, wave_col * 64 + j * 32, d, lane);
+                for (int j = 0; j < W; ++j) fb[t][j] = fragment<P::kStridedB, D, P::kSide>(second + t * P::kPlane, wave_col * (32 * W) + j * 32, d, lane);
 #pragma unroll
             for (int ta = P::kTermsA - 1; ta >= 0; --ta)           // small products first
 #pragma unroll
                 for (int tb = P::kTermsB - 1; tb >= 0; --tb) {
                     if (P::kTermsB > 1 && ta + tb > 2) continue;
 #pragma unroll
-                    for (int i = 0; i < 2; ++i)
+                    for (int i = 0; i < W; ++i)
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) acc[i][j] = multiply<P::kHalf>(fb[tb][j], fa[ta][i], acc[i][j]);
+                        for (int j = 0; j < W; ++j) acc[i][j] = multiply<P::kHalf>(fb[tb][j], fa[ta][i], acc[i][j]);
                 }
             if constexpr (OP == kWeightGrad)
                 if (with_sums) {
 #pragma unroll
-                    for (int ta = P::kTermsA - 1; ta >= 0; --ta) sums = multiply<false>(ones, wave_col ? fa[ta][1] : fa[ta][0], sums);
+                    for (int ta = P::kTermsA - 1; ta >= 0; --ta) sums = multiply<false>(ones, wave_col ? fa[ta][W - 1] : fa[ta][0], sums);
                 }
         }
     };
 
+    Set next;
     if (begin < end) {
-        load(begin);
-        store(lds);
+        load(next, begin);
+        store(lds, next);
         __syncthreads();
         int stage = 0;
         for (uint32_t k = begin; k < end; k += D) {
             const bool more = k + D < end;
-            if (more) load(k + D);
+            if (more) load(next, k + D);
             compute(lds + stage * P::kStageBytes);
             if constexpr (P::kStages == 1) __syncthreads();
             else stage ^= 1;
-            if (more) store(lds + stage * P::kStageBytes);
+            if (more) store(lds + stage * P::kStageBytes, next);
             __syncthreads();
         }
     }
 
     if constexpr (OP == kWeightGrad)
-        if (with_sums && lane < 32) finish_row_sum(p, sums[0], row0 + wave_row * 64 + wave_col * 32 + lane, split);
+        if (with_sums && lane < 32) finish_row_sum(p, sums[0], row0 + wave_row * (32 * W) + wave_col * 32 + lane, split);
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < W; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-            finish_tile<OP, DTYPE>(p, acc[i][j], row0 + wave_row * 64 + i * 32 + (lane & 31), col0 + wave_col * 64 + j * 32, lane, split);
+        for (int j = 0; j < W; ++j)
+            finish_tile<OP, DTYPE>(p, acc[i][j], row0 + wave_row * (32 * W) + i * 32 + (lane & 31), col0 + wave_col * (32 * W) + j * 32, lane, split);
 }
 
 // Sums of the splits, in their order, and the end of the product.  A thread has four columns, eight threads a block of a checkpoint.
@@ -244,9 +268,12 @@ template <class F> hipError_t for_type(Op op, uint32_t dtype, F f) {
 
 }  // namespace
 
-hipError_t launch_tiles(Op op, uint32_t dtype, const Product &p, hipStream_t st) {
-    const uint32_t grid = (uint32_t)((uint64_t)tiles_of(p.rows) * tiles_of(p.cols) * p.splits);
-    return for_type(op, dtype, [&](auto o, auto t) { k_tiles<decltype(o)::value, decltype(t)::value><<<grid, kThreads, 0, st>>>(p); });
+hipError_t launch_tiles(Op op, uint32_t dtype, const Product &p, uint32_t side, hipStream_t st) {
+    const uint32_t grid = tiles_of(p.rows, side) * tiles_of(p.cols, side) * p.splits;
+    return for_type(op, dtype, [&](auto o, auto t) {
+        if (side == 64) k_tiles<decltype(o)::value, decltype(t)::value, 1><<<grid, kThreads, 0, st>>>(p);
+        else k_tiles<decltype(o)::value, decltype(t)::value, 2><<<grid, kThreads, 0, st>>>(p);
+    });
 }
 
 hipError_t launch_join(Op op, uint32_t dtype, const Product &p, hipStream_t st) {
