@@ -267,16 +267,18 @@ template <int OP, uint32_t DTYPE, int T> __global__ __launch_bounds__(kThreads) 
                         codes.load(piece);
                     }
                 }
-                // row sums: two additions an instruction, cheaper for all than a branch
-                constexpr int pairs = T / 2 * 4, q = j * pairs / N;
-                if constexpr (j == 0 || (j - 1) * pairs / N != q) {
-                    const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
-                    const uint32_t pair = fa[set][q / 4][q % 4];                        // (a cast of the vector's element itself would take its first)
-                    sums[q / 4] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), ones, sums[q / 4], false);
-                }
             }
             __builtin_amdgcn_sched_barrier(0);
         });
+        if constexpr (kCodes)
+            if (with_sums) {                                       // row sums: two additions an instruction
+                const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+#pragma unroll
+                for (int q = 0; q < T / 2 * 4; ++q) {
+                    const uint32_t pair = fa[set][q / 4][q % 4];   // (a cast of the vector's element itself would take its first)
+                    sums[q / 4] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), ones, sums[q / 4], false);
+                }
+            }
     };
     // Tile number c (first operand of step s: 2 s, second: 2 s + 1) goes to slot c mod 5.
     auto on = [](uint32_t slot, uint32_t tiles) {

@@ -46,8 +46,7 @@ __global__ __launch_bounds__(kThreads) void k_save(const typename Elem<DTYPE>::t
         hi[i] = (float)v.v[4 + i];
         largest = max(largest, max(magnitude_bits(lo[i]), magnitude_bits(hi[i])));
     }
-    largest = max(largest, (uint32_t)__shfl_xor((int)largest, 1));
-    largest = max(largest, (uint32_t)__shfl_xor((int)largest, 2));
+    largest = largest_of_quad(largest);
     const uint32_t t = block_exponent(largest);
     const size_t block = (size_t)at.row * blocks + at.col / kBlock;
     *reinterpret_cast<u32x2 *>(codes + block * kBlock + at.col % kBlock) = u32x2{codes4(lo, t), codes4(hi, t)};

@@ -142,8 +142,7 @@ __device__ inline void finish8(const Product &p, uint32_t row, uint32_t col, int
                 z[1][e] = e + 4 < valid ? hi[e] : 0.0f;
                 largest = max(largest, max(magnitude_bits(z[0][e]), magnitude_bits(z[1][e])));
             }
-            largest = max(largest, (uint32_t)__shfl_xor((int)largest, 1));
-            largest = max(largest, (uint32_t)__shfl_xor((int)largest, 2));
+            largest = largest_of_quad(largest);
             const uint32_t t = block_exponent(largest);
             if (col < p.finish.blocks * kBlock) {
                 const size_t block = (size_t)row * p.finish.blocks + col / kBlock;

@@ -40,8 +40,8 @@ template <bool BLOCK, uint32_t DTYPE> __device__ inline void finish_quad(const P
                 z[e] = e < valid ? v[e] : 0.0f;
                 largest = max(largest, magnitude_bits(z[e]));
             }
-#pragma unroll
-            for (int step = 1; step < 8; step *= 2) largest = max(largest, (uint32_t)__shfl_xor((int)largest, step));
+            largest = largest_of_quad(largest);
+            largest = max(largest, (uint32_t)__shfl_xor((int)largest, 4));
             const uint32_t t = block_exponent(largest);
             if (row < p.rows) {                                    // (the workgroup has a column: its block exists)
                 const size_t block = (size_t)row * p.finish.blocks + col0 / kBlock;

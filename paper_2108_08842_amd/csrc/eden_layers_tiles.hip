@@ -237,8 +237,8 @@ template <int OP, uint32_t DTYPE> __global__ __launch_bounds__(256) void k_join(
                     z[e] = e < valid ? v[e] : 0.0f;
                     largest = max(largest, magnitude_bits(z[e]));
                 }
-#pragma unroll
-                for (int step = 1; step < 8; step *= 2) largest = max(largest, (uint32_t)__shfl_xor((int)largest, step));
+                largest = largest_of_quad(largest);
+                largest = max(largest, (uint32_t)__shfl_xor((int)largest, 4));
                 const uint32_t t = block_exponent(largest);
                 const size_t block = (size_t)row * p.finish.blocks + col / kBlock;
                 if (col % kBlock == 0) p.finish.exps_out[block] = (uint8_t)t;
