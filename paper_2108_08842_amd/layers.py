@@ -97,11 +97,13 @@ def _same(t, like, what):
         _refuse(f"{what}: {t.dtype} on {t.device}, expected {like.dtype} on {like.device}")
 
 
-def _output(out, shape, dtype, device, what):
+def _output(out, shape, like, what, dtype=None):
+    """`out`, or a new tensor of that shape of like's type (or `dtype`) on its device."""
     if out is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    if tuple(out.shape) != tuple(shape) or out.dtype is not dtype or out.device != device:
-        _refuse(f"{what}: {tuple(out.shape)} of {out.dtype} on {out.device}, expected {tuple(shape)} of {dtype} on {device}")
+        return like.new_empty(shape) if dtype is None else torch.empty(shape, dtype=dtype, device=like.device)
+    dtype = dtype or like.dtype
+    if tuple(out.shape) != tuple(shape) or out.dtype is not dtype or out.device != like.device:
+        _refuse(f"{what}: {tuple(out.shape)} of {out.dtype} on {out.device}, expected {tuple(shape)} of {dtype} on {like.device}")
     return out
 
 
@@ -119,21 +121,28 @@ class _On:
     __slots__ = ("stacked",)
 
     def __init__(self, device, stream):
-        self.stacked = []
-        if stream is not None:
-            if stream.device != device:
-                _refuse(f"stream on {stream.device}, tensors on {device}")
-            self.stacked.append(torch.cuda.stream(stream))
-        elif torch.cuda.current_device() != device.index:
-            self.stacked.append(torch.cuda.device(device))
+        if stream is not None and stream.device != device:
+            _refuse(f"stream on {stream.device}, tensors on {device}")
+        self.stacked = torch.cuda.device(device) if stream is None else torch.cuda.stream(stream)
 
     def __enter__(self):
-        for c in self.stacked:
-            c.__enter__()
+        return self.stacked.__enter__()
 
     def __exit__(self, *e):
-        for c in reversed(self.stacked):
-            c.__exit__(*e)
+        return self.stacked.__exit__(*e)
+
+
+def _elsewhere(device, stream):
+    """Whether a call has to change the current device or stream first."""
+    return stream is not None or torch.cuda.current_device() != device.index
+
+
+def _stream(device):
+    """Address of the device's current stream (the device is the current one)."""
+    try:
+        return torch._C._cuda_getCurrentRawStream(device.index)
+    except AttributeError:
+        return torch.cuda.current_stream(device).cuda_stream
 
 
 def _workspace(L, rows, cols, depth, dtype, device):
@@ -161,30 +170,38 @@ class Checkpoint:
 
     def restore(self, dtype=torch.bfloat16, out=None, stream=None):
         """The values it stands for (exact in bfloat16 and float32)."""
-        if out is not None:
-            dtype = out.dtype
-        if dtype not in _DTYPES:
-            _refuse(f"restore: {dtype}")
-        with _On(self.buffer.device, stream):
-            out = _output(out, (self.rows, self.cols) if out is None else out.shape, dtype, self.buffer.device, "restore: out")
-            p, ld, rows, cols = _rows(out, "restore: out")
-            if (rows, cols) != (self.rows, self.cols):
-                _refuse(f"restore: out is {rows} x {cols}, the checkpoint {self.rows} x {self.cols}")
-            _check(lib().eden_checkpoint_restore(self.buffer.data_ptr(), rows, cols, _DTYPES[dtype], p, ld, eden._stream_ptr(stream)),
-                   "eden_checkpoint_restore")
+        device = self.buffer.device
+        if _elsewhere(device, stream):
+            with _On(device, stream):
+                return self.restore(dtype, out)
+        if out is None:
+            code = _DTYPES.get(dtype)
+            if code is None:
+                _refuse(f"restore: {dtype}")
+            out = torch.empty((self.rows, self.cols), dtype=dtype, device=device)
+        else:
+            code = _dtype(out, "restore: out")
+            if out.device != device:
+                _refuse(f"restore: out on {out.device}, the checkpoint on {device}")
+        p, ld, rows, cols = _rows(out, "restore: out")
+        if rows != self.rows or cols != self.cols:
+            _refuse(f"restore: out is {rows} x {cols}, the checkpoint {self.rows} x {self.cols}")
+        _check((_lib or lib()).eden_checkpoint_restore(self.buffer.data_ptr(), rows, cols, code, p, ld, _stream(device)), "eden_checkpoint_restore")
         return out
 
 
 def _new_checkpoint(into, rows, cols, device):
     if into is None:
-        return Checkpoint(torch.empty(rows * -(-cols // BLOCK) * (BLOCK + 1), dtype=torch.uint8, device=device), rows, cols)
+        c = Checkpoint.__new__(Checkpoint)
+        c.buffer, c.rows, c.cols = torch.empty(rows * -(-cols // BLOCK) * (BLOCK + 1), dtype=torch.uint8, device=device), rows, cols
+        return c
     if (into.rows, into.cols) != (rows, cols) or into.buffer.device != device:
         _refuse(f"checkpoint of {into.rows} x {into.cols} on {into.buffer.device}, expected {rows} x {cols} on {device}")
     return into
 
 
 def _saved(c, rows, cols, device, what):
-    if (c.rows, c.cols) != (rows, cols) or c.buffer.device != device:
+    if c.rows != rows or c.cols != cols or c.buffer.device != device:
         _refuse(f"{what}: checkpoint of {c.rows} x {c.cols} on {c.buffer.device}, expected {rows} x {cols} on {device}")
     return c.buffer.data_ptr()
 
@@ -192,18 +209,25 @@ def _saved(c, rows, cols, device, what):
 def save_checkpoint(x, into=None, stream=None) -> Checkpoint:
     """The 8-bit checkpoint of x; `into`: a Checkpoint of the same size that is overwritten."""
     dtype = _dtype(x, "save_checkpoint: x")
+    device = x.device
+    if _elsewhere(device, stream):
+        with _On(device, stream):
+            return save_checkpoint(x, into)
     p, ld, rows, cols = _rows(x, "save_checkpoint: x")
-    with _On(x.device, stream):
-        c = _new_checkpoint(into, rows, cols, x.device)
-        _check(lib().eden_checkpoint_save(p, ld, rows, cols, dtype, c.buffer.data_ptr(), c.buffer.numel(), eden._stream_ptr(stream)),
-               "eden_checkpoint_save")
+    c = _new_checkpoint(into, rows, cols, device)
+    buffer = c.buffer
+    _check((_lib or lib()).eden_checkpoint_save(p, ld, rows, cols, dtype, buffer.data_ptr(), buffer.numel(), _stream(device)), "eden_checkpoint_save")
     return c
 
 
 def linear(x, w, bias=None, activation: str = "none", residual=None, checkpoint=False, out=None, stream=None):
     """act(x w^T + bias) + residual.  `checkpoint`: True or a Checkpoint to be overwritten: returns (y, checkpoint of x w^T + bias)."""
-    L = lib()
     dtype = _dtype(x, "linear: x")
+    device = x.device
+    if _elsewhere(device, stream):
+        with _On(device, stream):
+            return linear(x, w, bias, activation, residual, checkpoint, out)
+    L = _lib or lib()
     act = _act(activation, "linear")
     xp, ldx, m, k = _rows(x, "linear: x")
     _same(w, x, "linear: w")
@@ -214,53 +238,61 @@ def linear(x, w, bias=None, activation: str = "none", residual=None, checkpoint=
     ldr = n
     if bias is not None:
         _same(bias, x, "linear: bias")
-        if tuple(bias.shape) != (n,) or (n > 1 and bias.stride(0) != 1):
+        if bias.dim() != 1 or bias.shape[0] != n or (n > 1 and bias.stride(0) != 1):
             _refuse(f"linear: bias is {tuple(bias.shape)} with stride {bias.stride()}, expected {n} neighbours")
         bp = bias.data_ptr()
-    shape = x.shape[:-1] + (n,)
+    shape = (m, n) if x.dim() == 2 else x.shape[:-1] + (n,)
     if residual is not None:
         _same(residual, x, "linear: residual")
         if residual.shape != shape:
             _refuse(f"linear: residual is {tuple(residual.shape)}, expected {tuple(shape)}")
         rp, ldr, _, _ = _rows(residual, "linear: residual")
-    with _On(x.device, stream):
-        y = _output(out, shape, x.dtype, x.device, "linear: out")
-        yp, ldy, _, _ = _rows(y, "linear: out")
-        c = None if checkpoint is False or checkpoint is None else _new_checkpoint(None if checkpoint is True else checkpoint, m, n, x.device)
-        ws, wsp, size = _workspace(L, m, n, k, dtype, x.device)
-        _check(L.eden_linear(xp, ldx, wp, ldw, bp, rp, ldr, yp, ldy, c.buffer.data_ptr() if c else None, c.buffer.numel() if c else 0, m, n, k,
-                             dtype, act, wsp, size, eden._stream_ptr(stream)), "eden_linear")
-    return (y, c) if c is not None else y
+    y = _output(out, shape, x, "linear: out")
+    yp, ldy, _, _ = _rows(y, "linear: out")
+    c, cp, capacity = None, None, 0
+    if checkpoint is not False and checkpoint is not None:
+        c = _new_checkpoint(None if checkpoint is True else checkpoint, m, n, device)
+        cp, capacity = c.buffer.data_ptr(), c.buffer.numel()
+    ws, wsp, size = _workspace(L, m, n, k, dtype, device)
+    _check(L.eden_linear(xp, ldx, wp, ldw, bp, rp, ldr, yp, ldy, cp, capacity, m, n, k, dtype, act, wsp, size, _stream(device)), "eden_linear")
+    return y if c is None else (y, c)
 
 
 def linear_weight_grad(dy, saved: Checkpoint, bias: bool = False, out=None, bias_out=None, accumulate: bool = False, stream=None):
     """dy^T x (fp32) from the checkpoint of x; with `bias` (dw, sum of dy's rows).  `out`, `bias_out`: where to write them, for instance
     parts of the vector that Context.encode takes; `accumulate`: add to what they hold."""
-    L = lib()
     dtype = _dtype(dy, "linear_weight_grad: dy")
+    device = dy.device
+    if _elsewhere(device, stream):
+        with _On(device, stream):
+            return linear_weight_grad(dy, saved, bias, out, bias_out, accumulate)
+    L = _lib or lib()
     dp, ldy, m, n = _rows(dy, "linear_weight_grad: dy")
     k = saved.cols
-    sp = _saved(saved, m, k, dy.device, "linear_weight_grad")
+    sp = _saved(saved, m, k, device, "linear_weight_grad")
     if accumulate and (out is None or (bias and bias_out is None)):
         _refuse("linear_weight_grad: nothing to accumulate in")
-    with _On(dy.device, stream):
-        dw = _output(out, (n, k), torch.float32, dy.device, "linear_weight_grad: out")
-        wp, ldw, _, _ = _rows(dw, "linear_weight_grad: out")
-        db = None
-        if bias or bias_out is not None:
-            db = _output(bias_out, (n,), torch.float32, dy.device, "linear_weight_grad: bias_out")
-            if n > 1 and db.stride(0) != 1:
-                _refuse("linear_weight_grad: bias_out's elements must be neighbours")
-        ws, wsp, size = _workspace(L, n, k, m, dtype, dy.device)
-        _check(L.eden_linear_weight_grad(dp, ldy, sp, wp, ldw, db.data_ptr() if db is not None else None, m, n, k, dtype, 1 if accumulate else 0, wsp, size,
-                                         eden._stream_ptr(stream)), "eden_linear_weight_grad")
-    return (dw, db) if db is not None else dw
+    dw = _output(out, (n, k), dy, "linear_weight_grad: out", torch.float32)
+    wp, ldw, _, _ = _rows(dw, "linear_weight_grad: out")
+    db, bp = None, None
+    if bias or bias_out is not None:
+        db = _output(bias_out, (n,), dy, "linear_weight_grad: bias_out", torch.float32)
+        if n > 1 and db.stride(0) != 1:
+            _refuse("linear_weight_grad: bias_out's elements must be neighbours")
+        bp = db.data_ptr()
+    ws, wsp, size = _workspace(L, n, k, m, dtype, device)
+    _check(L.eden_linear_weight_grad(dp, ldy, sp, wp, ldw, bp, m, n, k, dtype, 1 if accumulate else 0, wsp, size, _stream(device)), "eden_linear_weight_grad")
+    return dw if db is None else (dw, db)
 
 
 def linear_input_grad(dz, w, activation: str = "none", checkpoint: Checkpoint = None, residual=None, out=None, stream=None):
     """(dz w) * act'(z) + residual; z: the checkpoint of the input of the activation in front of the layer (none without one)."""
-    L = lib()
     dtype = _dtype(dz, "linear_input_grad: dz")
+    device = dz.device
+    if _elsewhere(device, stream):
+        with _On(device, stream):
+            return linear_input_grad(dz, w, activation, checkpoint, residual, out)
+    L = _lib or lib()
     act = _act(activation, "linear_input_grad")
     dp, ldz, m, n = _rows(dz, "linear_input_grad: dz")
     _same(w, dz, "linear_input_grad: w")
@@ -269,31 +301,32 @@ def linear_input_grad(dz, w, activation: str = "none", checkpoint: Checkpoint = 
     wp, ldw, _, k = _rows(w, "linear_input_grad: w")
     if (checkpoint is None) != (act == 0):
         _refuse("linear_input_grad: an activation and the checkpoint of its input go together")
-    sp = None if checkpoint is None else _saved(checkpoint, m, k, dz.device, "linear_input_grad")
+    sp = None if checkpoint is None else _saved(checkpoint, m, k, device, "linear_input_grad")
     rp, ldr = None, k
-    shape = dz.shape[:-1] + (k,)
+    shape = (m, k) if dz.dim() == 2 else dz.shape[:-1] + (k,)
     if residual is not None:
         _same(residual, dz, "linear_input_grad: residual")
         if residual.shape != shape:
             _refuse(f"linear_input_grad: residual is {tuple(residual.shape)}, expected {tuple(shape)}")
         rp, ldr, _, _ = _rows(residual, "linear_input_grad: residual")
-    with _On(dz.device, stream):
-        dx = _output(out, shape, dz.dtype, dz.device, "linear_input_grad: out")
-        xp, ldx, _, _ = _rows(dx, "linear_input_grad: out")
-        ws, wsp, size = _workspace(L, m, k, n, dtype, dz.device)
-        _check(L.eden_linear_input_grad(dp, ldz, wp, ldw, sp, act, rp, ldr, xp, ldx, m, n, k, dtype, wsp, size, eden._stream_ptr(stream)),
-               "eden_linear_input_grad")
+    dx = _output(out, shape, dz, "linear_input_grad: out")
+    xp, ldx, _, _ = _rows(dx, "linear_input_grad: out")
+    ws, wsp, size = _workspace(L, m, k, n, dtype, device)
+    _check(L.eden_linear_input_grad(dp, ldz, wp, ldw, sp, act, rp, ldr, xp, ldx, m, n, k, dtype, wsp, size, _stream(device)), "eden_linear_input_grad")
     return dx
 
 
 def activation_grad(dy, saved: Checkpoint, activation: str, out=None, stream=None):
     """dy * act'(z), z from its checkpoint."""
     dtype = _dtype(dy, "activation_grad: dy")
+    device = dy.device
+    if _elsewhere(device, stream):
+        with _On(device, stream):
+            return activation_grad(dy, saved, activation, out)
     act = _act(activation, "activation_grad")
     dp, ldy, rows, cols = _rows(dy, "activation_grad: dy")
-    sp = _saved(saved, rows, cols, dy.device, "activation_grad")
-    with _On(dy.device, stream):
-        dz = _output(out, dy.shape, dy.dtype, dy.device, "activation_grad: out")
-        zp, ldz, _, _ = _rows(dz, "activation_grad: out")
-        _check(lib().eden_activation_grad(dp, ldy, sp, act, zp, ldz, rows, cols, dtype, eden._stream_ptr(stream)), "eden_activation_grad")
+    sp = _saved(saved, rows, cols, device, "activation_grad")
+    dz = _output(out, dy.shape, dy, "activation_grad: out")
+    zp, ldz, _, _ = _rows(dz, "activation_grad: out")
+    _check((_lib or lib()).eden_activation_grad(dp, ldy, sp, act, zp, ldz, rows, cols, dtype, _stream(device)), "eden_activation_grad")
     return dz
