@@ -40,15 +40,22 @@ struct Shape {
     uint32_t side;
     uint64_t splits;
 };
-// Loads straight into the LDS: 256 x 256 tiles where those give every CU work, else 128 x 128, two to a CU.
+// Loads straight into the LDS: tiles of 256 x 256, one to a CU, or of 128 x 128, two to a CU.  Measured (bf16, depth 4096): 64 deep take 1.6 us in a
+// full round of the former, 1.2 us where most of the CUs are idle (the clock is higher then), 1.05 us in a full round of the latter and 0.6 us with
+// one to a CU; a round's ends 10 and 5 us.  That puts 2048 x 8192 at the former (111 us against 131), 2048 x 4096 at the latter (67 against 87), 4096 x 5120 too
+// (a second round of 64 tiles; 92 against 103 at depth 2048).
 Shape direct_shape(uint64_t rows, uint64_t cols, uint64_t depth) {
-    if (tile_count(rows, cols, 256) >= 192) return {256, 1};
-    return {128, splits_of(tile_count(rows, cols, 128), depth, 512, 256)};
+    const uint64_t large = tile_count(rows, cols, 256), small = tile_count(rows, cols, 128), left_large = large % 256, left_small = small % 512;
+    const double deep = (double)((depth + 63) / 64);
+    const double cost_large = (1.6 * (double)(large / 256) + (left_large > 160 ? 1.6 : left_large ? 1.2 : 0.0)) * deep + 10.0 * (double)((large + 255) / 256);
+    const double cost_small = (1.05 * (double)(small / 512) + (left_small > 256 ? 1.05 : left_small ? 0.6 : 0.0)) * deep + 5.0 * (double)((small + 511) / 512);
+    if (cost_large < cost_small) return {256, 1};
+    return {128, splits_of(small, depth, 256, 512)};
 }
 // Through registers: 128 x 128 where those fill the device, else 64 x 64, three or more to a CU.
 Shape tiles_shape(uint64_t rows, uint64_t cols, uint64_t depth) {
     if (tile_count(rows, cols, 128) >= 256) return {128, 1};
-    return {64, splits_of(tile_count(rows, cols, 64), depth, 768, 128)};
+    return {64, splits_of(tile_count(rows, cols, 64), depth, 1024, 96)};
 }
 
 // Rows that start at, and hold, whole 16-byte pieces, and offsets inside a tile that 31 bits hold
