@@ -62,28 +62,62 @@ Shape tiles_shape(uint64_t rows, uint64_t cols, uint64_t depth) {
 bool whole_pieces(const void *p, uint64_t ld, uint64_t inner) {
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0 && inner % 8 == 0 && ld < (1u << 21);
 }
-// Whether the kernel whose loads go straight into the LDS takes a product.
-bool is_direct(Op op, uint32_t dtype, const Product &p) {
-    if (dtype == EDEN_F32 || (op == kWeightGrad && dtype == EDEN_F16) || p.depth == 0 || p.cols == 0) return false;
-    if (!whole_pieces(p.a, p.lda, op == kWeightGrad ? p.rows : p.depth)) return false;
-    return op == kWeightGrad ? p.ldb < (1u << 24) : whole_pieces(p.b, p.ldb, op == kForward ? p.depth : p.cols);
+// Whether the kernel whose loads go straight into the LDS takes a product: as it is, or with copies of the operands whose rows do not fit.
+bool direct_type(Op op, uint32_t dtype, const Product &p) {
+    return dtype != EDEN_F32 && !(op == kWeightGrad && dtype == EDEN_F16) && p.depth != 0 && p.cols != 0 && (op != kWeightGrad || p.ldb < (1u << 24));
 }
+bool whole_a(Op op, const Product &p) { return whole_pieces(p.a, p.lda, op == kWeightGrad ? p.rows : p.depth); }
+bool whole_b(Op op, const Product &p) { return op == kWeightGrad || whole_pieces(p.b, p.ldb, op == kForward ? p.depth : p.cols); }
+
+// Copies cost two passes over an operand; from 2^31 products on they are less than what they save (bf16, 1021 x 1001 x 2047: 34 us either way).
+uint64_t copy_bytes(uint64_t a, uint64_t b) { return (a + 63) / 64 * 64 * ((b + 63) / 64 * 64) * 2; }
+bool worth_copies(uint64_t rows, uint64_t cols, uint64_t depth) {
+    return rows > kFewRows && rows < (1u << 21) && cols < (1u << 21) && depth < (1u << 21) && rows * cols >= (1u << 31) / std::max<uint64_t>(depth, 1);
+}
+// Replaces a 2-byte operand by a copy in the workspace.
+hipError_t copy_operand(const void *&operand, size_t &ld, uint32_t rows, uint32_t cols, uint8_t *&workspace, size_t &room, hipStream_t st) {
+    const uint32_t to_ld = (cols + 63) / 64 * 64;
+    const hipError_t e = launch_copy_rows(operand, ld, rows, cols, workspace, to_ld, st);
+    const size_t used = copy_bytes(rows, cols);
+    operand = workspace, ld = to_ld, workspace += used, room -= used;
+    return e;
+}
+
 // Launches a product whose operands and end are set.
 int run(Op op, uint32_t dtype, Product &p, void *workspace, size_t workspace_bytes, void *stream) {
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return EDEN_ERR_INVALID_ARG;
     if (op == kForward && p.rows <= kFewRows) return status(launch_rows(dtype, p, st));
-    const bool direct = is_direct(op, dtype, p);
+    uint8_t *space = static_cast<uint8_t *>(workspace);
+    if (workspace == nullptr) workspace_bytes = 0;
+    p.a_width = op == kWeightGrad ? p.rows : p.depth;
+    p.b_width = op == kForward ? p.depth : p.cols;
+    bool direct = direct_type(op, dtype, p);
+    if (direct && !(whole_a(op, p) && whole_b(op, p))) {
+        // rows along the depth that do not end with a piece need zeros behind it in both operands
+        const bool a = !whole_a(op, p), b = !whole_b(op, p);
+        const uint64_t need = (a ? copy_bytes(p.rows, p.depth) : 0) + (b ? copy_bytes(p.cols, p.depth) : 0);
+        direct = worth_copies(p.rows, p.cols, p.depth) && need <= workspace_bytes;
+        hipError_t e = hipSuccess;
+        if (direct && a) {
+            e = op == kWeightGrad ? copy_operand(p.a, p.lda, p.depth, p.rows, space, workspace_bytes, st) : copy_operand(p.a, p.lda, p.rows, p.depth, space, workspace_bytes, st);
+            p.a_width = (uint32_t)p.lda;
+        }
+        if (direct && b && e == hipSuccess) {
+            e = op == kForward ? copy_operand(p.b, p.ldb, p.cols, p.depth, space, workspace_bytes, st) : copy_operand(p.b, p.ldb, p.depth, p.cols, space, workspace_bytes, st);
+            p.b_width = (uint32_t)p.ldb;
+        }
+        if (e != hipSuccess) return EDEN_ERR_HIP;
+    }
     const Shape shape = direct ? direct_shape(p.rows, p.cols, p.depth) : tiles_shape(p.rows, p.cols, p.depth);
     if (tile_count(p.rows, p.cols, shape.side) > kMostGroups / 64) return EDEN_ERR_INVALID_ARG;
     uint64_t splits = shape.splits;
-    if (workspace == nullptr) workspace_bytes = 0;
     while (splits > 1 && partial_bytes(p.rows, p.cols, splits) > workspace_bytes) --splits;
     const uint64_t each = ((p.depth + splits - 1) / splits + kSplitUnit - 1) / kSplitUnit * kSplitUnit;
     splits = each ? (p.depth + each - 1) / each : 1;
     p.splits = splits < 1 ? 1 : (uint32_t)splits;
     p.split_depth = (uint32_t)each;
-    p.partial = static_cast<float *>(workspace);
+    p.partial = reinterpret_cast<float *>(space);
     p.partial_ld = (p.cols + 3) / 4 * 4;
     hipError_t e = direct ? launch_direct(op, dtype, p, shape.side, st) : launch_tiles(op, dtype, p, shape.side, st);
     if (e == hipSuccess && p.splits > 1) e = launch_join(op, dtype, p, st);
@@ -121,6 +155,13 @@ size_t eden_layers_workspace_bytes(uint64_t rows, uint64_t cols, uint64_t depth,
     if (rows == 0 || cols == 0) return 0;
     const uint64_t splits = std::max(direct_shape(rows, cols, depth).splits, tiles_shape(rows, cols, depth).splits);
     return splits > 1 ? partial_bytes(rows, cols, splits) : 0;
+}
+
+size_t eden_layers_copying_bytes(uint64_t rows, uint64_t cols, uint64_t depth, uint32_t dtype) {
+    if (!known_type(dtype) || rows > kMostSize || cols > kMostSize || depth > kMostSize) return 0;
+    const size_t plain = eden_layers_workspace_bytes(rows, cols, depth, dtype);
+    if (dtype == EDEN_F32 || !worth_copies(rows, cols, depth)) return plain;
+    return plain + copy_bytes(rows, depth) + copy_bytes(cols, depth);
 }
 
 int eden_linear(const void *x, uint64_t ldx, const void *w, uint64_t ldw, const void *bias, const void *residual, uint64_t ldr, void *y, uint64_t ldy,

@@ -59,11 +59,12 @@ template <int T, bool STRIDED> struct Source {
     u32x4 now;                 // of the tile that is being fetched: descriptor, this lane's first offset
     uint32_t at;
 
+    // rows or columns first .. count - 1 of the operand, depths begin .. end - 1; `whole`: elements of a row of memory that may be read
     __device__ Source(const void *p, size_t ld, uint32_t first, uint32_t count, uint32_t begin, uint32_t end, uint32_t whole, int wave, int lane) {
         if constexpr (STRIDED) {
             base = static_cast<const char *>(p) + ((size_t)begin * ld + first) * 2;
             step = (size_t)kDeep * ld * 2;
-            reach = ((uint64_t)(end - begin - 1) * ld + (count - first)) * 2;
+            reach = ((uint64_t)(end - begin - 1) * ld + (whole - first)) * 2;
             const uint32_t d = (wave * 64 + lane) / kPieces, piece = (lane % kPieces) ^ (4 * (d & 3));
             offset = (uint32_t)(d * ld * 2) + piece * 16;
             stride = (uint32_t)(kThreads / kPieces * ld * 2);
@@ -222,8 +223,8 @@ template <int OP, uint32_t DTYPE, int T> __global__ __launch_bounds__(kThreads) 
     const uint32_t begin = split * p.split_depth, end = min(p.depth, begin + p.split_depth);
     const uint32_t steps = (end - begin + kDeep - 1) / kDeep;      // begin < end: launched for depths above 0 only
 
-    Source<T, kStridedA> a(p.a, p.lda, row0, p.rows, begin, end, p.depth, wave, lane);
-    Source<T, kStridedB> b(p.b, kCodes ? 0 : p.ldb, col0, kCodes ? col0 + 1 : p.cols, begin, end, p.depth, wave, lane);
+    Source<T, kStridedA> a(p.a, p.lda, row0, p.rows, begin, end, p.a_width, wave, lane);
+    Source<T, kStridedB> b(p.b, kCodes ? 0 : p.ldb, col0, kCodes ? col0 + 1 : p.cols, begin, end, kCodes ? col0 + 1 : p.b_width, wave, lane);
     const int swap = kCodes ? wave_col * (T / 2) : 0;
     const Reader<T, kStridedA> reader_a(wave_row * (kSide / 2), lane, swap);
     const Reader<T, kStridedB> reader_b(wave_col * (kSide / 2), lane);

@@ -22,7 +22,7 @@ from .eden import EdenError
 F32, F16, BF16 = 0, 1, 2
 BLOCK = 32                                                        # columns of a checkpoint block
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
-EXPORTS = ["eden_checkpoint_bytes", "eden_checkpoint_save", "eden_checkpoint_restore", "eden_layers_workspace_bytes", "eden_linear",
+EXPORTS = ["eden_checkpoint_bytes", "eden_checkpoint_save", "eden_checkpoint_restore", "eden_layers_workspace_bytes", "eden_layers_copying_bytes", "eden_linear",
            "eden_linear_weight_grad", "eden_linear_input_grad", "eden_activation_grad"]
 
 _DTYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
@@ -40,6 +40,8 @@ def lib():
     L.eden_checkpoint_bytes.restype = sz
     L.eden_layers_workspace_bytes.argtypes = [u64, u64, u64, u32]
     L.eden_layers_workspace_bytes.restype = sz
+    L.eden_layers_copying_bytes.argtypes = [u64, u64, u64, u32]
+    L.eden_layers_copying_bytes.restype = sz
     for name, args in (("eden_checkpoint_save", [vp, u64, u64, u64, u32, vp, sz, vp]),
                        ("eden_checkpoint_restore", [vp, u64, u64, u32, vp, u64, vp]),
                        ("eden_linear", [vp, u64, vp, u64, vp, vp, u64, vp, u64, vp, sz, u64, u64, u64, u32, u32, vp, sz, vp]),
@@ -145,8 +147,10 @@ def _stream(device):
         return torch.cuda.current_stream(device).cuda_stream
 
 
-def _workspace(L, rows, cols, depth, dtype, device):
-    size = L.eden_layers_workspace_bytes(rows, cols, depth, dtype)
+def _workspace(L, rows, cols, depth, dtype, device, pieces):
+    """A workspace; `pieces`: the operands' addresses, distances and widths in elements or-ed together: multiples of eight (and of 16 bytes)
+    need no copies."""
+    size = (L.eden_layers_copying_bytes if pieces % 8 and dtype != F32 else L.eden_layers_workspace_bytes)(rows, cols, depth, dtype)
     if not size:
         return None, None, 0
     t = torch.empty(size, dtype=torch.uint8, device=device)
@@ -253,7 +257,7 @@ def linear(x, w, bias=None, activation: str = "none", residual=None, checkpoint=
     if checkpoint is not False and checkpoint is not None:
         c = _new_checkpoint(None if checkpoint is True else checkpoint, m, n, device)
         cp, capacity = c.buffer.data_ptr(), c.buffer.numel()
-    ws, wsp, size = _workspace(L, m, n, k, dtype, device)
+    ws, wsp, size = _workspace(L, m, n, k, dtype, device, xp >> 1 | wp >> 1 | ldx | ldw | k)
     _check(L.eden_linear(xp, ldx, wp, ldw, bp, rp, ldr, yp, ldy, cp, capacity, m, n, k, dtype, act, wsp, size, _stream(device)), "eden_linear")
     return y if c is None else (y, c)
 
@@ -280,7 +284,7 @@ def linear_weight_grad(dy, saved: Checkpoint, bias: bool = False, out=None, bias
         if n > 1 and db.stride(0) != 1:
             _refuse("linear_weight_grad: bias_out's elements must be neighbours")
         bp = db.data_ptr()
-    ws, wsp, size = _workspace(L, n, k, m, dtype, device)
+    ws, wsp, size = _workspace(L, n, k, m, dtype, device, dp >> 1 | ldy | n)
     _check(L.eden_linear_weight_grad(dp, ldy, sp, wp, ldw, bp, m, n, k, dtype, 1 if accumulate else 0, wsp, size, _stream(device)), "eden_linear_weight_grad")
     return dw if db is None else (dw, db)
 
@@ -311,7 +315,7 @@ def linear_input_grad(dz, w, activation: str = "none", checkpoint: Checkpoint = 
         rp, ldr, _, _ = _rows(residual, "linear_input_grad: residual")
     dx = _output(out, shape, dz, "linear_input_grad: out")
     xp, ldx, _, _ = _rows(dx, "linear_input_grad: out")
-    ws, wsp, size = _workspace(L, m, k, n, dtype, device)
+    ws, wsp, size = _workspace(L, m, k, n, dtype, device, dp >> 1 | wp >> 1 | ldz | ldw | n | k)
     _check(L.eden_linear_input_grad(dp, ldz, wp, ldw, sp, act, rp, ldr, xp, ldx, m, n, k, dtype, wsp, size, _stream(device)), "eden_linear_input_grad")
     return dx
 

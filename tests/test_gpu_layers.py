@@ -343,6 +343,28 @@ def test_large_weight_grad(layers, depth, pad):
     assert bool((flat[:3] == 4.0).all()) and bool((flat[-2:] == 4.0).all())
 
 
+@pytest.mark.parametrize("m,n,k,pad", [(1500, 1501, 1499, 0), (1501, 1504, 1496, 3), (1499, 1500, 1501, 8)])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_large_products_of_rows_that_begin_anywhere(layers, dtype, m, n, k, pad):
+    # operands are copied first where a workspace is given; the same call without one gives the same up to the order of additions
+    t = TYPES[dtype]
+    x, w, dy = wide(1, m, k, t, pad), wide(2, n, k, t, pad, k ** -0.5), wide(3, m, n, t, pad)
+    assert layers.lib().eden_layers_copying_bytes(m, n, k, 1) > layers.lib().eden_layers_workspace_bytes(m, n, k, 1)
+    X, W, Y = x.double(), w.double(), dy.double()
+    y, z = layers.linear(x, w, checkpoint=True)
+    want = X @ W.t().contiguous()
+    assert bool(((y.double() - want).abs() <= ref.product_bound(X, W, k) + ref.ROUND[t] * want.abs() + ref.TINY[t]).all()) and ref.rel(y, want) <= ref.norm_bound(k, t)
+    dx = layers.linear_input_grad(dy, w, activation="gelu_tanh", checkpoint=layers.save_checkpoint(x), residual=x)
+    product = Y @ W
+    want = product * ref.slope(layers.save_checkpoint(x).restore(torch.float32).double(), "gelu_tanh") + X
+    near = 1.13 * ref.product_bound(Y, W.t().contiguous(), n) + 2.0 ** -19 * product.abs() + (4 * ref.EPS + ref.ROUND[t]) * want.abs() + ref.TINY[t]
+    assert bool(((dx.double() - want).abs() <= near).all())
+    c = layers.save_checkpoint(x)
+    dw, db = layers.linear_weight_grad(dy, c, bias=True)
+    want = Y.t().contiguous() @ c.restore(torch.float32).double()
+    assert ref.rel(dw, want) <= ref.norm_bound(m, torch.float32) and ref.rel(db, Y.sum(0)) <= ref.norm_bound(m, torch.float32)
+
+
 def test_large_products_give_the_same_bits_every_time(layers):
     # loads into the LDS, barriers and stages: a missing wait would show as results that come and go
     x, w, dy = wide(1, 4096, 2048, torch.bfloat16), wide(2, 4096, 2048, torch.bfloat16), wide(3, 4096, 4096, torch.bfloat16)
