@@ -69,10 +69,10 @@ bool direct_type(Op op, uint32_t dtype, const Product &p) {
 bool whole_a(Op op, const Product &p) { return whole_pieces(p.a, p.lda, op == kWeightGrad ? p.rows : p.depth); }
 bool whole_b(Op op, const Product &p) { return op == kWeightGrad || whole_pieces(p.b, p.ldb, op == kForward ? p.depth : p.cols); }
 
-// Copies cost two passes over an operand; from 2^31 products on they are less than what they save (bf16, 1021 x 1001 x 2047: 34 us either way).
+// Copies cost two passes over an operand; from 2^30 products on they are less than what they save (bf16, 1021 x 1001 x 2047: 34 -> 27.5 us; 200 x 4001 x 1001: 21 -> 27).
 uint64_t copy_bytes(uint64_t a, uint64_t b) { return (a + 63) / 64 * 64 * ((b + 63) / 64 * 64) * 2; }
 bool worth_copies(uint64_t rows, uint64_t cols, uint64_t depth) {
-    return rows > kFewRows && rows < (1u << 21) && cols < (1u << 21) && depth < (1u << 21) && rows * cols >= (1u << 31) / std::max<uint64_t>(depth, 1);
+    return rows > kFewRows && rows < (1u << 21) && cols < (1u << 21) && depth < (1u << 21) && rows * cols >= (1u << 30) / std::max<uint64_t>(depth, 1);
 }
 // Replaces a 2-byte operand by a copy in the workspace.
 hipError_t copy_operand(const void *&operand, size_t &ld, uint32_t rows, uint32_t cols, uint8_t *&workspace, size_t &room, hipStream_t st) {
