@@ -10,9 +10,7 @@
 //   barriers           one in 64 deep, between the last reads of two tiles and their last products
 // 16-byte pieces of a row are swapped on the way into the LDS (each lane fetches the piece that belongs to its place).  A checkpoint's codes cannot go
 // straight into the LDS: they are read into registers 64 deep ahead, turned into bf16 numbers and stored while the products run.
-#include "eden_layers_product.h"
-
-#include <utility>
+#include "eden_layers_fetch.h"
 
 namespace eden_layers {
 namespace {
@@ -25,29 +23,6 @@ template <int T> struct Tile {
     static constexpr int kLoads = kOperand / 16 / kThreads;        // 16-byte pieces per thread
     static constexpr int kPieces = kSide / 8;                      // of a row of columns
 };
-constexpr uint32_t kMostBytes = 0x7FFFFF00u;       // reach of a descriptor; offsets from kNowhere on lie beyond it (and below 2^32)
-constexpr uint32_t kNowhere = 0x7FFFFFF0u;
-
-using rsrc_t = __amdgpu_buffer_rsrc_t;
-typedef __attribute__((address_space(3))) char lds_char;
-
-// A barrier behind which every wave finds what all waves' loads, but for a wave's last LATER, have written into the LDS, and behind which no wave has LDS
-// reads or writes on their way.  (__syncthreads() would wait for all loads, or for none.)
-template <int LATER> __device__ inline void meet() {
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LATER) : "memory");
-}
-
-template <int... I, class F> __device__ inline void each_of(std::integer_sequence<int, I...>, F f) { (f(std::integral_constant<int, I>()), ...); }
-template <int N, class F> __device__ inline void each(F f) { each_of(std::make_integer_sequence<int, N>(), f); }
-
-// A descriptor in scalar registers
-__device__ inline u32x4 descriptor(const char *base, uint64_t reach) {
-    const uint64_t at = reinterpret_cast<uint64_t>(base);
-    const uint32_t bytes = reach < kMostBytes ? (uint32_t)reach : kMostBytes;
-    return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)at), (uint32_t)__builtin_amdgcn_readfirstlane((int)(at >> 32) & 0xFFFF),
-                 (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), 0x00020000u};
-}
-
 // Where a thread's pieces of an operand come from: byte offsets from the tile's first element.
 template <int T, bool STRIDED> struct Source {
     static constexpr int kSide = Tile<T>::kSide, kPieces = Tile<T>::kPieces;
@@ -87,11 +62,9 @@ template <int T, bool STRIDED> struct Source {
         base += step;
         reach = reach > step ? reach - step : 0;
     }
-    // Load i of the tile, into the LDS at `slot`.  (Written out: the compiler would have every LDS read wait for the loads into any other part of the LDS.
-    // It has no result in registers; meet() waits for it.)
+    // Load i of the tile, into the LDS at `slot`.
     __device__ void fetch(uint32_t slot, int wave, int i) const {
-        const uint32_t to = (uint32_t)__builtin_amdgcn_readfirstlane((int)(slot + (i * 4 + wave) * 1024));
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(at + i * stride), "s"(now) : "memory", "m0");
+        load_to_lds(slot + (i * 4 + wave) * 1024, at + i * stride, now);
     }
 };
 
@@ -163,51 +136,6 @@ template <int T, bool STRIDED> struct Reader {
         }
     }
 };
-
-// Orders a wave's own accesses to the LDS.
-__device__ inline void wave_fence() {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
-
-// The end of 32 x 32 T sums that a wave has left in the LDS: eight columns a lane, so that four lanes have a checkpoint's block and a row's
-// results leave in pieces of 16 bytes side by side; four rows at a time.
-template <int T> constexpr int kRowFloats = 32 * T + 4;            // the four: neighbouring rows begin in different banks
-template <int OP, uint32_t DTYPE, int T>
-__device__ inline void finish_rows(const Product &p, const float *sums, uint32_t row0, uint32_t col0, int lane, uint32_t split) {
-    constexpr int kLanes = 4 * T, kStep = 64 / kLanes;             // lanes of a row; rows side by side
-    const uint32_t first = lane / kLanes, within = lane % kLanes * 8, col = col0 + within;
-    if (row0 + 32 <= p.rows && col0 + 32 * T <= p.cols) {
-        for (uint32_t r = first; r < 32; r += 4 * kStep) {
-            float v[4][8];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                *reinterpret_cast<f32x4 *>(v[i]) = *reinterpret_cast<const f32x4 *>(sums + (r + kStep * i) * kRowFloats<T> + within);
-                *reinterpret_cast<f32x4 *>(v[i] + 4) = *reinterpret_cast<const f32x4 *>(sums + (r + kStep * i) * kRowFloats<T> + within + 4);
-            }
-            if (p.splits > 1) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float *out = p.partial + ((size_t)split * p.rows + row0 + r + kStep * i) * p.partial_ld + col;
-                    *reinterpret_cast<f32x4 *>(out) = *reinterpret_cast<f32x4 *>(v[i]);
-                    *reinterpret_cast<f32x4 *>(out + 4) = *reinterpret_cast<f32x4 *>(v[i] + 4);
-                }
-            } else {
-                finish_inside<OP, DTYPE, 4, kStep>(p.finish, row0 + r, col, v);
-            }
-        }
-        return;
-    }
-    const int valid = col < p.cols ? (int)min(8u, p.cols - col) : 0;
-    for (uint32_t r = first; r < 32; r += kStep) {
-        const uint32_t row = row0 + r;
-        if (row >= p.rows) break;
-        float lo[4], hi[4];
-        *reinterpret_cast<f32x4 *>(lo) = *reinterpret_cast<const f32x4 *>(sums + r * kRowFloats<T> + within);
-        *reinterpret_cast<f32x4 *>(hi) = *reinterpret_cast<const f32x4 *>(sums + r * kRowFloats<T> + within + 4);
-        finish8<OP, DTYPE>(p, row, col, valid, split, lo, hi);
-    }
-}
 
 template <int OP, uint32_t DTYPE, int T> __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(T == 4 ? 1 : 2, T == 4 ? 1 : 2))) void k_direct(const Product p) {
     constexpr int kSide = Tile<T>::kSide, kOperand = Tile<T>::kOperand, kLoads = Tile<T>::kLoads, N = T * T;
@@ -342,24 +270,7 @@ template <int OP, uint32_t DTYPE, int T> __global__ __launch_bounds__(kThreads) 
         }
     }
     meet<0>();                                                     // nothing is read or fetched any more: the LDS takes the sums, 32 rows of each wave at a time
-    float *mine = reinterpret_cast<float *>(lds) + wave * 32 * kRowFloats<T>;
-    for (int i = 0; i < T; ++i) {
-        wave_fence();
-        auto put = [&](const f32x16 (&from)[T]) {
-#pragma unroll
-            for (int j = 0; j < T; ++j)
-#pragma unroll
-                for (int g = 0; g < 4; ++g)
-                    *reinterpret_cast<f32x4 *>(mine + (lane & 31) * kRowFloats<T> + j * 32 + 8 * g + 4 * (lane >> 5)) =
-                        f32x4{from[j][4 * g], from[j][4 * g + 1], from[j][4 * g + 2], from[j][4 * g + 3]};
-        };
-        if (i == 0) put(acc[0]);
-        else if (T == 2 || i == 1) put(acc[1]);
-        else if (i == 2) put(acc[T / 2]);
-        else put(acc[T - 1]);
-        wave_fence();
-        finish_rows<OP, DTYPE, T>(p, mine, row0 + wave_row * (kSide / 2) + (i ^ swap) * 32, col0 + wave_col * (kSide / 2), lane, split);
-    }
+    finish_wave<OP, DTYPE, T>(p, acc, reinterpret_cast<float *>(lds) + wave * 32 * kRowFloats<T>, row0 + wave_row * (kSide / 2), col0 + wave_col * (kSide / 2), swap, lane, split);
 }
 
 }  // namespace

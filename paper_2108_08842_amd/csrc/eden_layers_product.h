@@ -69,56 +69,6 @@ __device__ inline void place_of(uint32_t id, uint32_t total, uint32_t row_tiles,
     col_tile = within / height;
 }
 
-// The end of 32 x 32 sums: a lane has row lane % 32 and columns 8 g + 4 (lane / 32) .. + 3 of the tile's, g = 0 .. 3.
-template <int OP, uint32_t DTYPE>
-__device__ inline void finish_tile(const Product &p, const f32x16 &acc, uint32_t row, uint32_t block_col, int lane, uint32_t split) {
-    if (block_col >= p.cols) return;
-    float v[4][4];
-    int valid[4];
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-        const uint32_t col = block_col + 8 * g + 4 * (lane >> 5);
-        valid[g] = row < p.rows && col < p.cols ? (int)min(4u, p.cols - col) : 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[g][e] = acc[4 * g + e];
-    }
-    if (p.splits > 1) {
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            if (!valid[g]) continue;
-            float *out = p.partial + ((size_t)split * p.rows + row) * p.partial_ld + block_col + 8 * g + 4 * (lane >> 5);
-            *reinterpret_cast<f32x4 *>(out) = f32x4{v[g][0], v[g][1], v[g][2], v[g][3]};      // partial_ld is a multiple of 4
-        }
-        return;
-    }
-#pragma unroll
-    for (int g = 0; g < 4; ++g)
-        if (valid[g]) finish_bias<OP, DTYPE>(p.finish, block_col + 8 * g + 4 * (lane >> 5), valid[g], v[g]);
-    if constexpr (OP == kForward)
-        if (p.finish.codes_out) {
-            uint32_t largest = 0;
-            float z[4][4];
-#pragma unroll
-            for (int g = 0; g < 4; ++g)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    z[g][e] = e < valid[g] ? v[g][e] : 0.0f;
-                    largest = max(largest, magnitude_bits(z[g][e]));
-                }
-            largest = max(largest, (uint32_t)__shfl_xor((int)largest, 32));
-            const uint32_t t = block_exponent(largest);
-            if (row < p.rows) {
-                const size_t block = (size_t)row * p.finish.blocks + block_col / kBlock;
-                if (lane < 32) p.finish.exps_out[block] = (uint8_t)t;
-#pragma unroll
-                for (int g = 0; g < 4; ++g)
-                    *reinterpret_cast<uint32_t *>(p.finish.codes_out + block * kBlock + 8 * g + 4 * (lane >> 5)) = codes4(z[g], t);
-            }
-        }
-#pragma unroll
-    for (int g = 0; g < 4; ++g)
-        if (valid[g]) finish_store<OP, DTYPE>(p.finish, row, block_col + 8 * g + 4 * (lane >> 5), valid[g], v[g]);
-}
 // The end of eight neighbouring sums of a row, `valid` of which the result has (0: the lane takes part in a block's largest value only).  Four lanes side
 // by side have a block of 32.
 template <int OP, uint32_t DTYPE>
@@ -152,6 +102,75 @@ __device__ inline void finish8(const Product &p, uint32_t row, uint32_t col, int
         }
     finish_store8<OP, DTYPE>(p.finish, row, col, valid, lo, hi);
 }
+// Orders a wave's own accesses to the LDS.
+__device__ inline void wave_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// The end of 32 x 32 T sums that a wave has left in the LDS: eight columns a lane, so that four lanes have a checkpoint's block and a row's
+// results leave in pieces of 16 bytes side by side; up to four rows at a time.
+template <int T> constexpr int kRowFloats = 32 * T + 4;            // the four: neighbouring rows begin in different banks
+template <int OP, uint32_t DTYPE, int T>
+__device__ inline void finish_rows(const Product &p, const float *sums, uint32_t row0, uint32_t col0, int lane, uint32_t split) {
+    constexpr int kLanes = 4 * T, kStep = 64 / kLanes;             // lanes of a row; rows side by side
+    constexpr int kRows = 32 / kStep < 4 ? 32 / kStep : 4;
+    const uint32_t first = lane / kLanes, within = lane % kLanes * 8, col = col0 + within;
+    if (row0 + 32 <= p.rows && col0 + 32 * T <= p.cols) {
+        for (uint32_t r = first; r < 32; r += kRows * kStep) {
+            float v[kRows][8];
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) {
+                *reinterpret_cast<f32x4 *>(v[i]) = *reinterpret_cast<const f32x4 *>(sums + (r + kStep * i) * kRowFloats<T> + within);
+                *reinterpret_cast<f32x4 *>(v[i] + 4) = *reinterpret_cast<const f32x4 *>(sums + (r + kStep * i) * kRowFloats<T> + within + 4);
+            }
+            if (p.splits > 1) {
+#pragma unroll
+                for (int i = 0; i < kRows; ++i) {
+                    float *out = p.partial + ((size_t)split * p.rows + row0 + r + kStep * i) * p.partial_ld + col;
+                    *reinterpret_cast<f32x4 *>(out) = *reinterpret_cast<f32x4 *>(v[i]);
+                    *reinterpret_cast<f32x4 *>(out + 4) = *reinterpret_cast<f32x4 *>(v[i] + 4);
+                }
+            } else {
+                finish_inside<OP, DTYPE, kRows, kStep>(p.finish, row0 + r, col, v);
+            }
+        }
+        return;
+    }
+    const int valid = col < p.cols ? (int)min(8u, p.cols - col) : 0;
+    for (uint32_t r = first; r < 32; r += kStep) {
+        const uint32_t row = row0 + r;
+        if (row >= p.rows) break;
+        float lo[4], hi[4];
+        *reinterpret_cast<f32x4 *>(lo) = *reinterpret_cast<const f32x4 *>(sums + r * kRowFloats<T> + within);
+        *reinterpret_cast<f32x4 *>(hi) = *reinterpret_cast<const f32x4 *>(sums + r * kRowFloats<T> + within + 4);
+        finish8<OP, DTYPE>(p, row, col, valid, split, lo, hi);
+    }
+}
+
+// The end of a wave's T x T tiles of 32 x 32 through `mine`, its own 32 * kRowFloats<T> floats of the LDS (that nobody else uses any more); row tile i is
+// number i ^ swap from row0 on.
+template <int OP, uint32_t DTYPE, int T>
+__device__ inline void finish_wave(const Product &p, const f32x16 (&acc)[T][T], float *mine, uint32_t row0, uint32_t col0, int swap, int lane, uint32_t split) {
+    for (int i = 0; i < T; ++i) {
+        wave_fence();
+        auto put = [&](const f32x16 (&from)[T]) {
+#pragma unroll
+            for (int j = 0; j < T; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    *reinterpret_cast<f32x4 *>(mine + (lane & 31) * kRowFloats<T> + j * 32 + 8 * g + 4 * (lane >> 5)) =
+                        f32x4{from[j][4 * g], from[j][4 * g + 1], from[j][4 * g + 2], from[j][4 * g + 3]};
+        };
+        if (i == 0) put(acc[0]);
+        else if (T <= 2 || i == 1) put(acc[T > 1 ? 1 : 0]);
+        else if (i == 2) put(acc[T / 2]);
+        else put(acc[T - 1]);
+        wave_fence();
+        finish_rows<OP, DTYPE, T>(p, mine, row0 + (i ^ swap) * 32, col0, lane, split);
+    }
+}
+
 // Row sums (sums: the product with ones, any of its rows) of row `row`, for one lane of each.
 __device__ inline void finish_row_sum(const Product &p, float sum, uint32_t row, uint32_t split) {
     if (row >= p.rows) return;

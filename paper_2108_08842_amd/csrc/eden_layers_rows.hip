@@ -153,11 +153,8 @@ template <int N, int DISTANCE = 32> __device__ inline float sum_lanes(const floa
     }
 }
 
-constexpr size_t kMostShared = 61440;              // bytes of x in the LDS: two workgroups a CU at least
-template <uint32_t DTYPE> size_t shared_bytes(uint32_t depth, int rows) {
-    constexpr uint32_t kRun = 1024 / Elem<DTYPE>::kBytes;          // elements of a wave's load
-    return (size_t)((depth + kRun - 1) / kRun) * 1024 * rows;
-}
+constexpr uint32_t kMostShared = 61440;            // bytes of x in the LDS at a time: two workgroups a CU at least
+template <int ROWS> __host__ __device__ constexpr uint32_t part_of() { return kMostShared / 16 / ROWS / 64 * 64; }       // pieces of a row
 
 // EACH: rows of w a wave has; ROWS: rows of x (a power of two, those beyond p.rows are zeros)
 template <uint32_t DTYPE, int EACH, int ROWS> __global__ __launch_bounds__(kWaves * 64) void k_dots(const Product p) {
@@ -166,6 +163,7 @@ template <uint32_t DTYPE, int EACH, int ROWS> __global__ __launch_bounds__(kWave
     extern __shared__ u32x4 shared[];                              // x: row r, piece i at r * pieces + i; then the sums
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t pieces = (p.depth + kPiece * 64 - 1) / (kPiece * 64) * 64;                     // a lane has one of every 64
+    const uint32_t part = min(pieces, part_of<ROWS>());                                           // of x in the LDS at a time
     const uint32_t col0 = blockIdx.x * kCols, first = col0 + wave * EACH;
     const T *w[EACH];
     bool has[EACH];
@@ -185,38 +183,42 @@ template <uint32_t DTYPE, int EACH, int ROWS> __global__ __launch_bounds__(kWave
             for (int e = 0; e < EACH; ++e) to.q[i][e] = __builtin_bit_cast(u32x4, load_some<T, kPiece>(w[e] + at, has[e] ? valid : 0));
         }
     };
-    Run even, odd;
-    load(even, 0);                                                 // w is on its way while x is fetched
-    for (uint32_t i = tid; i < ROWS * pieces; i += kWaves * 64) {
-        const uint32_t row = i / pieces, k = (i - row * pieces) * kPiece;
-        const int valid = row < p.rows && k < p.depth ? (int)min((uint32_t)kPiece, p.depth - k) : 0;
-        shared[i] = __builtin_bit_cast(u32x4, load_some<T, kPiece>(static_cast<const T *>(p.a) + (row < p.rows ? row * p.lda + k : 0), valid));
-    }
-    __syncthreads();
-
     float sums[EACH * ROWS] = {};
-    auto multiply = [&](const Run &from, uint32_t piece) {
-#pragma unroll
-        for (int i = 0; i < kRun; ++i) {
-            if (piece + i * 64 >= pieces) break;
-#pragma unroll
-            for (int r = 0; r < ROWS; ++r) {
-                const u32x4 x = shared[r * pieces + piece + i * 64 + lane];
-#pragma unroll
-                for (int e = 0; e < EACH; ++e) sums[e * ROWS + r] = dot_piece<DTYPE>(from.q[i][e], x, sums[e * ROWS + r]);
-            }
+    for (uint32_t from = 0; from < pieces; from += part) {
+        const uint32_t end = min(pieces, from + part), held = end - from;
+        Run even, odd;
+        load(even, from);                                          // w is on its way while x is fetched
+        if (from) __syncthreads();
+        for (uint32_t i = tid; i < ROWS * held; i += kWaves * 64) {
+            const uint32_t row = i / held, piece = i - row * held, k = (from + piece) * kPiece;
+            const int valid = row < p.rows && k < p.depth ? (int)min((uint32_t)kPiece, p.depth - k) : 0;
+            shared[row * part + piece] = __builtin_bit_cast(u32x4, load_some<T, kPiece>(static_cast<const T *>(p.a) + (valid ? row * p.lda + k : 0), valid));
         }
-    };
-    for (uint32_t piece = 0; piece < pieces;) {
-        if (piece + kRun * 64 < pieces) load(odd, piece + kRun * 64);
-        multiply(even, piece);
-        piece += kRun * 64;
-        if (piece >= pieces) break;
-        if (piece + kRun * 64 < pieces) load(even, piece + kRun * 64);
-        multiply(odd, piece);
-        piece += kRun * 64;
+        __syncthreads();
+
+        auto multiply = [&](const Run &run, uint32_t piece) {
+#pragma unroll
+            for (int i = 0; i < kRun; ++i) {
+                if (piece + i * 64 >= end) break;
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r) {
+                    const u32x4 x = shared[r * part + piece - from + i * 64 + lane];
+#pragma unroll
+                    for (int e = 0; e < EACH; ++e) sums[e * ROWS + r] = dot_piece<DTYPE>(run.q[i][e], x, sums[e * ROWS + r]);
+                }
+            }
+        };
+        for (uint32_t piece = from; piece < end;) {
+            if (piece + kRun * 64 < end) load(odd, piece + kRun * 64);
+            multiply(even, piece);
+            piece += kRun * 64;
+            if (piece >= end) break;
+            if (piece + kRun * 64 < end) load(even, piece + kRun * 64);
+            multiply(odd, piece);
+            piece += kRun * 64;
+        }
     }
-    float *out = reinterpret_cast<float *>(shared + ROWS * pieces);                               // [ROWS][kCols]
+    float *out = reinterpret_cast<float *>(shared + ROWS * part);                                 // [ROWS][kCols]
     const float sum = sum_lanes<EACH * ROWS>(sums, lane);
     constexpr int kSame = 64 / (EACH * ROWS);                                                     // lanes with the same sum
     if (lane % kSame == 0) out[lane / kSame % ROWS * kCols + wave * EACH + lane / kSame / ROWS] = sum;
@@ -238,10 +240,12 @@ template <uint32_t DTYPE, int COLS> void launch(const Product &p, hipStream_t st
     k_rows<DTYPE, COLS><<<(p.cols + 16 * COLS - 1) / (16 * COLS), kWaves * 64, 0, st>>>(p);
 }
 template <uint32_t DTYPE, int EACH> void launch_dots(const Product &p, hipStream_t st) {
-    const uint32_t grid = (p.cols + kWaves * EACH - 1) / (kWaves * EACH);
+    constexpr uint32_t kRun = 1024 / Elem<DTYPE>::kBytes;          // elements of a wave's load
+    const uint32_t grid = (p.cols + kWaves * EACH - 1) / (kWaves * EACH), pieces = (p.depth + kRun - 1) / kRun * 64;
     auto with_rows = [&](auto rows) {
         constexpr int ROWS = decltype(rows)::value;
-        k_dots<DTYPE, EACH, ROWS><<<grid, kWaves * 64, shared_bytes<DTYPE>(p.depth, ROWS) + ROWS * kWaves * EACH * sizeof(float), st>>>(p);
+        const uint32_t part = pieces < part_of<ROWS>() ? pieces : part_of<ROWS>();
+        k_dots<DTYPE, EACH, ROWS><<<grid, kWaves * 64, ROWS * (part * 16 + kWaves * EACH * sizeof(float)), st>>>(p);
     };
     if (p.rows == 1) with_rows(std::integral_constant<int, 1>());
     else if (p.rows == 2) with_rows(std::integral_constant<int, 2>());
@@ -250,8 +254,7 @@ template <uint32_t DTYPE, int EACH> void launch_dots(const Product &p, hipStream
 }
 template <uint32_t DTYPE> hipError_t launch_type(const Product &p, hipStream_t st) {
     const bool keeps = p.finish.codes_out != nullptr;              // a checkpoint's block is 32 columns
-    const int rows = p.rows == 1 ? 1 : p.rows == 2 ? 2 : p.rows <= 4 ? 4 : 8;
-    if (p.rows <= 8 && shared_bytes<DTYPE>(p.depth, rows) <= kMostShared) {
+    if (p.rows <= 8) {
         // several rows of w a wave read x less often; fewer leave no CU idle
         if (keeps || p.cols >= 512 * 32) launch_dots<DTYPE, 4>(p, st);
         else if (p.cols >= 512 * 16) launch_dots<DTYPE, 2>(p, st);

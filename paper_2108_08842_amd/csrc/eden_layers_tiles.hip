@@ -30,6 +30,8 @@ template <int OP, uint32_t DTYPE, int W> struct Plan {
     static constexpr int kStages = kTermsA * kTermsB == 1 ? 2 : 1;
     static constexpr int kPlane = kSide * kDepth * 2;                          // bytes of one term of an operand's tile
     static constexpr int kStageBytes = (kTermsA + kTermsB) * kPlane;
+    static constexpr int kEnd = 4 * 32 * kRowFloats<W> * 4;                    // what the end of the sums takes of the LDS
+    static constexpr int kShared = kStages * kStageBytes > kEnd ? kStages * kStageBytes : kEnd;
     static constexpr int kPieces = kSide * kDepth / 8 / kThreads;              // pieces of 8 elements per thread and operand
 };
 
@@ -77,7 +79,7 @@ template <int OP, uint32_t DTYPE, int W> __global__ __launch_bounds__(kThreads, 
     using T = typename Elem<DTYPE>::type;
     constexpr int D = P::kDepth, N = P::kPieces;
     constexpr uint32_t kSide = P::kSide, kAcross = kSide / 8;         // pieces of a row of columns
-    __shared__ __attribute__((aligned(16))) char lds[P::kStages * P::kStageBytes];
+    __shared__ __attribute__((aligned(16))) char lds[P::kShared];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wave_row = wave >> 1, wave_col = wave & 1;
     const uint32_t row_tiles = tiles_of(p.rows, kSide), col_tiles = tiles_of(p.cols, kSide);
@@ -206,11 +208,8 @@ template <int OP, uint32_t DTYPE, int W> __global__ __launch_bounds__(kThreads, 
 
     if constexpr (OP == kWeightGrad)
         if (with_sums && lane < 32) finish_row_sum(p, sums[0], row0 + wave_row * (32 * W) + wave_col * 32 + lane, split);
-#pragma unroll
-    for (int i = 0; i < W; ++i)
-#pragma unroll
-        for (int j = 0; j < W; ++j)
-            finish_tile<OP, DTYPE>(p, acc[i][j], row0 + wave_row * (32 * W) + i * 32 + (lane & 31), col0 + wave_col * (32 * W) + j * 32, lane, split);
+    // (behind the last barrier nobody reads a stage any more)
+    finish_wave<OP, DTYPE, W>(p, acc, reinterpret_cast<float *>(lds) + wave * 32 * kRowFloats<W>, row0 + wave_row * (32 * W), col0 + wave_col * (32 * W), 0, lane, split);
 }
 
 // Sums of the splits, in their order, and the end of the product.  A thread has four columns, eight threads a block of a checkpoint.
