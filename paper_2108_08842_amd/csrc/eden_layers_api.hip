@@ -60,16 +60,20 @@ Shape tiles_shape(uint64_t rows, uint64_t cols, uint64_t depth) {
     return {64, splits_of(tile_count(rows, cols, 64), depth, 1024, 96)};
 }
 
+// fp32 operands straight into the LDS: 128 x 128, two to a CU.
+Shape fp32_shape(uint64_t rows, uint64_t cols, uint64_t depth) { return {128, splits_of(tile_count(rows, cols, 128), depth, 512, 128)}; }
+
 // Rows that start at, and hold, whole 16-byte pieces, and offsets inside a tile that 31 bits hold
-bool whole_pieces(const void *p, uint64_t ld, uint64_t inner) {
-    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0 && inner % 8 == 0 && ld < (1u << 21);
+bool whole_pieces(const void *p, uint64_t ld, uint64_t inner, uint32_t dtype) {
+    const uint64_t piece = dtype == EDEN_F32 ? 4 : 8;
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % piece == 0 && inner % piece == 0 && ld < (1u << 21);
 }
 // Whether the kernel whose loads go straight into the LDS takes a product: as it is, or with copies of the operands whose rows do not fit.
 bool direct_type(Op op, uint32_t dtype, const Product &p) {
-    return dtype != EDEN_F32 && !(op == kWeightGrad && dtype == EDEN_F16) && p.depth != 0 && p.cols != 0 && (op != kWeightGrad || p.ldb < (1u << 24));
+    return !(op == kWeightGrad && dtype != EDEN_BF16) && p.depth != 0 && p.cols != 0 && (op != kWeightGrad || p.ldb < (1u << 24));
 }
-bool whole_a(Op op, const Product &p) { return whole_pieces(p.a, p.lda, op == kWeightGrad ? p.rows : p.depth); }
-bool whole_b(Op op, const Product &p) { return op == kWeightGrad || whole_pieces(p.b, p.ldb, op == kForward ? p.depth : p.cols); }
+bool whole_a(Op op, uint32_t dtype, const Product &p) { return whole_pieces(p.a, p.lda, op == kWeightGrad ? p.rows : p.depth, dtype); }
+bool whole_b(Op op, uint32_t dtype, const Product &p) { return op == kWeightGrad || whole_pieces(p.b, p.ldb, op == kForward ? p.depth : p.cols, dtype); }
 
 // Copies cost two passes over an operand; from 2^30 products on they are less than what they save (bf16, 1021 x 1001 x 2047: 34 -> 27.5 us; 200 x 4001 x 1001: 21 -> 27).
 uint64_t copy_bytes(uint64_t a, uint64_t b) { return (a + 63) / 64 * 64 * ((b + 63) / 64 * 64) * 2; }
@@ -95,11 +99,11 @@ int run(Op op, uint32_t dtype, Product &p, void *workspace, size_t workspace_byt
     p.a_width = op == kWeightGrad ? p.rows : p.depth;
     p.b_width = op == kForward ? p.depth : p.cols;
     bool direct = direct_type(op, dtype, p);
-    if (direct && !(whole_a(op, p) && whole_b(op, p))) {
+    if (direct && !(whole_a(op, dtype, p) && whole_b(op, dtype, p))) {
         // rows along the depth that do not end with a piece need zeros behind it in both operands
-        const bool a = !whole_a(op, p), b = !whole_b(op, p);
+        const bool a = !whole_a(op, dtype, p), b = !whole_b(op, dtype, p);
         const uint64_t need = (a ? copy_bytes(p.rows, p.depth) : 0) + (b ? copy_bytes(p.cols, p.depth) : 0);
-        direct = worth_copies(p.rows, p.cols, p.depth) && need <= workspace_bytes;
+        direct = dtype != EDEN_F32 && worth_copies(p.rows, p.cols, p.depth) && need <= workspace_bytes;
         hipError_t e = hipSuccess;
         if (direct && a) {
             e = op == kWeightGrad ? copy_operand(p.a, p.lda, p.depth, p.rows, space, workspace_bytes, st) : copy_operand(p.a, p.lda, p.rows, p.depth, space, workspace_bytes, st);
@@ -111,7 +115,7 @@ int run(Op op, uint32_t dtype, Product &p, void *workspace, size_t workspace_byt
         }
         if (e != hipSuccess) return EDEN_ERR_HIP;
     }
-    const Shape shape = direct ? direct_shape(p.rows, p.cols, p.depth) : tiles_shape(p.rows, p.cols, p.depth);
+    const Shape shape = !direct ? tiles_shape(p.rows, p.cols, p.depth) : dtype == EDEN_F32 ? fp32_shape(p.rows, p.cols, p.depth) : direct_shape(p.rows, p.cols, p.depth);
     if (tile_count(p.rows, p.cols, shape.side) > kMostGroups / 64) return EDEN_ERR_INVALID_ARG;
     uint64_t splits = shape.splits;
     while (splits > 1 && partial_bytes(p.rows, p.cols, splits) > workspace_bytes) --splits;
@@ -121,7 +125,7 @@ int run(Op op, uint32_t dtype, Product &p, void *workspace, size_t workspace_byt
     p.split_depth = (uint32_t)each;
     p.partial = reinterpret_cast<float *>(space);
     p.partial_ld = (p.cols + 3) / 4 * 4;
-    hipError_t e = direct ? launch_direct(op, dtype, p, shape.side, st) : launch_tiles(op, dtype, p, shape.side, st);
+    hipError_t e = !direct ? launch_tiles(op, dtype, p, shape.side, st) : dtype == EDEN_F32 ? launch_direct_fp32(op, p, st) : launch_direct(op, dtype, p, shape.side, st);
     if (e == hipSuccess && p.splits > 1) e = launch_join(op, dtype, p, st);
     return status(e);
 }
@@ -155,7 +159,7 @@ int eden_checkpoint_restore(const void *checkpoint, uint64_t rows, uint64_t cols
 size_t eden_layers_workspace_bytes(uint64_t rows, uint64_t cols, uint64_t depth, uint32_t dtype) {
     if (!known_type(dtype) || rows > kMostSize || cols > kMostSize || depth > kMostSize) return 0;
     if (rows == 0 || cols == 0) return 0;
-    const uint64_t splits = std::max(direct_shape(rows, cols, depth).splits, tiles_shape(rows, cols, depth).splits);
+    const uint64_t splits = std::max(dtype == EDEN_F32 ? fp32_shape(rows, cols, depth).splits : direct_shape(rows, cols, depth).splits, tiles_shape(rows, cols, depth).splits);
     return splits > 1 ? partial_bytes(rows, cols, splits) : 0;
 }
 

@@ -1,13 +1,12 @@
-// Matrix products of fp32 operands whose rows are whole 16-byte pieces.
+// Matrix products of two fp32 operands whose rows are whole 16-byte pieces (eden_linear, eden_linear_input_grad).
 //
-// out[r][c] = sum_d A(r, d) B(c, d) as products of bf16 terms: x = h + m + l, each the upper 16 bits of what the ones before leave (exact).  Two fp32 operands take
-// the six products down to 2^-16 of the first, an fp32 operand and a checkpoint three (all).  The matrix cores do that at 2500 / 6 and 2500 / 3 TFLOP/s at
-// most; their own fp32 products end at 157.
+// out[r][c] = sum_d A(r, d) B(c, d) as products of bf16 terms: x = h + m + l, each the upper 16 bits of what the ones before leave (exact), and the six products
+// down to 2^-16 of the first.  The matrix cores do that at 2500 / 6 TFLOP/s at most; their own fp32 products end at 157.
 //
 // A workgroup has a tile of 128 x 128, two to a CU, a wave 64 x 64.  Operands' tiles are 32 deep (128-byte lines) and go straight into the LDS as fp32; the LDS
 // holds five, in turns as in the kernel for two-byte types: the two in use, the next two, the first of the two after that.  A wave reads the
-// operands of the next 16 deep and takes them apart in registers while it multiplies those of the last: 5.5 vector instructions an element (7.5 where infinities
-// have to stay what they are), 176 in the time of 24 products.
+// operands of the next 16 deep and takes them apart in registers while it multiplies those of the last: 5.5 vector instructions an element,
+// 176 in the time of 24 products.  Bound by the card's power: 4096 x 8192 x 4096 runs at 204 TFLOP/s with the matrix cores busy 68% of the cycles at 1.5 GHz.
 #include "eden_layers_fetch.h"
 
 namespace eden_layers {
@@ -72,12 +71,12 @@ struct Raw { float v[8]; };
 template <bool STRIDED> struct Reader {
     uint32_t at[STRIDED ? 2 : 4];
 
-    __device__ Reader(int base, int lane, int swap = 0) {
+    __device__ Reader(int base, int lane) {
         const int half = lane >> 5;
         if constexpr (STRIDED) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const int col = base + (i ^ swap) * 32 + (lane & 31);
+                const int col = base + i * 32 + (lane & 31);
                 at[i] = piece_of_fp32_depth(8 * half, col >> 2) + (col & 3) * 4;
             }
         } else {
@@ -98,55 +97,21 @@ template <bool STRIDED> struct Reader {
     }
 };
 
-// Elements 2 q and 2 q + 1 as three terms each.  KEEP: an infinity is its first term alone (else the others are NaN).
-template <bool KEEP> __device__ inline void take_apart(const Raw &r, int q, u32x4 (&terms)[3]) {
+// Elements 2 q and 2 q + 1 as three terms each (of an infinity the others are NaN).
+__device__ inline void take_apart(const Raw &r, int q, u32x4 (&terms)[3]) {
     float a = r.v[2 * q], b = r.v[2 * q + 1];
 #pragma unroll
     for (int t = 0; t < 3; ++t) {
         terms[t][q] = upper_halves(a, b);
-        if (t == 2) break;
-        const float rest_a = a - __uint_as_float(__float_as_uint(a) & 0xFFFF0000u), rest_b = b - __uint_as_float(__float_as_uint(b) & 0xFFFF0000u);
-        a = KEEP && t == 0 && __builtin_isinf(a) ? 0.0f : rest_a;
-        b = KEEP && t == 0 && __builtin_isinf(b) ? 0.0f : rest_b;
+        a -= __uint_as_float(__float_as_uint(a) & 0xFFFF0000u);
+        b -= __uint_as_float(__float_as_uint(b) & 0xFFFF0000u);
     }
 }
 
-// A checkpoint's codes: 16 neighbouring lanes have the pieces of one depth (8 codes each), a thread two depths of a tile.  What lies beyond the depths of the split is
-// read as zeros (codes 0, unit 0).
-struct Codes {
-    const uint8_t *codes, *exps;
-    uint64_t codes_reach, exps_reach;
-    size_t ld;
-    uint32_t blocks, at, exp_at;
-    rsrc_t codes_now, exps_now;
-    u32x2 q[2];
-    uint32_t t[2];
-
-    __device__ Codes(const Product &p, uint32_t col0, uint32_t begin, uint32_t end, int tid)
-        : codes(static_cast<const uint8_t *>(p.b) + (size_t)begin * p.ldb + col0), exps(p.b_exps + (size_t)begin * p.b_blocks + col0 / kBlock),
-          codes_reach((uint64_t)(end - begin) * p.ldb - col0), exps_reach((uint64_t)(end - begin) * p.b_blocks - col0 / kBlock), ld(p.ldb), blocks(p.b_blocks),
-          at((tid / 16) * (uint32_t)p.ldb + tid % 16 * 8), exp_at((tid / 16) * p.b_blocks + tid % 16 / 4) {}
-    __device__ void start() {
-        codes_now = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(codes), 0, (int)(codes_reach < kMostBytes ? (uint32_t)codes_reach : kMostBytes), 0x00020000);
-        exps_now = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(exps), 0, (int)(exps_reach < kMostBytes ? (uint32_t)exps_reach : kMostBytes), 0x00020000);
-        codes += kDeep * ld;
-        exps += (size_t)kDeep * blocks;
-        codes_reach = codes_reach > kDeep * ld ? codes_reach - kDeep * ld : 0;
-        exps_reach = exps_reach > (uint64_t)kDeep * blocks ? exps_reach - (uint64_t)kDeep * blocks : 0;
-    }
-    __device__ void load(int i) {
-        q[i] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(codes_now, (int)(at + i * 16 * (uint32_t)ld), 0, 0));
-        t[i] = __builtin_amdgcn_raw_buffer_load_b8(exps_now, (int)(exp_at + i * 16 * blocks), 0, 0);
-    }
-    __device__ void store(char *tile, int tid, int i) const {
-        *reinterpret_cast<u32x4 *>(tile + piece_of_depth<kSide>(i * 16 + tid / 16, tid % 16)) = code_values(q[i][0], q[i][1], block_unit(t[i]));
-    }
-};
-
 template <int OP> __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_direct_fp32(const Product p) {
-    constexpr bool kStridedA = OP == kWeightGrad, kStridedB = OP != kForward, kCodes = OP == kWeightGrad;
-    constexpr int kProducts = kCodes ? 3 : 6, N = 4 * kProducts;   // terms' products; products 16 deep
-    constexpr int kTermA[6] = {2, 1, kCodes ? 0 : 1, 0, 0, 0}, kTermB[6] = {0, kCodes ? 0 : 1, 0, 2, 1, 0};      // small ones first
+    constexpr bool kStridedB = OP == kInputGrad;
+    constexpr int N = 24;                                          // products 16 deep
+    constexpr int kTermA[6] = {2, 1, 0, 1, 0, 0}, kTermB[6] = {0, 1, 2, 0, 1, 0};      // small ones first
     __shared__ __attribute__((aligned(1024))) char lds[kSlots * kOperand];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wave_row = wave >> 1, wave_col = wave & 1;
@@ -157,62 +122,39 @@ template <int OP> __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_w
     const uint32_t begin = split * p.split_depth, end = min(p.depth, begin + p.split_depth);
     const uint32_t steps = (end - begin + kDeep - 1) / kDeep;      // begin < end: launched for depths above 0 only
 
-    Source<kStridedA> a(p.a, p.lda, row0, p.rows, begin, end, p.a_width, wave, lane);
-    Source<kStridedB> b(p.b, kCodes ? 0 : p.ldb, col0, kCodes ? col0 + 1 : p.cols, begin, end, kCodes ? col0 + 1 : p.b_width, wave, lane);
-    const int swap = kCodes ? wave_col : 0;
-    const Reader<kStridedA> reader_a(wave_row * 64, lane, swap);
+    Source<false> a(p.a, p.lda, row0, p.rows, begin, end, p.a_width, wave, lane);
+    Source<kStridedB> b(p.b, p.ldb, col0, p.cols, begin, end, p.b_width, wave, lane);
+    const Reader<false> reader_a(wave_row * 64, lane);
     const Reader<kStridedB> reader_b(wave_col * 64, lane);
-    Codes codes(p, col0, begin, end, tid);
 
     f32x16 acc[2][2] = {};
-    float sum = 0.0f;                                              // row sum of this lane's depths, of the tile i = 0: the two waves of a row of waves
-    const bool with_sums = kCodes && p.row_sums && col_tile == 0;  // begin with different ones
     u32x4 ta[2][2][3], tb[2][2][3];                                // [set][tile][term]
     Raw raw[4];                                                    // of A's tiles, of B's
 
     const uint32_t lds0 = (uint32_t)(size_t)(lds_char *)lds;
     auto depth_left = [&](uint32_t step) { return end - begin > step * kDeep ? end - begin - step * kDeep : 0u; };
-    auto read = [&](const char *slot_a, const char *slot_b, int s, int set, int i) {              // raw operand i of four
-        if (i < 2) raw[i] = reader_a.read(slot_a, i, s);
-        else if constexpr (!kCodes) raw[i] = reader_b.read(slot_b, i - 2, s);
-        else tb[set][i - 2][0] = fragment<true, kDeep, kSide>(slot_b, wave_col * 64 + (i - 2) * 32, 16 * s, lane);
+    auto read = [&](const char *slot_a, const char *slot_b, int s, int i) {       // raw operand i of four
+        raw[i] = i < 2 ? reader_a.read(slot_a, i, s) : reader_b.read(slot_b, i - 2, s);
     };
     auto split_quarter = [&](int set, int n) {                     // elements 2 (n / 4) .. + 1 of raw operand n % 4
         const int i = n % 4, q = n / 4;
-        if (i < 2) take_apart<kCodes>(raw[i], q, ta[set][i]);
-        else if constexpr (!kCodes) take_apart<false>(raw[i], q, tb[set][i - 2]);
-    };
-    auto add_rows = [&]() {
-        if constexpr (kCodes)
-            if (with_sums) sum += ((raw[0].v[0] + raw[0].v[1]) + (raw[0].v[2] + raw[0].v[3])) + ((raw[0].v[4] + raw[0].v[5]) + (raw[0].v[6] + raw[0].v[7]));
+        take_apart(raw[i], q, i < 2 ? ta[set][i] : tb[set][i - 2]);
     };
     // Products 16 deep of the half S of a tile, while the next half's operands are read (S = 1: of the next tiles, behind a barrier since when nobody needs the present
     // ones) and taken apart.  S = 0 fetches the first operand's tile after the next, S = 1 the second's.
-    auto deep16 = [&](auto half, const char *slot_a, const char *slot_b, uint32_t fetch_to, char *codes_to) {
+    auto deep16 = [&](auto half, const char *slot_a, const char *slot_b, uint32_t fetch_to) {
         constexpr int S = decltype(half)::value;
         each<N>([&](auto number) {
             constexpr int j = decltype(number)::value, product = j / 4, i = j % 4 / 2, c = j % 2;
             acc[i][c] = multiply<false>(tb[S][c][kTermB[product]], ta[S][i][kTermA[product]], acc[i][c]);
-            if constexpr (S == 1 && j == 0) meet<kLoads + (kCodes ? 4 : 0)>();      // (later: the first operand's tile after the next; codes)
-            if constexpr (j < 4) read(slot_a, slot_b, S ^ 1, S ^ 1, j);
-            constexpr int load = due(j, kLoads, N), quarter = due(j - N / 3, 16, N - N / 3);
+            if constexpr (S == 1 && j == 0) meet<kLoads>();        // (later: the first operand's tile after the next)
+            if constexpr (j < 4) read(slot_a, slot_b, S ^ 1, j);
+            constexpr int load = due(j, kLoads, N);
             if constexpr (load >= 0 && S == 0) a.fetch(fetch_to, wave, load);
-            if constexpr (load >= 0 && S == 1 && !kCodes) b.fetch(fetch_to, wave, load);
-            if constexpr (N < 16 ? j >= N / 3 : quarter >= 0) {
-                if constexpr (N < 16) {                            // 16 quarters in 8 places, half of them nothing to do
-                    split_quarter(S ^ 1, 2 * (j - N / 3));
-                    split_quarter(S ^ 1, 2 * (j - N / 3) + 1);
-                } else {
-                    split_quarter(S ^ 1, quarter);
-                }
-            }
-            if constexpr (kCodes && j == N / 2) {
-                codes.store(codes_to, tid, S ^ 1);                 // the first piece in S = 1, the second in the next S = 0
-                codes.load(S ^ 1);
-            }
+            if constexpr (load >= 0 && S == 1) b.fetch(fetch_to, wave, load);
+            if constexpr (j >= 8) split_quarter(S ^ 1, j - 8);
             __builtin_amdgcn_sched_barrier(0);
         });
-        add_rows();
     };
     // Tile number c (first operand of step s: 2 s, second: 2 s + 1) goes to slot c mod 5.
     auto on = [](uint32_t slot, uint32_t tiles) {
@@ -224,43 +166,27 @@ template <int OP> __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_w
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) source.fetch(lds0 + slot * kOperand, wave, i);
     };
-    if constexpr (kCodes) {
-        codes.start();
-        codes.load(0), codes.load(1);
-        codes.store(lds + kOperand, tid, 0), codes.store(lds + kOperand, tid, 1);
-        codes.start();
-        codes.load(0), codes.load(1);
-        codes.start();
-        codes.store(lds + 3 * kOperand, tid, 0);                   // what S = 1 does
-        codes.load(0);
-    }
     fetch_tile(a, 0, 0);
-    if constexpr (!kCodes) fetch_tile(b, 0, 1);
+    fetch_tile(b, 0, 1);
     fetch_tile(a, 1, 2);
-    if constexpr (!kCodes) fetch_tile(b, 1, 3);
+    fetch_tile(b, 1, 3);
     meet<0>();
 #pragma unroll
-    for (int i = 0; i < 4; ++i) read(lds, lds + kOperand, 0, 0, i);
+    for (int i = 0; i < 4; ++i) read(lds, lds + kOperand, 0, i);
 #pragma unroll
     for (int n = 0; n < 16; ++n) split_quarter(0, n);
-    add_rows();
     uint32_t slot = 0;                                             // of the first operand of the present step
     for (uint32_t step = 0; step < steps; ++step) {
         const uint32_t slot_b = on(slot, 1), next_a = on(slot, 2), next_b = on(slot, 3), after_a = on(slot, 4);
         a.start(depth_left(step + 2));
-        deep16(std::integral_constant<int, 0>(), lds + slot, lds + slot_b, lds0 + after_a, lds + next_b);
-        if constexpr (kCodes) codes.start();
-        else b.start(depth_left(step + 2));
-        deep16(std::integral_constant<int, 1>(), lds + next_a, lds + next_b, lds0 + slot, lds + slot);
+        deep16(std::integral_constant<int, 0>(), lds + slot, lds + slot_b, lds0 + after_a);
+        b.start(depth_left(step + 2));
+        deep16(std::integral_constant<int, 1>(), lds + next_a, lds + next_b, lds0 + slot);
         slot = next_a;
     }
 
-    if constexpr (kCodes) {
-        sum += __shfl_xor(sum, 32);
-        if (with_sums && lane < 32) finish_row_sum(p, sum, row0 + wave_row * 64 + swap * 32 + lane, split);
-    }
     meet<0>();                                                     // nothing is read or fetched any more: the LDS takes the sums
-    finish_wave<OP, EDEN_F32, 2>(p, acc, reinterpret_cast<float *>(lds) + wave * 32 * kRowFloats<2>, row0 + wave_row * 64, col0 + wave_col * 64, swap, lane, split);
+    finish_wave<OP, EDEN_F32, 2>(p, acc, reinterpret_cast<float *>(lds) + wave * 32 * kRowFloats<2>, row0 + wave_row * 64, col0 + wave_col * 64, 0, lane, split);
 }
 
 }  // namespace
@@ -268,8 +194,7 @@ template <int OP> __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_w
 hipError_t launch_direct_fp32(Op op, const Product &p, hipStream_t st) {
     const uint32_t grid = tiles_of(p.rows, kSide) * tiles_of(p.cols, kSide) * p.splits;
     if (op == kForward) k_direct_fp32<kForward><<<grid, kThreads, 0, st>>>(p);
-    else if (op == kInputGrad) k_direct_fp32<kInputGrad><<<grid, kThreads, 0, st>>>(p);
-    else k_direct_fp32<kWeightGrad><<<grid, kThreads, 0, st>>>(p);
+    else k_direct_fp32<kInputGrad><<<grid, kThreads, 0, st>>>(p);
     return hipGetLastError();
 }
 

@@ -32,6 +32,8 @@ __host__ __device__ inline uint32_t tiles_of(uint32_t n, uint32_t side) { return
 hipError_t launch_tiles(Op op, uint32_t dtype, const Product &p, uint32_t side, hipStream_t st);
 // side: 128 or 256
 hipError_t launch_direct(Op op, uint32_t dtype, const Product &p, uint32_t side, hipStream_t st);
+// fp32 operands, tiles of 128 x 128
+hipError_t launch_direct_fp32(Op op, const Product &p, hipStream_t st);
 constexpr uint32_t kFewRows = 16;
 hipError_t launch_rows(uint32_t dtype, const Product &p, hipStream_t st);
 hipError_t launch_join(Op op, uint32_t dtype, const Product &p, hipStream_t st);
