@@ -220,12 +220,25 @@ template <int OP, uint32_t DTYPE> __global__ __launch_bounds__(256) void k_join(
         const uint32_t row = (uint32_t)(at / quads), col = (uint32_t)(at % quads) * 4;
         const int valid = col < p.cols ? (int)min(4u, p.cols - col) : 0;
         float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (valid)
-            for (uint32_t s = 0; s < p.splits; ++s) {
-                const f32x4 add = *reinterpret_cast<const f32x4 *>(p.partial + ((size_t)s * p.rows + row) * p.partial_ld + col);
+        if (valid) {
+            const float *from = p.partial + (size_t)row * p.partial_ld + col;
+            const size_t step = (size_t)p.rows * p.partial_ld;
+            uint32_t s = 0;
+            for (; s + 8 <= p.splits; s += 8) {                    // eight reads on their way at a time
+                f32x4 add[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) add[i] = *reinterpret_cast<const f32x4 *>(from + (s + i) * step);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] += add[i][e];
+            }
+            for (; s < p.splits; ++s) {
+                const f32x4 add = *reinterpret_cast<const f32x4 *>(from + s * step);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] += add[e];
             }
+        }
         if (valid) finish_bias<OP, DTYPE>(p.finish, col, valid, v);
         if constexpr (OP == kForward)
             if (p.finish.codes_out) {                              // whole blocks are in range together: quads is a multiple of 8
@@ -246,8 +259,17 @@ template <int OP, uint32_t DTYPE> __global__ __launch_bounds__(256) void k_join(
         if (valid) finish_store<OP, DTYPE>(p.finish, row, col, valid, v);
         if constexpr (OP == kWeightGrad)
             if (p.row_sums && col == 0) {
+                const float *from = p.partial + (size_t)p.splits * p.rows * p.partial_ld + row;
                 float sum = 0.0f;
-                for (uint32_t s = 0; s < p.splits; ++s) sum += p.partial[(size_t)p.splits * p.rows * p.partial_ld + (size_t)s * p.rows + row];
+                uint32_t s = 0;
+                for (; s + 8 <= p.splits; s += 8) {
+                    float add[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) add[i] = from[(size_t)(s + i) * p.rows];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) sum += add[i];
+                }
+                for (; s < p.splits; ++s) sum += from[(size_t)s * p.rows];
                 p.row_sums[row] = p.finish.accumulate ? p.row_sums[row] + sum : sum;
             }
     }
