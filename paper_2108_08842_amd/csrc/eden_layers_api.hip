@@ -50,8 +50,9 @@ Shape direct_shape(uint64_t rows, uint64_t cols, uint64_t depth) {
     const double cost_large = (1.6 * (double)(large / 256) + (left_large > 160 ? 1.6 : left_large ? 1.2 : 0.0)) * deep + 10.0 * (double)((large + 255) / 256);
     const double cost_small = (1.05 * (double)(small / 512) + (left_small > 256 ? 1.05 : left_small ? 0.6 : 0.0)) * deep + 5.0 * (double)((small + 511) / 512);
     if (cost_large < cost_small) return {256, 1};
-    // up to 128 rows the second operand is streamed once: two workgroups a CU read faster where each has enough of it (64 x 16384 x 4096: 42 -> 33 us)
-    const uint64_t splits = splits_of(small, depth, 256, 512);
+    // a split is worth its share of the join from 512 deep on (300 x 512 x 1024: 8.5 us against 8.7 with two), from 128 where there is little to join (32 x 1024 x
+    // 1024: 9.1 -> 7); up to 128 rows the second operand is streamed once: two workgroups a CU read faster where each has enough of it (64 x 16384 x 4096: 42 -> 33)
+    const uint64_t splits = rows * cols <= 40000 ? splits_of(small, depth, 512, 128) : splits_of(small, depth, 256, 512);
     return {128, rows <= 128 ? std::max(splits, splits_of(small, depth, 512, 1024)) : splits};
 }
 // Through registers: 128 x 128 where those fill the device, else 64 x 64, three or more to a CU.
@@ -61,7 +62,7 @@ Shape tiles_shape(uint64_t rows, uint64_t cols, uint64_t depth) {
 }
 
 // fp32 operands straight into the LDS: 128 x 128, two to a CU.
-Shape fp32_shape(uint64_t rows, uint64_t cols, uint64_t depth) { return {128, splits_of(tile_count(rows, cols, 128), depth, 512, 128)}; }
+Shape fp32_shape(uint64_t rows, uint64_t cols, uint64_t depth) { return {128, splits_of(tile_count(rows, cols, 128), depth, 256, 128)}; }
 
 // Rows that start at, and hold, whole 16-byte pieces, and offsets inside a tile that 31 bits hold
 bool whole_pieces(const void *p, uint64_t ld, uint64_t inner, uint32_t dtype) {
