@@ -59,7 +59,7 @@ int eden_checkpoint_restore(const void *checkpoint, uint64_t rows, uint64_t cols
  * (eden_linear: m, n, k;  eden_linear_weight_grad: n, k, m;  eden_linear_input_grad: m, k, n). */
 size_t eden_layers_workspace_bytes(uint64_t rows, uint64_t cols, uint64_t depth, uint32_t dtype);
 
-/* The same and, for large products of fp16 or bf16, room for copies of both operands: a call whose operands' rows do not all start at multiples of
+/* The same and, for large products, room for copies of both operands: a call whose operands' rows do not all start at multiples of
  * 16 bytes and hold whole 16-byte pieces then copies those that do not before it multiplies, which is faster.  Equal to eden_layers_workspace_bytes
  * where that is not worth it; no use where all rows are so. */
 size_t eden_layers_copying_bytes(uint64_t rows, uint64_t cols, uint64_t depth, uint32_t dtype);

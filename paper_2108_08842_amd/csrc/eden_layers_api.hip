@@ -76,16 +76,18 @@ bool direct_type(Op op, uint32_t dtype, const Product &p) {
 bool whole_a(Op op, uint32_t dtype, const Product &p) { return whole_pieces(p.a, p.lda, op == kWeightGrad ? p.rows : p.depth, dtype); }
 bool whole_b(Op op, uint32_t dtype, const Product &p) { return op == kWeightGrad || whole_pieces(p.b, p.ldb, op == kForward ? p.depth : p.cols, dtype); }
 
-// Copies cost two passes over an operand; from 2^30 products on they are less than what they save (bf16, 1021 x 1001 x 2047: 34 -> 27.5 us; 200 x 4001 x 1001: 21 -> 27).
-uint64_t copy_bytes(uint64_t a, uint64_t b) { return (a + 63) / 64 * 64 * ((b + 63) / 64 * 64) * 2; }
-bool worth_copies(uint64_t rows, uint64_t cols, uint64_t depth) {
-    return rows > kFewRows && rows < (1u << 21) && cols < (1u << 21) && depth < (1u << 21) && rows * cols >= (1u << 30) / std::max<uint64_t>(depth, 1);
+// Copies cost two passes over an operand and are worth it from about 2^30 products on in 2 bytes (1021 x 1001 x 2047: 34 -> 27.5 us; 200 x 4001 x 1001 would take 27 in
+// place of 21), from 2^29 in fp32 (1235 x 7079 x 2681: 679 -> 360 us, 301 x 2001 x 1001: 60 -> 34, 831 x 831 x 831: 34 -> 31, 777 x 777 x 777: no difference).
+uint64_t copy_bytes(uint64_t a, uint64_t b, uint32_t dtype) { return (a + 63) / 64 * 64 * ((b + 63) / 64 * 64) * bytes_of(dtype); }
+bool worth_copies(uint64_t rows, uint64_t cols, uint64_t depth, uint32_t dtype) {
+    const uint64_t most = 1u << 21, least = dtype == EDEN_F32 ? 1u << 29 : 1u << 30;
+    return rows > kFewRows && rows < most && cols < most && depth < most && rows * cols >= least / std::max<uint64_t>(depth, 1);
 }
-// Replaces a 2-byte operand by a copy in the workspace.
-hipError_t copy_operand(const void *&operand, size_t &ld, uint32_t rows, uint32_t cols, uint8_t *&workspace, size_t &room, hipStream_t st) {
+// Replaces an operand by a copy in the workspace.
+hipError_t copy_operand(uint32_t dtype, const void *&operand, size_t &ld, uint32_t rows, uint32_t cols, uint8_t *&workspace, size_t &room, hipStream_t st) {
     const uint32_t to_ld = (cols + 63) / 64 * 64;
-    const hipError_t e = launch_copy_rows(operand, ld, rows, cols, workspace, to_ld, st);
-    const size_t used = copy_bytes(rows, cols);
+    const hipError_t e = launch_copy_rows(dtype, operand, ld, rows, cols, workspace, to_ld, st);
+    const size_t used = copy_bytes(rows, cols, dtype);
     operand = workspace, ld = to_ld, workspace += used, room -= used;
     return e;
 }
@@ -103,15 +105,15 @@ int run(Op op, uint32_t dtype, Product &p, void *workspace, size_t workspace_byt
     if (direct && !(whole_a(op, dtype, p) && whole_b(op, dtype, p))) {
         // rows along the depth that do not end with a piece need zeros behind it in both operands
         const bool a = !whole_a(op, dtype, p), b = !whole_b(op, dtype, p);
-        const uint64_t need = (a ? copy_bytes(p.rows, p.depth) : 0) + (b ? copy_bytes(p.cols, p.depth) : 0);
-        direct = dtype != EDEN_F32 && worth_copies(p.rows, p.cols, p.depth) && need <= workspace_bytes;
+        const uint64_t need = (a ? copy_bytes(p.rows, p.depth, dtype) : 0) + (b ? copy_bytes(p.cols, p.depth, dtype) : 0);
+        direct = worth_copies(p.rows, p.cols, p.depth, dtype) && need <= workspace_bytes;
         hipError_t e = hipSuccess;
         if (direct && a) {
-            e = op == kWeightGrad ? copy_operand(p.a, p.lda, p.depth, p.rows, space, workspace_bytes, st) : copy_operand(p.a, p.lda, p.rows, p.depth, space, workspace_bytes, st);
+            e = op == kWeightGrad ? copy_operand(dtype, p.a, p.lda, p.depth, p.rows, space, workspace_bytes, st) : copy_operand(dtype, p.a, p.lda, p.rows, p.depth, space, workspace_bytes, st);
             p.a_width = (uint32_t)p.lda;
         }
         if (direct && b && e == hipSuccess) {
-            e = op == kForward ? copy_operand(p.b, p.ldb, p.cols, p.depth, space, workspace_bytes, st) : copy_operand(p.b, p.ldb, p.depth, p.cols, space, workspace_bytes, st);
+            e = op == kForward ? copy_operand(dtype, p.b, p.ldb, p.cols, p.depth, space, workspace_bytes, st) : copy_operand(dtype, p.b, p.ldb, p.depth, p.cols, space, workspace_bytes, st);
             p.b_width = (uint32_t)p.ldb;
         }
         if (e != hipSuccess) return EDEN_ERR_HIP;
@@ -167,8 +169,8 @@ size_t eden_layers_workspace_bytes(uint64_t rows, uint64_t cols, uint64_t depth,
 size_t eden_layers_copying_bytes(uint64_t rows, uint64_t cols, uint64_t depth, uint32_t dtype) {
     if (!known_type(dtype) || rows > kMostSize || cols > kMostSize || depth > kMostSize) return 0;
     const size_t plain = eden_layers_workspace_bytes(rows, cols, depth, dtype);
-    if (dtype == EDEN_F32 || !worth_copies(rows, cols, depth)) return plain;
-    return plain + copy_bytes(rows, depth) + copy_bytes(cols, depth);
+    if (!worth_copies(rows, cols, depth, dtype)) return plain;
+    return plain + copy_bytes(rows, depth, dtype) + copy_bytes(cols, depth, dtype);
 }
 
 int eden_linear(const void *x, uint64_t ldx, const void *w, uint64_t ldw, const void *bias, const void *residual, uint64_t ldr, void *y, uint64_t ldy,

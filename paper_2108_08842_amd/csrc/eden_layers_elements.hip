@@ -98,18 +98,18 @@ __global__ __launch_bounds__(kThreads) void k_activation_grad(const typename Ele
     store_some<T, 8>(dz + (size_t)at.row * ldz + at.col, v, valid);
 }
 
-__global__ __launch_bounds__(kThreads) void k_copy_rows(const uint16_t *from, size_t ld, uint32_t rows, uint32_t cols, uint16_t *to, uint32_t to_ld, uint32_t shift,
-                                                        uint32_t segments) {
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_copy_rows(const T *from, size_t ld, uint32_t rows, uint32_t cols, T *to, uint32_t to_ld, uint32_t shift, uint32_t segments) {
     const Place at = place(shift, segments);
     if (at.row >= rows || at.col >= to_ld) return;
-    Vec<uint16_t, 8> v;
+    Vec<T, 8> v;
     const int valid = valid_of(at.col, cols);
-    const uint16_t *p = from + (size_t)at.row * ld + at.col;
+    const T *p = from + (size_t)at.row * ld + at.col;
     if (valid == 8) {
         __builtin_memcpy(&v, p, sizeof(v));
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v.v[i] = i < valid ? p[i] : (uint16_t)0;
+        for (int i = 0; i < 8; ++i) v.v[i] = i < valid ? p[i] : (T)0;
     }
     __builtin_memcpy(__builtin_assume_aligned(to + (size_t)at.row * to_ld + at.col, 16), &v, sizeof(v));
 }
@@ -132,9 +132,11 @@ hipError_t launch_save(uint32_t dtype, const void *x, size_t ldx, uint32_t rows,
     });
 }
 
-hipError_t launch_copy_rows(const void *from, size_t ld, uint32_t rows, uint32_t cols, void *to, uint32_t to_ld, hipStream_t st) {
+hipError_t launch_copy_rows(uint32_t dtype, const void *from, size_t ld, uint32_t rows, uint32_t cols, void *to, uint32_t to_ld, hipStream_t st) {
     const Spread s = spread(rows, to_ld);
-    k_copy_rows<<<(uint32_t)s.groups, kThreads, 0, st>>>(static_cast<const uint16_t *>(from), ld, rows, cols, static_cast<uint16_t *>(to), to_ld, s.shift, s.segments);
+    if (dtype == EDEN_F32)
+        k_copy_rows<<<(uint32_t)s.groups, kThreads, 0, st>>>(static_cast<const uint32_t *>(from), ld, rows, cols, static_cast<uint32_t *>(to), to_ld, s.shift, s.segments);
+    else k_copy_rows<<<(uint32_t)s.groups, kThreads, 0, st>>>(static_cast<const uint16_t *>(from), ld, rows, cols, static_cast<uint16_t *>(to), to_ld, s.shift, s.segments);
     return hipGetLastError();
 }
 

@@ -38,8 +38,8 @@ constexpr uint32_t kFewRows = 16;
 hipError_t launch_rows(uint32_t dtype, const Product &p, hipStream_t st);
 hipError_t launch_join(Op op, uint32_t dtype, const Product &p, hipStream_t st);
 
-// 2-byte elements: rows x cols at distance ld -> rows at distance `to_ld`, zeros behind the columns
-hipError_t launch_copy_rows(const void *from, size_t ld, uint32_t rows, uint32_t cols, void *to, uint32_t to_ld, hipStream_t st);
+// rows x cols at distance ld -> rows at distance `to_ld`, zeros behind the columns
+hipError_t launch_copy_rows(uint32_t dtype, const void *from, size_t ld, uint32_t rows, uint32_t cols, void *to, uint32_t to_ld, hipStream_t st);
 
 hipError_t launch_save(uint32_t dtype, const void *x, size_t ldx, uint32_t rows, uint32_t cols, uint8_t *codes, uint8_t *exps, hipStream_t st);
 hipError_t launch_restore(uint32_t dtype, const uint8_t *codes, const uint8_t *exps, uint32_t rows, uint32_t cols, void *x, size_t ldx, hipStream_t st);

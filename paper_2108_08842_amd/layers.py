@@ -147,10 +147,10 @@ def _stream(device):
         return torch.cuda.current_stream(device).cuda_stream
 
 
-def _workspace(L, rows, cols, depth, dtype, device, pieces):
-    """A workspace; `pieces`: the operands' addresses, distances and widths in elements or-ed together: multiples of eight (and of 16 bytes)
-    need no copies."""
-    size = (L.eden_layers_copying_bytes if pieces % 8 and dtype != F32 else L.eden_layers_workspace_bytes)(rows, cols, depth, dtype)
+def _workspace(L, rows, cols, depth, dtype, device, addresses, elements):
+    """A workspace; `addresses`: those of the operands or-ed together, `elements`: distances and widths: multiples of 16 bytes need no copies."""
+    whole = addresses % 16 == 0 and elements % (4 if dtype == F32 else 8) == 0
+    size = (L.eden_layers_workspace_bytes if whole else L.eden_layers_copying_bytes)(rows, cols, depth, dtype)
     if not size:
         return None, None, 0
     t = torch.empty(size, dtype=torch.uint8, device=device)
@@ -257,7 +257,7 @@ def linear(x, w, bias=None, activation: str = "none", residual=None, checkpoint=
     if checkpoint is not False and checkpoint is not None:
         c = _new_checkpoint(None if checkpoint is True else checkpoint, m, n, device)
         cp, capacity = c.buffer.data_ptr(), c.buffer.numel()
-    ws, wsp, size = _workspace(L, m, n, k, dtype, device, xp >> 1 | wp >> 1 | ldx | ldw | k)
+    ws, wsp, size = _workspace(L, m, n, k, dtype, device, xp | wp, ldx | ldw | k)
     _check(L.eden_linear(xp, ldx, wp, ldw, bp, rp, ldr, yp, ldy, cp, capacity, m, n, k, dtype, act, wsp, size, _stream(device)), "eden_linear")
     return y if c is None else (y, c)
 
@@ -284,7 +284,7 @@ def linear_weight_grad(dy, saved: Checkpoint, bias: bool = False, out=None, bias
         if n > 1 and db.stride(0) != 1:
             _refuse("linear_weight_grad: bias_out's elements must be neighbours")
         bp = db.data_ptr()
-    ws, wsp, size = _workspace(L, n, k, m, dtype, device, dp >> 1 | ldy | n)
+    ws, wsp, size = _workspace(L, n, k, m, dtype, device, dp, ldy | n) if dtype == BF16 else _workspace(L, n, k, m, dtype, device, 0, 0)
     _check(L.eden_linear_weight_grad(dp, ldy, sp, wp, ldw, bp, m, n, k, dtype, 1 if accumulate else 0, wsp, size, _stream(device)), "eden_linear_weight_grad")
     return dw if db is None else (dw, db)
 
@@ -315,7 +315,7 @@ def linear_input_grad(dz, w, activation: str = "none", checkpoint: Checkpoint = 
         rp, ldr, _, _ = _rows(residual, "linear_input_grad: residual")
     dx = _output(out, shape, dz, "linear_input_grad: out")
     xp, ldx, _, _ = _rows(dx, "linear_input_grad: out")
-    ws, wsp, size = _workspace(L, m, k, n, dtype, device, dp >> 1 | wp >> 1 | ldz | ldw | n | k)
+    ws, wsp, size = _workspace(L, m, k, n, dtype, device, dp | wp, ldz | ldw | n | k)
     _check(L.eden_linear_input_grad(dp, ldz, wp, ldw, sp, act, rp, ldr, xp, ldx, m, n, k, dtype, wsp, size, _stream(device)), "eden_linear_input_grad")
     return dx
 

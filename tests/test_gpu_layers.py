@@ -344,7 +344,7 @@ def test_large_weight_grad(layers, depth, pad):
 
 
 @pytest.mark.parametrize("m,n,k,pad", [(1500, 1501, 1499, 0), (1501, 1504, 1496, 3), (1499, 1500, 1501, 8)])
-@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("dtype", TYPES)
 def test_large_products_of_rows_that_begin_anywhere(layers, dtype, m, n, k, pad):
     # operands are copied first where a workspace is given; the same call without one gives the same up to the order of additions
     t = TYPES[dtype]
@@ -363,6 +363,23 @@ def test_large_products_of_rows_that_begin_anywhere(layers, dtype, m, n, k, pad)
     dw, db = layers.linear_weight_grad(dy, c, bias=True)
     want = Y.t().contiguous() @ c.restore(torch.float32).double()
     assert ref.rel(dw, want) <= ref.norm_bound(m, torch.float32) and ref.rel(db, Y.sum(0)) <= ref.norm_bound(m, torch.float32)
+
+
+@pytest.mark.parametrize("m,depth,n,pad", [(129, 4, 260, 0), (300, 36, 516, 4), (1000, 1000, 1284, 0), (2100, 100, 2052, 12)])
+def test_large_fp32_products(layers, m, depth, n, pad):
+    # rows of whole 16-byte pieces: depths around the kernel's steps of 32, tiles that end inside the result, one and several splits
+    x, w, bias, r = wide(1, m, depth, torch.float32, pad), wide(2, n, depth, torch.float32, pad, depth ** -0.5), wide(3, 1, n, torch.float32)[0], wide(4, m, n, torch.float32, pad)
+    y, c = layers.linear(x, w, bias, residual=r, checkpoint=True)
+    z = x.double() @ w.double().t().contiguous() + bias.double()
+    want = z + r.double()
+    assert bool(((y.double() - want).abs() <= ref.product_bound(x.double(), w.double(), depth) + 6 * ref.EPS * (z.abs() + want.abs())).all())
+    assert ref.rel(y, want) <= ref.norm_bound(depth, torch.float32)
+    assert torch.equal(layers.save_checkpoint(layers.linear(x, w, bias)).buffer, c.buffer)
+    dz, v = wide(5, m, depth, torch.float32, pad), wide(6, depth, n, torch.float32, pad)
+    want = dz.double() @ v.double()
+    dx = layers.linear_input_grad(dz, v)
+    assert bool(((dx.double() - want).abs() <= ref.product_bound(dz.double(), v.double().t().contiguous(), depth)).all())
+    assert ref.rel(dx, want) <= ref.norm_bound(depth, torch.float32)
 
 
 def test_large_products_give_the_same_bits_every_time(layers):

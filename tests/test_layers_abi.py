@@ -49,10 +49,10 @@ def test_workspace_is_for_long_sums_of_small_results_only(layers):
     assert size(1, 1, 1, 3) == 0 and size(2 ** 30 + 1, 1, 1, 0) == 0
 
 
-def test_room_for_copies_is_for_large_products_of_two_byte_types(layers):
+def test_room_for_copies_is_for_large_products(layers):
     plain, copying = layers.lib().eden_layers_workspace_bytes, layers.lib().eden_layers_copying_bytes
     assert copying(4001, 4001, 4001, layers.BF16) >= plain(4001, 4001, 4001, layers.BF16) + 2 * 2 * 4001 * 4001
-    assert copying(4001, 4001, 4001, layers.F32) == plain(4001, 4001, 4001, layers.F32)
+    assert copying(4001, 4001, 4001, layers.F32) >= plain(4001, 4001, 4001, layers.F32) + 2 * 4 * 4001 * 4001
     assert copying(100, 100, 8192, layers.F16) == plain(100, 100, 8192, layers.F16) and copying(5, 5, 0, layers.F16) == 0
     assert copying(2 ** 30 + 1, 1, 1, 0) == 0 and copying(1, 1, 1, 9) == 0
 
