@@ -186,11 +186,6 @@ template <bool FULL, int R, int C> __device__ inline void multiply_slopes(float 
             for (int c = 0; c < C; ++c) v[r][c] *= slope_as<decltype(a)::value, FULL>(z[r][c]);
     });
 }
-template <bool FULL> __device__ inline float activate(float z, uint32_t act) {
-    float v[1][1] = {{z}};
-    activate_all<FULL>(v, act);
-    return v[0][0];
-}
 template <bool FULL> __device__ inline float slope(float z, uint32_t act) {
     float v[1][1] = {{1.0f}};
     const float at[1][1] = {{z}};
@@ -227,111 +222,73 @@ template <int OP, uint32_t DTYPE> __device__ inline void finish_bias(const Finis
 }
 // ... and what follows.  `valid`: columns of the four that the result has (the caller sees to it that there is one).
 template <int OP, uint32_t DTYPE>
-__device__ inline void finish_store(const Finish &f, uint32_t row, uint32_t col, int valid, float (&v)[4]) {
+__device__ inline void finish_store(const Finish &f, uint32_t row, uint32_t col, int valid, const float (&sums)[4]) {
+    float v[1][4] = {{sums[0], sums[1], sums[2], sums[3]}};
     if constexpr (OP == kWeightGrad) {
         float *out = static_cast<float *>(f.out) + (size_t)row * f.ld_out + col;
         Vec<float, 4> r;
         if (f.accumulate) {
             r = load_some<float, 4>(out, valid);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) r.v[i] += v[i];
+            for (int i = 0; i < 4; ++i) r.v[i] += v[0][i];
         } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) r.v[i] = v[i];
+            for (int i = 0; i < 4; ++i) r.v[i] = v[0][i];
         }
         store_some<float, 4>(out, r, valid);
     } else {
         using T = typename Elem<DTYPE>::type;
         if constexpr (OP == kForward) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = activate<DTYPE == EDEN_F32>(v[i], f.activation);
+            activate_all<DTYPE == EDEN_F32>(v, f.activation);
         } else if (f.codes_in) {
             const uint32_t block = col / kBlock;
-            float z[4];
+            float z[1][4];
             uint32_t codes;
             __builtin_memcpy(&codes, f.codes_in + ((size_t)row * f.blocks + block) * kBlock + col % kBlock, 4);
-            values4(codes, block_unit(f.exps_in[(size_t)row * f.blocks + block]), z);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] *= slope<DTYPE == EDEN_F32>(z[i], f.activation);
+            values4(codes, block_unit(f.exps_in[(size_t)row * f.blocks + block]), z[0]);
+            multiply_slopes<DTYPE == EDEN_F32>(v, z, f.activation);
         }
         if (f.residual) {
             const auto a = load_some<T, 4>(static_cast<const T *>(f.residual) + (size_t)row * f.ld_residual + col, valid);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] += (float)a.v[i];
+            for (int i = 0; i < 4; ++i) v[0][i] += (float)a.v[i];
         }
         Vec<T, 4> r;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) r.v[i] = (T)v[i];
+        for (int i = 0; i < 4; ++i) r.v[i] = (T)v[0][i];
         store_some<T, 4>(static_cast<T *>(f.out) + (size_t)row * f.ld_out + col, r, valid);
     }
 }
 
-// The same for eight neighbouring columns at once where the result has them all: whole 16-byte pieces.
-template <int OP, uint32_t DTYPE>
-__device__ inline void finish_store8(const Finish &f, uint32_t row, uint32_t col, int valid, float (&lo)[4], float (&hi)[4]) {
-    if (OP == kWeightGrad || valid < 8) {
-        if (valid > 0) finish_store<OP, DTYPE>(f, row, col, min(valid, 4), lo);
-        if (valid > 4) finish_store<OP, DTYPE>(f, row, col + 4, valid - 4, hi);
-        return;
-    }
-    using T = typename Elem<DTYPE>::type;
-    if constexpr (OP == kForward) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            lo[i] = activate<DTYPE == EDEN_F32>(lo[i], f.activation);
-            hi[i] = activate<DTYPE == EDEN_F32>(hi[i], f.activation);
-        }
-    } else if (f.codes_in) {
-        const size_t block = (size_t)row * f.blocks + col / kBlock;
-        const u32x2 c = *reinterpret_cast<const u32x2 *>(f.codes_in + block * kBlock + col % kBlock);
-        const float unit = block_unit(f.exps_in[block]);
-        float z0[4], z1[4];
-        values4(c[0], unit, z0);
-        values4(c[1], unit, z1);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            lo[i] *= slope<DTYPE == EDEN_F32>(z0[i], f.activation);
-            hi[i] *= slope<DTYPE == EDEN_F32>(z1[i], f.activation);
-        }
-    }
-    if (f.residual) {
-        const auto a = load_some<T, 8>(static_cast<const T *>(f.residual) + (size_t)row * f.ld_residual + col, 8);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            lo[i] += (float)a.v[i];
-            hi[i] += (float)a.v[4 + i];
-        }
-    }
-    Vec<T, 8> r;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        r.v[i] = (T)lo[i];
-        r.v[4 + i] = (T)hi[i];
-    }
-    store_some<T, 8>(static_cast<T *>(f.out) + (size_t)row * f.ld_out + col, r, 8);
-}
-
-// The whole end of eight neighbouring columns from `col` on of ROWS rows STEP apart, all inside the result; four lanes side by side have a checkpoint's
-// block.  The rows go through it side by side, so that their reads and exponentials overlap.
-template <int OP, uint32_t DTYPE, int ROWS, int STEP> __device__ inline void finish_inside(const Finish &f, uint32_t row, uint32_t col, float (&v)[ROWS][8]) {
+// The whole end of eight neighbouring columns from `col` on of ROWS rows STEP apart; four lanes side by side have a checkpoint's block.  The rows go
+// through it side by side, so that their reads and exponentials overlap, and the activation is chosen once for all of them (once for each value: 301 x 2056
+// bf16, 64 deep, 9.1 us in place of 5.9).
+// Unless INSIDE, the result has `valid` of the columns (none or less: the lane only takes part in its block's largest value) and `rows` rows.
+template <bool INSIDE, int OP, uint32_t DTYPE, int ROWS, int STEP>
+__device__ inline void finish_eight(const Finish &f, uint32_t row, uint32_t rows, uint32_t col, int valid, float (&v)[ROWS][8]) {
+    auto has = [&](int r) { return INSIDE || (valid > 0 && row + r * STEP < rows); };
+    const int n = INSIDE ? 8 : valid;
     if constexpr (OP == kWeightGrad) {
         float *out = static_cast<float *>(f.out) + (size_t)row * f.ld_out + col;
         if (f.accumulate) {
             Vec<float, 8> held[ROWS];
 #pragma unroll
-            for (int r = 0; r < ROWS; ++r) held[r] = load_some<float, 8>(out + (size_t)(r * STEP) * f.ld_out, 8);
+            for (int r = 0; r < ROWS; ++r)
+                if (has(r)) held[r] = load_some<float, 8>(out + (size_t)(r * STEP) * f.ld_out, n);
 #pragma unroll
             for (int r = 0; r < ROWS; ++r)
+                if (has(r))
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[r][i] += held[r].v[i];
+                    for (int i = 0; i < 8; ++i) v[r][i] += held[r].v[i];
         }
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
-            Vec<float, 8> to;
+        for (int r = 0; r < ROWS; ++r)
+            if (has(r)) {
+                Vec<float, 8> to;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) to.v[i] = v[r][i];
-            store_some<float, 8>(out + (size_t)(r * STEP) * f.ld_out, to, 8);
-        }
+                for (int i = 0; i < 8; ++i) to.v[i] = v[r][i];
+                store_some<float, 8>(out + (size_t)(r * STEP) * f.ld_out, to, n);
+            }
     } else {
         using T = typename Elem<DTYPE>::type;
         constexpr bool FULL = DTYPE == EDEN_F32;
@@ -339,11 +296,12 @@ template <int OP, uint32_t DTYPE, int ROWS, int STEP> __device__ inline void fin
         Vec<T, 8> added[ROWS];
         if (f.residual) {
 #pragma unroll
-            for (int r = 0; r < ROWS; ++r) added[r] = load_some<T, 8>(static_cast<const T *>(f.residual) + (size_t)(row + r * STEP) * f.ld_residual + col, 8);
+            for (int r = 0; r < ROWS; ++r)
+                if (has(r)) added[r] = load_some<T, 8>(static_cast<const T *>(f.residual) + (size_t)(row + r * STEP) * f.ld_residual + col, n);
         }
         if constexpr (OP == kForward) {
-            if (f.bias) {
-                const auto b = load_some<T, 8>(static_cast<const T *>(f.bias) + col, 8);
+            if (f.bias && (INSIDE || valid > 0)) {
+                const auto b = load_some<T, 8>(static_cast<const T *>(f.bias) + col, n);
 #pragma unroll
                 for (int r = 0; r < ROWS; ++r)
 #pragma unroll
@@ -356,14 +314,16 @@ template <int OP, uint32_t DTYPE, int ROWS, int STEP> __device__ inline void fin
                     uint32_t largest = 0;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        lo[i] = v[r][i], hi[i] = v[r][4 + i];
+                        lo[i] = i < n ? v[r][i] : 0.0f, hi[i] = 4 + i < n ? v[r][4 + i] : 0.0f;
                         largest = max(largest, max(magnitude_bits(lo[i]), magnitude_bits(hi[i])));
                     }
                     largest = largest_of_quad(largest);
                     const uint32_t t = block_exponent(largest);
                     const size_t at = block + (size_t)(r * STEP) * f.blocks;
-                    *reinterpret_cast<u32x2 *>(f.codes_out + at * kBlock + col % kBlock) = u32x2{codes4(lo, t), codes4(hi, t)};
-                    if (col % kBlock == 0) f.exps_out[at] = (uint8_t)t;
+                    if (INSIDE || (row + r * STEP < rows && col < f.blocks * kBlock)) {
+                        *reinterpret_cast<u32x2 *>(f.codes_out + at * kBlock + col % kBlock) = u32x2{codes4(lo, t), codes4(hi, t)};
+                        if (col % kBlock == 0) f.exps_out[at] = (uint8_t)t;
+                    }
                 }
             }
             activate_all<FULL>(v, f.activation);
@@ -372,8 +332,8 @@ template <int OP, uint32_t DTYPE, int ROWS, int STEP> __device__ inline void fin
 #pragma unroll
             for (int r = 0; r < ROWS; ++r) {
                 const size_t at = block + (size_t)(r * STEP) * f.blocks;
-                const u32x2 c = *reinterpret_cast<const u32x2 *>(f.codes_in + at * kBlock + col % kBlock);
-                const float unit = block_unit(f.exps_in[at]);
+                const u32x2 c = has(r) ? *reinterpret_cast<const u32x2 *>(f.codes_in + at * kBlock + col % kBlock) : u32x2{0, 0};
+                const float unit = block_unit(has(r) ? f.exps_in[at] : (uint8_t)0);
                 float lo[4], hi[4];
                 values4(c[0], unit, lo);
                 values4(c[1], unit, hi);
@@ -383,12 +343,13 @@ template <int OP, uint32_t DTYPE, int ROWS, int STEP> __device__ inline void fin
             multiply_slopes<FULL>(v, z, f.activation);
         }
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
-            Vec<T, 8> to;
+        for (int r = 0; r < ROWS; ++r)
+            if (has(r)) {
+                Vec<T, 8> to;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) to.v[i] = (T)(f.residual ? v[r][i] + (float)added[r].v[i] : v[r][i]);
-            store_some<T, 8>(static_cast<T *>(f.out) + (size_t)(row + r * STEP) * f.ld_out + col, to, 8);
-        }
+                for (int i = 0; i < 8; ++i) to.v[i] = (T)(f.residual ? v[r][i] + (float)added[r].v[i] : v[r][i]);
+                store_some<T, 8>(static_cast<T *>(f.out) + (size_t)(row + r * STEP) * f.ld_out + col, to, n);
+            }
     }
 }
 

@@ -69,39 +69,6 @@ __device__ inline void place_of(uint32_t id, uint32_t total, uint32_t row_tiles,
     col_tile = within / height;
 }
 
-// The end of eight neighbouring sums of a row, `valid` of which the result has (0: the lane takes part in a block's largest value only).  Four lanes side
-// by side have a block of 32.
-template <int OP, uint32_t DTYPE>
-__device__ inline void finish8(const Product &p, uint32_t row, uint32_t col, int valid, uint32_t split, float (&lo)[4], float (&hi)[4]) {
-    const int valid_lo = min(valid, 4), valid_hi = max(valid - 4, 0);
-    if (p.splits > 1) {
-        float *out = p.partial + ((size_t)split * p.rows + row) * p.partial_ld + col;                 // partial_ld is a multiple of 4
-        if (valid_lo) *reinterpret_cast<f32x4 *>(out) = f32x4{lo[0], lo[1], lo[2], lo[3]};
-        if (valid_hi) *reinterpret_cast<f32x4 *>(out + 4) = f32x4{hi[0], hi[1], hi[2], hi[3]};
-        return;
-    }
-    if (valid_lo) finish_bias<OP, DTYPE>(p.finish, col, valid_lo, lo);
-    if (valid_hi) finish_bias<OP, DTYPE>(p.finish, col + 4, valid_hi, hi);
-    if constexpr (OP == kForward)
-        if (p.finish.codes_out) {
-            uint32_t largest = 0;
-            float z[2][4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                z[0][e] = e < valid ? lo[e] : 0.0f;
-                z[1][e] = e + 4 < valid ? hi[e] : 0.0f;
-                largest = max(largest, max(magnitude_bits(z[0][e]), magnitude_bits(z[1][e])));
-            }
-            largest = largest_of_quad(largest);
-            const uint32_t t = block_exponent(largest);
-            if (col < p.finish.blocks * kBlock) {
-                const size_t block = (size_t)row * p.finish.blocks + col / kBlock;
-                *reinterpret_cast<u32x2 *>(p.finish.codes_out + block * kBlock + col % kBlock) = u32x2{codes4(z[0], t), codes4(z[1], t)};
-                if (col % kBlock == 0) p.finish.exps_out[block] = (uint8_t)t;
-            }
-        }
-    finish_store8<OP, DTYPE>(p.finish, row, col, valid, lo, hi);
-}
 // Orders a wave's own accesses to the LDS.
 __device__ inline void wave_fence() {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -116,35 +83,29 @@ __device__ inline void finish_rows(const Product &p, const float *sums, uint32_t
     constexpr int kLanes = 4 * T, kStep = 64 / kLanes;             // lanes of a row; rows side by side
     constexpr int kRows = 32 / kStep < 4 ? 32 / kStep : 4;
     const uint32_t first = lane / kLanes, within = lane % kLanes * 8, col = col0 + within;
-    if (row0 + 32 <= p.rows && col0 + 32 * T <= p.cols) {
-        for (uint32_t r = first; r < 32; r += kRows * kStep) {
-            float v[kRows][8];
+    const int valid = col < p.cols ? (int)min(8u, p.cols - col) : 0;
+    const bool inside = row0 + 32 <= p.rows && col0 + 32 * T <= p.cols;
+    for (uint32_t r = first; r < 32; r += kRows * kStep) {
+        const uint32_t row = row0 + r;
+        float v[kRows][8];
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            *reinterpret_cast<f32x4 *>(v[i]) = *reinterpret_cast<const f32x4 *>(sums + (r + kStep * i) * kRowFloats<T> + within);
+            *reinterpret_cast<f32x4 *>(v[i] + 4) = *reinterpret_cast<const f32x4 *>(sums + (r + kStep * i) * kRowFloats<T> + within + 4);
+        }
+        if (p.splits > 1) {
+            float *out = p.partial + ((size_t)split * p.rows + row) * p.partial_ld + col;             // partial_ld is a multiple of 4
 #pragma unroll
             for (int i = 0; i < kRows; ++i) {
-                *reinterpret_cast<f32x4 *>(v[i]) = *reinterpret_cast<const f32x4 *>(sums + (r + kStep * i) * kRowFloats<T> + within);
-                *reinterpret_cast<f32x4 *>(v[i] + 4) = *reinterpret_cast<const f32x4 *>(sums + (r + kStep * i) * kRowFloats<T> + within + 4);
+                if (row + kStep * i >= p.rows) break;
+                if (valid > 0) *reinterpret_cast<f32x4 *>(out + (size_t)(kStep * i) * p.partial_ld) = *reinterpret_cast<f32x4 *>(v[i]);
+                if (valid > 4) *reinterpret_cast<f32x4 *>(out + (size_t)(kStep * i) * p.partial_ld + 4) = *reinterpret_cast<f32x4 *>(v[i] + 4);
             }
-            if (p.splits > 1) {
-#pragma unroll
-                for (int i = 0; i < kRows; ++i) {
-                    float *out = p.partial + ((size_t)split * p.rows + row0 + r + kStep * i) * p.partial_ld + col;
-                    *reinterpret_cast<f32x4 *>(out) = *reinterpret_cast<f32x4 *>(v[i]);
-                    *reinterpret_cast<f32x4 *>(out + 4) = *reinterpret_cast<f32x4 *>(v[i] + 4);
-                }
-            } else {
-                finish_inside<OP, DTYPE, kRows, kStep>(p.finish, row0 + r, col, v);
-            }
+        } else if (inside) {
+            finish_eight<true, OP, DTYPE, kRows, kStep>(p.finish, row, p.rows, col, 8, v);
+        } else {
+            finish_eight<false, OP, DTYPE, kRows, kStep>(p.finish, row, p.rows, col, valid, v);
         }
-        return;
-    }
-    const int valid = col < p.cols ? (int)min(8u, p.cols - col) : 0;
-    for (uint32_t r = first; r < 32; r += kStep) {
-        const uint32_t row = row0 + r;
-        if (row >= p.rows) break;
-        float lo[4], hi[4];
-        *reinterpret_cast<f32x4 *>(lo) = *reinterpret_cast<const f32x4 *>(sums + r * kRowFloats<T> + within);
-        *reinterpret_cast<f32x4 *>(hi) = *reinterpret_cast<const f32x4 *>(sums + r * kRowFloats<T> + within + 4);
-        finish8<OP, DTYPE>(p, row, col, valid, split, lo, hi);
     }
 }
 
