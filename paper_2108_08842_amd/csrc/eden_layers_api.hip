@@ -55,7 +55,8 @@ Shape direct_shape(uint64_t rows, uint64_t cols, uint64_t depth) {
     const uint64_t splits = rows * cols <= 40000 ? splits_of(small, depth, 512, 128) : splits_of(small, depth, 256, 512);
     return {128, rows <= 128 ? std::max(splits, splits_of(small, depth, 512, 1024)) : splits};
 }
-// Through registers: 128 x 128 where those fill the device, else 64 x 64, three or more to a CU.
+// Through registers: 128 x 128 where those fill the device (fp16 weight gradient 2048 x 4096, 1024 deep: 60 us against 75 with 64 x 64), else 64 x 64, three or more to
+// a CU (512 x 1001 x 1003 bf16: 21 against 24).
 Shape tiles_shape(uint64_t rows, uint64_t cols, uint64_t depth) {
     if (tile_count(rows, cols, 128) >= 256) return {128, 1};
     return {64, splits_of(tile_count(rows, cols, 64), depth, 1024, 96)};
@@ -73,8 +74,24 @@ bool whole_pieces(const void *p, uint64_t ld, uint64_t inner, uint32_t dtype) {
 bool direct_type(Op op, uint32_t dtype, const Product &p) {
     return !(op == kWeightGrad && dtype != EDEN_BF16) && p.depth != 0 && p.cols != 0 && (op != kWeightGrad || p.ldb < (1u << 24));
 }
+// ... and whether that is the faster one: it has a long way to its first product.  2 bytes: two steps deep and up to 2^20 results the general kernel is (1024 x
+// 1024 x 128 bf16 5.0 us against 5.6; 1024 x 1024 x 256 12.5 against 6.3, 2048 x 2048 x 128 8.9 against 6.8).  With a checkpoint below 2^28 products (512 x 512 x 768
+// 11.5 against 14.1; 1024 x 1024 x 256 12.8 against 8.6).  fp32 below 1.5 * 2^28 (1024 x 1024 x 256 15.2 against 17.3; 768 x 768 x 768 23.3 against 22.3,
+// 2048 x 2048 x 512 43 against 34).
+bool direct_pays(Op op, uint32_t dtype, const Product &p) {
+    const double results = (double)p.rows * p.cols, products = results * p.depth;
+    if (dtype == EDEN_F32) return products >= 1.5 * (1u << 28);
+    if (op == kWeightGrad) return products >= 1u << 28;
+    return p.depth > 128 || results > 1u << 20;
+}
 bool whole_a(Op op, uint32_t dtype, const Product &p) { return whole_pieces(p.a, p.lda, op == kWeightGrad ? p.rows : p.depth, dtype); }
 bool whole_b(Op op, uint32_t dtype, const Product &p) { return op == kWeightGrad || whole_pieces(p.b, p.ldb, op == kForward ? p.depth : p.cols, dtype); }
+// More than four rows and so many columns that the 128 x 128 tiles' splits fill the device: the few rows' kernel would read x once for every 16 columns (16 x 16384 x
+// 4096 bf16: 40 us against 32; 16 x 8192 x 4096 22 against 24).
+bool many_columns(uint32_t dtype, const Product &p, uint64_t room) {
+    return dtype != EDEN_F32 && p.rows > 4 && p.cols >= 128 * 128 && whole_a(kForward, dtype, p) && whole_b(kForward, dtype, p) &&
+           partial_bytes(p.rows, p.cols, direct_shape(p.rows, p.cols, p.depth).splits) <= room;
+}
 
 // Copies cost two passes over an operand and are worth it from about 2^30 products on in 2 bytes (1021 x 1001 x 2047: 34 -> 27.5 us; 200 x 4001 x 1001 would take 27 in
 // place of 21), from 2^29 in fp32 (1235 x 7079 x 2681: 679 -> 360 us, 301 x 2001 x 1001: 60 -> 34, 831 x 831 x 831: 34 -> 31, 777 x 777 x 777: no difference).
@@ -96,12 +113,12 @@ hipError_t copy_operand(uint32_t dtype, const void *&operand, size_t &ld, uint32
 int run(Op op, uint32_t dtype, Product &p, void *workspace, size_t workspace_bytes, void *stream) {
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return EDEN_ERR_INVALID_ARG;
-    if (op == kForward && p.rows <= kFewRows) return status(launch_rows(dtype, p, st));
     uint8_t *space = static_cast<uint8_t *>(workspace);
     if (workspace == nullptr) workspace_bytes = 0;
     p.a_width = op == kWeightGrad ? p.rows : p.depth;
     p.b_width = op == kForward ? p.depth : p.cols;
-    bool direct = direct_type(op, dtype, p);
+    bool direct = direct_type(op, dtype, p) && direct_pays(op, dtype, p);
+    if (op == kForward && p.rows <= kFewRows && !(direct && many_columns(dtype, p, workspace_bytes))) return status(launch_rows(dtype, p, st));
     if (direct && !(whole_a(op, dtype, p) && whole_b(op, dtype, p))) {
         // rows along the depth that do not end with a piece need zeros behind it in both operands
         const bool a = !whole_a(op, dtype, p), b = !whole_b(op, dtype, p);

@@ -1,6 +1,6 @@
 // eden_linear for up to 16 rows (single tokens, a few tokens at a time): the weights are read once and everything else is small.  Bound by memory: w's bytes.
 //
-// k_dots, up to 8 rows: x lies in the LDS, a wave has one, two or four rows of w and reads a kilobyte of one at a time; every lane multiplies
+// k_dots, up to 4 rows (fp32: 8): x lies in the LDS, a wave has one, two or four rows of w and reads a kilobyte of one at a time; every lane multiplies
 // its 16 bytes with those of x two elements an instruction, the lanes' sums are added at the end.
 // k_rows, up to 16 rows: a workgroup has 16 or 32 columns of the result and all rows; its eight waves go through the depth in turn, 256 bytes of
 // each of w's rows at a time, from memory to the matrix cores' registers without the LDS (lane l holds row l % 16 of w and 16 bytes of the
@@ -249,15 +249,19 @@ template <uint32_t DTYPE, int EACH> void launch_dots(const Product &p, hipStream
     };
     if (p.rows == 1) with_rows(std::integral_constant<int, 1>());
     else if (p.rows == 2) with_rows(std::integral_constant<int, 2>());
-    else if (p.rows <= 4) with_rows(std::integral_constant<int, 4>());
-    else with_rows(std::integral_constant<int, 8>());
+    else if (DTYPE != EDEN_F32 || p.rows <= 4) with_rows(std::integral_constant<int, 4>());
+    else if constexpr (DTYPE == EDEN_F32) with_rows(std::integral_constant<int, 8>());
 }
 template <uint32_t DTYPE> hipError_t launch_type(const Product &p, hipStream_t st) {
-    const bool keeps = p.finish.codes_out != nullptr;              // a checkpoint's block is 32 columns
-    if (p.rows <= 8) {
-        // several rows of w a wave read x less often; fewer leave no CU idle
-        if (keeps || p.cols >= 512 * 32) launch_dots<DTYPE, 4>(p, st);
-        else if (p.cols >= 512 * 16) launch_dots<DTYPE, 2>(p, st);
+    // k_dots in us, w of 16384 x 4096: 4 rows of bf16 28.5 (k_rows 34), 5 rows 40 (35); fp32, 8 rows 67 (72) and at 1024 x 1024 5.9 (6.3).
+    // Rows of w a wave: a checkpoint's block takes four.  Rows of up to 2 KiB are two loads, so that four of them keep a wave's eight loads on their way
+    // (bf16, 1024 x 1024: 3.8 us against 4.7 with one).  Else two read x half as often where they leave no CU idle (8192 x 4096 bf16, 4 rows:
+    // 16.8 against 18.7 with one, but 4096 x 4096 11.8 against 10.6), one is best while x is small (fp32, 16384 x 4096, 2 rows: 47 against 54 with two).
+    const bool keeps = p.finish.codes_out != nullptr;
+    constexpr bool kFull = DTYPE == EDEN_F32;
+    if (p.rows <= (kFull ? 8 : 4)) {
+        if (keeps || (!kFull && p.depth <= 1024)) launch_dots<DTYPE, 4>(p, st);
+        else if (p.cols >= 512 * 16 && p.rows > (kFull ? 2 : 1)) launch_dots<DTYPE, 2>(p, st);
         else launch_dots<DTYPE, 1>(p, st);
     } else {
         if (keeps) launch<DTYPE, 2>(p, st);

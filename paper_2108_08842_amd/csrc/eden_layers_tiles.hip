@@ -19,7 +19,6 @@ constexpr int kThreads = 256;
 
 // W: a wave has W x W products of 32 x 32, a workgroup 64 W x 64 W
 template <int OP, uint32_t DTYPE, int W> struct Plan {
-    static constexpr bool kTwoBytes = DTYPE != EDEN_F32;
     static constexpr int kTermsA = DTYPE == EDEN_F32 ? 3 : (OP == kWeightGrad && DTYPE == EDEN_F16) ? 2 : 1;
     static constexpr int kTermsB = OP == kWeightGrad ? 1 : DTYPE == EDEN_F32 ? 3 : 1;
     static constexpr bool kHalf = DTYPE == EDEN_F16 && OP != kWeightGrad;      // fp16 products

@@ -365,7 +365,43 @@ def test_large_products_of_rows_that_begin_anywhere(layers, dtype, m, n, k, pad)
     assert ref.rel(dw, want) <= ref.norm_bound(m, torch.float32) and ref.rel(db, Y.sum(0)) <= ref.norm_bound(m, torch.float32)
 
 
-@pytest.mark.parametrize("m,depth,n,pad", [(129, 4, 260, 0), (300, 36, 516, 4), (1000, 1000, 1284, 0), (2100, 100, 2052, 12)])
+@pytest.mark.parametrize("m,n,k,pad", [(300, 264, 136, 0), (1100, 1000, 72, 8), (1033, 1016, 8, 0), (200, 520, 1000, 16), (32, 1000, 1928, 0), (5, 16400, 264, 0), (16, 16385, 1032, 8), (8, 20000, 136, 0)])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_middle_sizes_of_whole_pieces(layers, dtype, m, n, k, pad):
+    # with and without splits of the depth, and few rows next to many columns
+    t = TYPES[dtype]
+    x, w, bias, r = wide(1, m, k, t, pad), wide(2, n, k, t, pad, k ** -0.5), wide(3, 1, n, t)[0], wide(4, m, n, t, pad)
+    y, c = layers.linear(x, w, bias, activation="relu", residual=r, checkpoint=True)
+    z = x.double() @ w.double().t().contiguous() + bias.double()
+    want = ref.act(z, "relu") + r.double()
+    dz = ref.product_bound(x.double(), w.double(), k) + 4 * ref.EPS * z.abs()
+    assert bool(((y.double() - want).abs() <= 1.01 * dz + (4 * ref.EPS + ref.ROUND[t]) * want.abs() + ref.TINY[t]).all())
+    assert ref.rel(y, want) <= 1.5 * ref.norm_bound(k, t)
+    codes, exps = ref.unpack(c.buffer, m, n)
+    unit = torch.from_numpy(np.repeat(np.exp2(exps.astype(np.float64) - 127), 32, axis=1)[:, :n])
+    got = torch.from_numpy(ref.decode(codes, exps, n))
+    assert bool(((got - z.cpu()).abs() <= unit * torch.where(got.abs() == 127 * unit, 1.0, 0.5) + dz.cpu()).all()) and not codes[:, n:].any()
+    if n % 8 == 0:
+        g, v = wide(5, m, k, t, pad), wide(6, k, n, t, pad, k ** -0.5)
+        want = g.double() @ v.double() + r.double()
+        dx = layers.linear_input_grad(g, v, residual=r)
+        near = 1.01 * ref.product_bound(g.double(), v.double().t().contiguous(), k) + (4 * ref.EPS + ref.ROUND[t]) * want.abs() + ref.TINY[t]
+        assert bool(((dx.double() - want).abs() <= near).all())
+
+
+@pytest.mark.parametrize("rows,n,k,pad", [(4100, 264, 260, 0), (40, 2600, 2600, 8), (1032, 520, 513, 0)])
+def test_middle_sizes_of_weight_grad(layers, rows, n, k, pad):
+    dy = wide(1, rows, n, torch.bfloat16, pad)
+    c = layers.save_checkpoint(wide(2, rows, k, torch.bfloat16, 0, 10.0))
+    X, Y = c.restore(torch.float32).double(), dy.double()
+    dw, db = layers.linear_weight_grad(dy, c, bias=True)
+    want, want_b = Y.t().contiguous() @ X, Y.sum(0)
+    near = ref.product_bound(Y.t().contiguous(), X.t().contiguous(), rows) + 2.0 ** -24 * want.abs()
+    assert bool(((dw.double() - want).abs() <= near).all()) and ref.rel(dw, want) <= ref.norm_bound(rows, torch.float32)
+    assert bool(((db.double() - want_b).abs() <= (rows + 8) * 2.0 ** -23 * Y.abs().sum(0)).all())
+
+
+@pytest.mark.parametrize("m,depth,n,pad", [(129, 4, 260, 0), (300, 36, 516, 4), (1000, 1000, 1284, 0), (2100, 100, 2052, 12), (129, 3200, 1000, 0), (9000, 12, 4004, 4)])
 def test_large_fp32_products(layers, m, depth, n, pad):
     # rows of whole 16-byte pieces: depths around the kernel's steps of 32, tiles that end inside the result, one and several splits
     x, w, bias, r = wide(1, m, depth, torch.float32, pad), wide(2, n, depth, torch.float32, pad, depth ** -0.5), wide(3, 1, n, torch.float32)[0], wide(4, m, n, torch.float32, pad)
