@@ -10,6 +10,15 @@
 //   barriers           one in 64 deep, between the last reads of two tiles and their last products
 // 16-byte pieces of a row are swapped on the way into the LDS (each lane fetches the piece that belongs to its place).  A checkpoint's codes cannot go
 // straight into the LDS: they are read into registers 64 deep ahead, turned into bf16 numbers and stored while the products run.
+//
+// Where 256 x 256 would leave CUs idle, tiles of 128 x 128 with waves of 64 x 64, two workgroups to a CU.
+//
+// Bound by the card's power: bf16, 8192 x 16384 with 4096 products each takes 806 to 845 us without an end (1300 to 1365 TFLOP/s; a matrix product alone 726 to
+// 808), the matrix cores are busy 86% of the cycles at 1.5 GHz, and the clock falls where they are busier.  Bias, gelu, residual and checkpoint, 0.4 GB to be
+// written, add 140 to 170 us that the one workgroup of a CU has nothing to hide behind.  Input gradient of these sizes with gelu's slope 970, weight gradient
+// 4096 x 8192 from a checkpoint, 8192 deep, 480 (1140 TFLOP/s; decoding takes the vector unit).  Tiles of 128: 1021 x 5000, 2048 deep, fp16 33 us (640 TFLOP/s).
+// Not faster: nine tiles in the LDS in place of five for tiles of 128 (four steps ahead; a CU's loads bound them, 0.4 to 0.5 us for 64 deep), a second set of
+// registers for the codes, tiles of 256 x 128, loads 32 deep (half a line each: twice the requests).
 #include "eden_layers_fetch.h"
 
 namespace eden_layers {

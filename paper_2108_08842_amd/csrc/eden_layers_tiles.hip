@@ -10,6 +10,10 @@
 // input gradient), which the transposing reads of the LDS turn by the way.  16-byte pieces of a row are swapped so that neither kind of
 // read meets its own bank.  The operand of the columns goes first into the products, so that a lane ends up with one row and runs of four
 // columns of the result: the end of the product works on vectors, and a checkpoint's block of 32 columns is 16 values in each of two lanes.
+//
+// Takes what the kernels with loads straight into the LDS do not: rows that begin anywhere, small products, fp32 and fp16 next to a checkpoint.  Bound by the way
+// through the registers: a step's loads are as far ahead as its registers reach, and its vector instructions (terms) stand between products.  Weight gradient of
+// 4096 x 4096, 4096 deep: fp16 417 us (329 TFLOP/s, twice that in terms), fp32 460 us; 555 x 1001, 1024 deep, fp32: 16 us and 4.5 for the join, most of it waiting.
 #include "eden_layers_product.h"
 
 namespace eden_layers {
