@@ -56,7 +56,8 @@ int eden_checkpoint_restore(const void *checkpoint, uint64_t rows, uint64_t cols
  * fp32 additions, so results may differ in their last bits from those with another workspace size.  16-byte aligned; what it
  * holds before or after a call does not matter.
  *   rows x cols   size of the result;  depth   length of the sums
- * (eden_linear: m, n, k;  eden_linear_weight_grad: n, k, m;  eden_linear_input_grad: m, k, n). */
+ * (eden_linear: m, n, k;  eden_linear_weight_grad: n, k, m;  eden_linear_input_grad: m, k, n).
+ * eden_linear of up to 4 rows, in fp32 up to 16, uses none. */
 size_t eden_layers_workspace_bytes(uint64_t rows, uint64_t cols, uint64_t depth, uint32_t dtype);
 
 /* The same and, for large products, room for copies of both operands: a call whose operands' rows do not all start at multiples of

@@ -100,13 +100,15 @@ def _same(t, like, what):
 
 
 def _output(out, shape, like, what, dtype=None):
-    """`out`, or a new tensor of that shape of like's type (or `dtype`) on its device."""
+    """(tensor, address, distance between rows) of `out`, or of a new tensor of that shape of like's type (or `dtype`) on its device."""
     if out is None:
-        return like.new_empty(shape) if dtype is None else torch.empty(shape, dtype=dtype, device=like.device)
+        out = like.new_empty(shape) if dtype is None else like.new_empty(shape, dtype=dtype)
+        return out, out.data_ptr(), shape[-1]
     dtype = dtype or like.dtype
     if tuple(out.shape) != tuple(shape) or out.dtype is not dtype or out.device != like.device:
         _refuse(f"{what}: {tuple(out.shape)} of {out.dtype} on {out.device}, expected {tuple(shape)} of {dtype} on {like.device}")
-    return out
+    address, ld, _, _ = _rows(out, what)
+    return out, address, ld
 
 
 def _act(name, what):
@@ -251,13 +253,14 @@ def linear(x, w, bias=None, activation: str = "none", residual=None, checkpoint=
         if residual.shape != shape:
             _refuse(f"linear: residual is {tuple(residual.shape)}, expected {tuple(shape)}")
         rp, ldr, _, _ = _rows(residual, "linear: residual")
-    y = _output(out, shape, x, "linear: out")
-    yp, ldy, _, _ = _rows(y, "linear: out")
+    y, yp, ldy = _output(out, shape, x, "linear: out")
     c, cp, capacity = None, None, 0
     if checkpoint is not False and checkpoint is not None:
         c = _new_checkpoint(None if checkpoint is True else checkpoint, m, n, device)
         cp, capacity = c.buffer.data_ptr(), c.buffer.numel()
-    ws, wsp, size = _workspace(L, m, n, k, dtype, device, xp | wp, ldx | ldw | k)
+    ws, wsp, size = None, None, 0
+    if m > 16 or (m > 4 and dtype != F32):                         # fewer rows use none
+        ws, wsp, size = _workspace(L, m, n, k, dtype, device, xp | wp, ldx | ldw | k)
     _check(L.eden_linear(xp, ldx, wp, ldw, bp, rp, ldr, yp, ldy, cp, capacity, m, n, k, dtype, act, wsp, size, _stream(device)), "eden_linear")
     return y if c is None else (y, c)
 
@@ -276,14 +279,10 @@ def linear_weight_grad(dy, saved: Checkpoint, bias: bool = False, out=None, bias
     sp = _saved(saved, m, k, device, "linear_weight_grad")
     if accumulate and (out is None or (bias and bias_out is None)):
         _refuse("linear_weight_grad: nothing to accumulate in")
-    dw = _output(out, (n, k), dy, "linear_weight_grad: out", torch.float32)
-    wp, ldw, _, _ = _rows(dw, "linear_weight_grad: out")
+    dw, wp, ldw = _output(out, (n, k), dy, "linear_weight_grad: out", torch.float32)
     db, bp = None, None
     if bias or bias_out is not None:
-        db = _output(bias_out, (n,), dy, "linear_weight_grad: bias_out", torch.float32)
-        if n > 1 and db.stride(0) != 1:
-            _refuse("linear_weight_grad: bias_out's elements must be neighbours")
-        bp = db.data_ptr()
+        db, bp, _ = _output(bias_out, (n,), dy, "linear_weight_grad: bias_out", torch.float32)
     ws, wsp, size = _workspace(L, n, k, m, dtype, device, dp, ldy | n) if dtype == BF16 else _workspace(L, n, k, m, dtype, device, 0, 0)
     _check(L.eden_linear_weight_grad(dp, ldy, sp, wp, ldw, bp, m, n, k, dtype, 1 if accumulate else 0, wsp, size, _stream(device)), "eden_linear_weight_grad")
     return dw if db is None else (dw, db)
@@ -313,8 +312,7 @@ def linear_input_grad(dz, w, activation: str = "none", checkpoint: Checkpoint = 
         if residual.shape != shape:
             _refuse(f"linear_input_grad: residual is {tuple(residual.shape)}, expected {tuple(shape)}")
         rp, ldr, _, _ = _rows(residual, "linear_input_grad: residual")
-    dx = _output(out, shape, dz, "linear_input_grad: out")
-    xp, ldx, _, _ = _rows(dx, "linear_input_grad: out")
+    dx, xp, ldx = _output(out, shape, dz, "linear_input_grad: out")
     ws, wsp, size = _workspace(L, m, k, n, dtype, device, dp | wp, ldz | ldw | n | k)
     _check(L.eden_linear_input_grad(dp, ldz, wp, ldw, sp, act, rp, ldr, xp, ldx, m, n, k, dtype, wsp, size, _stream(device)), "eden_linear_input_grad")
     return dx
@@ -330,7 +328,6 @@ def activation_grad(dy, saved: Checkpoint, activation: str, out=None, stream=Non
     act = _act(activation, "activation_grad")
     dp, ldy, rows, cols = _rows(dy, "activation_grad: dy")
     sp = _saved(saved, rows, cols, device, "activation_grad")
-    dz = _output(out, dy.shape, dy, "activation_grad: out")
-    zp, ldz, _, _ = _rows(dz, "activation_grad: out")
+    dz, zp, ldz = _output(out, dy.shape, dy, "activation_grad: out")
     _check((_lib or lib()).eden_activation_grad(dp, ldy, sp, act, zp, ldz, rows, cols, dtype, _stream(device)), "eden_activation_grad")
     return dz
