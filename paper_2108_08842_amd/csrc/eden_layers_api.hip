@@ -56,10 +56,11 @@ Shape direct_shape(uint64_t rows, uint64_t cols, uint64_t depth) {
     return {128, rows <= 128 ? std::max(splits, splits_of(small, depth, 512, 1024)) : splits};
 }
 // Through registers: 128 x 128 where those fill the device (fp16 weight gradient 2048 x 4096, 1024 deep: 60 us against 75 with 64 x 64), else 64 x 64, three or more to
-// a CU (512 x 1001 x 1003 bf16: 21 against 24).
-Shape tiles_shape(uint64_t rows, uint64_t cols, uint64_t depth) {
+// a CU.  `slots`: as many workgroups as split a sum together: 512 where each product has one term (512 x 1001 x 1003 bf16: 17 us against 21 with 1024), else 1024
+// (fp16 weight gradient 568 x 696, 2624 deep: 25 against 27.5 with 512).
+Shape tiles_shape(uint64_t rows, uint64_t cols, uint64_t depth, uint64_t slots) {
     if (tile_count(rows, cols, 128) >= 256) return {128, 1};
-    return {64, splits_of(tile_count(rows, cols, 64), depth, 1024, 96)};
+    return {64, splits_of(tile_count(rows, cols, 64), depth, slots, 96)};
 }
 
 // fp32 operands straight into the LDS: 128 x 128, two to a CU.
@@ -135,7 +136,7 @@ int run(Op op, uint32_t dtype, Product &p, void *workspace, size_t workspace_byt
         }
         if (e != hipSuccess) return EDEN_ERR_HIP;
     }
-    const Shape shape = !direct ? tiles_shape(p.rows, p.cols, p.depth) : dtype == EDEN_F32 ? fp32_shape(p.rows, p.cols, p.depth) : direct_shape(p.rows, p.cols, p.depth);
+    const Shape shape = !direct ? tiles_shape(p.rows, p.cols, p.depth, op == kWeightGrad || dtype == EDEN_F32 ? 1024 : 512) : dtype == EDEN_F32 ? fp32_shape(p.rows, p.cols, p.depth) : direct_shape(p.rows, p.cols, p.depth);
     if (tile_count(p.rows, p.cols, shape.side) > kMostGroups / 64) return EDEN_ERR_INVALID_ARG;
     uint64_t splits = shape.splits;
     while (splits > 1 && partial_bytes(p.rows, p.cols, splits) > workspace_bytes) --splits;
@@ -179,7 +180,7 @@ int eden_checkpoint_restore(const void *checkpoint, uint64_t rows, uint64_t cols
 size_t eden_layers_workspace_bytes(uint64_t rows, uint64_t cols, uint64_t depth, uint32_t dtype) {
     if (!known_type(dtype) || rows > kMostSize || cols > kMostSize || depth > kMostSize) return 0;
     if (rows == 0 || cols == 0) return 0;
-    const uint64_t splits = std::max(dtype == EDEN_F32 ? fp32_shape(rows, cols, depth).splits : direct_shape(rows, cols, depth).splits, tiles_shape(rows, cols, depth).splits);
+    const uint64_t splits = std::max(dtype == EDEN_F32 ? fp32_shape(rows, cols, depth).splits : direct_shape(rows, cols, depth).splits, tiles_shape(rows, cols, depth, 1024).splits);
     return splits > 1 ? partial_bytes(rows, cols, splits) : 0;
 }
 
