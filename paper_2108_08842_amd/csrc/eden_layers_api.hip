@@ -94,8 +94,8 @@ bool many_columns(uint32_t dtype, const Product &p, uint64_t room) {
            partial_bytes(p.rows, p.cols, direct_shape(p.rows, p.cols, p.depth).splits) <= room;
 }
 
-// Copies cost two passes over an operand and are worth it from about 2^30 products on in 2 bytes (1021 x 1001 x 2047: 34 -> 27.5 us; 200 x 4001 x 1001 would take 27 in
-// place of 21), from 2^29 in fp32 (1235 x 7079 x 2681: 679 -> 360 us, 301 x 2001 x 1001: 60 -> 34, 831 x 831 x 831: 34 -> 31, 777 x 777 x 777: no difference).
+// Copies cost two passes over an operand and are worth it from about 2^30 products on in 2 bytes (1501 x 1501 x 1501: 40 -> 31 us, 1021 x 1001 x 2047: 31 -> 27; 801 x 1001 x
+// 1335: no difference), from 2^29 in fp32 (1235 x 7079 x 2681: 513 -> 361 us, 301 x 2001 x 1001: 54 -> 34, 831 x 831 x 831: 33 -> 31).
 uint64_t copy_bytes(uint64_t a, uint64_t b, uint32_t dtype) { return (a + 63) / 64 * 64 * ((b + 63) / 64 * 64) * bytes_of(dtype); }
 bool worth_copies(uint64_t rows, uint64_t cols, uint64_t depth, uint32_t dtype) {
     const uint64_t most = 1u << 21, least = dtype == EDEN_F32 ? 1u << 29 : 1u << 30;
