@@ -95,11 +95,12 @@ bool many_columns(uint32_t dtype, const Product &p, uint64_t room) {
 }
 
 // Copies cost two passes over an operand and are worth it from about 2^30 products on in 2 bytes (1501 x 1501 x 1501: 40 -> 31 us, 1021 x 1001 x 2047: 31 -> 27; 801 x 1001 x
-// 1335: no difference), from 2^29 in fp32 (1235 x 7079 x 2681: 513 -> 361 us, 301 x 2001 x 1001: 54 -> 34, 831 x 831 x 831: 33 -> 31).
+// 1335: no difference), from 2^29 in fp32 (1235 x 7079 x 2681: 513 -> 361 us, 301 x 2001 x 1001: 54 -> 34, 831 x 831 x 831: 33 -> 31), but not for a
+// narrow result (fp32, 2318 x 192 x 3081: 52 us in place of 43).
 uint64_t copy_bytes(uint64_t a, uint64_t b, uint32_t dtype) { return (a + 63) / 64 * 64 * ((b + 63) / 64 * 64) * bytes_of(dtype); }
 bool worth_copies(uint64_t rows, uint64_t cols, uint64_t depth, uint32_t dtype) {
     const uint64_t most = 1u << 21, least = dtype == EDEN_F32 ? 1u << 29 : 1u << 30;
-    return rows > kFewRows && rows < most && cols < most && depth < most && rows * cols >= least / std::max<uint64_t>(depth, 1);
+    return rows >= 256 && cols >= 256 && rows < most && cols < most && depth < most && rows * cols >= least / std::max<uint64_t>(depth, 1);
 }
 // Replaces an operand by a copy in the workspace.
 hipError_t copy_operand(uint32_t dtype, const void *&operand, size_t &ld, uint32_t rows, uint32_t cols, uint8_t *&workspace, size_t &room, hipStream_t st) {
