@@ -250,10 +250,15 @@ template <uint32_t DTYPE, int EACH> void launch_dots(const Product &p, hipStream
         const uint32_t part = pieces < part_of<ROWS>() ? pieces : part_of<ROWS>();
         k_dots<DTYPE, EACH, ROWS><<<grid, kWaves * 64, ROWS * (part * 16 + kWaves * EACH * sizeof(float)), st>>>(p);
     };
-    if (p.rows == 1) with_rows(std::integral_constant<int, 1>());
-    else if (p.rows == 2) with_rows(std::integral_constant<int, 2>());
-    else if (DTYPE != EDEN_F32 || p.rows <= 4) with_rows(std::integral_constant<int, 4>());
-    else if constexpr (DTYPE == EDEN_F32) with_rows(std::integral_constant<int, 8>());
+    constexpr bool kFull = DTYPE == EDEN_F32;
+    if constexpr (EACH != 2) {                                     // (two rows of w are for more rows of x)
+        if (p.rows == 1) return with_rows(std::integral_constant<int, 1>());
+    }
+    if constexpr (EACH != 2 || !kFull) {
+        if (p.rows <= 2) return with_rows(std::integral_constant<int, 2>());
+    }
+    if (!kFull || p.rows <= 4) with_rows(std::integral_constant<int, 4>());
+    else if constexpr (kFull) with_rows(std::integral_constant<int, 8>());
 }
 template <uint32_t DTYPE> hipError_t launch_type(const Product &p, hipStream_t st) {
     // k_dots in us, w of 16384 x 4096: 4 rows of bf16 28.5 (k_rows 34), 5 rows 40 (35); fp32, 8 rows 67 (72) and at 1024 x 1024 5.9 (6.3).

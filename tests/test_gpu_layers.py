@@ -389,6 +389,19 @@ def test_middle_sizes_of_whole_pieces(layers, dtype, m, n, k, pad):
         assert bool(((dx.double() - want).abs() <= near).all())
 
 
+@pytest.mark.parametrize("m", [1, 2, 3, 4, 7, 11])
+@pytest.mark.parametrize("n,k,pad", [(8195, 1101, 3), (8192, 1160, 0), (16390, 1100, 0), (516, 3000, 5)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_few_rows_next_to_many_columns(layers, dtype, n, k, pad, m):
+    t = TYPES[dtype]
+    x, w, bias, r = wide(1, m, k, t, pad), wide(2, n, k, t, pad, k ** -0.5), wide(3, 1, n, t)[0], wide(4, m, n, t, pad)
+    y = layers.linear(x, w, bias, activation="relu", residual=r)
+    z = x.double() @ w.double().t().contiguous() + bias.double()
+    want = ref.act(z, "relu") + r.double()
+    near = 1.01 * ref.product_bound(x.double(), w.double(), k) + 4 * ref.EPS * z.abs() + (4 * ref.EPS + ref.ROUND[t]) * want.abs() + ref.TINY[t]
+    assert bool(((y.double() - want).abs() <= near).all())
+
+
 @pytest.mark.parametrize("rows,n,k,pad", [(4100, 264, 260, 0), (40, 2600, 2600, 8), (1032, 520, 513, 0)])
 def test_middle_sizes_of_weight_grad(layers, rows, n, k, pad):
     dy = wide(1, rows, n, torch.bfloat16, pad)
