@@ -139,7 +139,7 @@ int run(Op op, uint32_t dtype, Product &p, void *workspace, size_t workspace_byt
     }
     const Shape shape = !direct ? tiles_shape(p.rows, p.cols, p.depth, op == kWeightGrad || dtype == EDEN_F32 ? 1024 : 512) : dtype == EDEN_F32 ? fp32_shape(p.rows, p.cols, p.depth) : direct_shape(p.rows, p.cols, p.depth);
     if (tile_count(p.rows, p.cols, shape.side) > kMostGroups / 64) return EDEN_ERR_INVALID_ARG;
-    uint64_t splits = shape.splits;
+    uint64_t splits = p.cols ? shape.splits : 1;                   // (row sums alone have no columns at which a join would find them)
     while (splits > 1 && partial_bytes(p.rows, p.cols, splits) > workspace_bytes) --splits;
     const uint64_t each = ((p.depth + splits - 1) / splits + kSplitUnit - 1) / kSplitUnit * kSplitUnit;
     splits = each ? (p.depth + each - 1) / each : 1;
