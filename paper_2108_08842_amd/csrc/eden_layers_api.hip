@@ -20,6 +20,9 @@ bool matrix_ok(const void *p, uint64_t ld, uint64_t rows, uint64_t cols, size_t 
     if (rows == 0 || cols == 0) return true;
     return p != nullptr && reinterpret_cast<uintptr_t>(p) % element == 0 && (rows == 1 || (ld >= cols && ld <= (1ull << 40)));
 }
+// The distance between rows of an operand as the kernels take it.  That of a single row may be anything, but loads of whole tiles count on a second row's place, which has to be
+// read as zeros, lying behind the first row's end: it becomes the row's length in whole pieces.
+uint64_t distance(uint64_t ld, uint64_t rows, uint64_t cols) { return rows > 1 ? ld : (cols + 7) / 8 * 8; }
 bool checkpoint_ok(const void *p, uint64_t rows, uint64_t cols) {
     return rows == 0 || cols == 0 || (p != nullptr && reinterpret_cast<uintptr_t>(p) % 16 == 0);
 }
@@ -203,7 +206,7 @@ int eden_linear(const void *x, uint64_t ldx, const void *w, uint64_t ldw, const 
     if (z_checkpoint && z_capacity < eden_checkpoint_bytes(m, n)) return EDEN_ERR_CAPACITY;
     if (m == 0 || n == 0) return EDEN_OK;
     Product p = {};
-    p.a = x, p.lda = ldx, p.b = w, p.ldb = ldw;
+    p.a = x, p.lda = distance(ldx, m, k), p.b = w, p.ldb = distance(ldw, n, k);
     p.rows = (uint32_t)m, p.cols = (uint32_t)n, p.depth = (uint32_t)k;
     p.finish.bias = bias, p.finish.residual = residual, p.finish.ld_residual = ldr, p.finish.out = y, p.finish.ld_out = ldy;
     p.finish.activation = activation, p.finish.blocks = (uint32_t)blocks_of(n);
@@ -221,7 +224,7 @@ int eden_linear_weight_grad(const void *dy, uint64_t ldy, const void *x_checkpoi
     if (bias_grad && !matrix_ok(bias_grad, n, 1, n, 4)) return EDEN_ERR_INVALID_ARG;
     if (n == 0 || (k == 0 && !bias_grad)) return EDEN_OK;
     Product p = {};
-    p.a = dy, p.lda = ldy, p.b = x_checkpoint, p.ldb = blocks_of(k) * kBlock;
+    p.a = dy, p.lda = distance(ldy, m, n), p.b = x_checkpoint, p.ldb = blocks_of(k) * kBlock;
     p.b_blocks = (uint32_t)blocks_of(k);
     p.b_exps = static_cast<const uint8_t *>(x_checkpoint) + codes_bytes(m, k);
     p.rows = (uint32_t)n, p.cols = (uint32_t)k, p.depth = (uint32_t)m;
@@ -241,7 +244,7 @@ int eden_linear_input_grad(const void *dz, uint64_t ldz, const void *w, uint64_t
     if (slopes ? !checkpoint_ok(z_checkpoint, m, k) : z_checkpoint != nullptr) return EDEN_ERR_INVALID_ARG;
     if (m == 0 || k == 0) return EDEN_OK;
     Product p = {};
-    p.a = dz, p.lda = ldz, p.b = w, p.ldb = ldw;
+    p.a = dz, p.lda = distance(ldz, m, n), p.b = w, p.ldb = distance(ldw, n, k);
     p.rows = (uint32_t)m, p.cols = (uint32_t)k, p.depth = (uint32_t)n;
     p.finish.residual = residual, p.finish.ld_residual = ldr, p.finish.out = dx, p.finish.ld_out = ldx;
     p.finish.activation = activation, p.finish.blocks = (uint32_t)blocks_of(k);
