@@ -17,9 +17,9 @@
  * residual itself and eden_activation_grad's dz may be dy itself (same pointer, same distance).
  *
  * Sums are held in fp32 and results rounded once, to nearest even.  The products of fp16 and bf16 operands are exact.  fp32
- * operands are taken as three bf16 terms (exact); in eden_linear and eden_linear_input_grad, where both operands are fp32,
- * products of terms below 2^-24 of the whole product are left out, and an infinity among the operands gives NaN
- * in the results it reaches.  (A call with at most 16 rows in eden_linear multiplies in fp32 and has no such exception.)
+ * operands are taken as three bf16 terms (exact down to 2^-133); in eden_linear and eden_linear_input_grad, where both operands are fp32,
+ * the smallest products of terms are left out, less than 2^-22 of the whole product and of either sign, and an infinity among
+ * the operands gives NaN in the results it reaches.  (A call with at most 16 rows in eden_linear multiplies in fp32 and has no such exception.)
  *
  * Checkpoint of an m x c matrix: blocks of 32 consecutive columns of a row, the last one filled up with zeros.  A block has an
  * exponent byte t and 32 codes q of -127 .. 127, which stand for q 2^(t - 127).  t = max(1, e - 6), e = exponent field of the fp32

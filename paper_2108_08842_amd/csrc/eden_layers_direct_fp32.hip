@@ -1,7 +1,7 @@
 // Matrix products of two fp32 operands whose rows are whole 16-byte pieces (eden_linear, eden_linear_input_grad).
 //
-// out[r][c] = sum_d A(r, d) B(c, d) as products of bf16 terms: x = h + m + l, each the upper 16 bits of what the ones before leave (exact), and the six products
-// down to 2^-16 of the first.  The matrix cores do that at 2500 / 6 TFLOP/s at most; their own fp32 products end at 157.
+// out[r][c] = sum_d A(r, d) B(c, d) as products of bf16 terms: x = h + m + l, h the upper 16 bits, m and l the nearest bf16 numbers to what the ones before leave
+// (exact), and the six products down to 2^-16 of the first; the others are below 2^-22 together.  The matrix cores do that at 2500 / 6 TFLOP/s at most; their own fp32 products end at 157.
 //
 // A workgroup has a tile of 128 x 128, two to a CU, a wave 64 x 64.  Operands' tiles are 32 deep (128-byte lines) and go straight into the LDS as fp32; the LDS
 // holds five, in turns as in the kernel for two-byte types: the two in use, the next two, the first of the two after that.  A wave reads the
@@ -97,15 +97,11 @@ template <bool STRIDED> struct Reader {
     }
 };
 
-// Elements 2 q and 2 q + 1 as three terms each (of an infinity the others are NaN).
+// Elements 2 q and 2 q + 1 as three terms each.
 __device__ inline void take_apart(const Raw &r, int q, u32x4 (&terms)[3]) {
     float a = r.v[2 * q], b = r.v[2 * q + 1];
 #pragma unroll
-    for (int t = 0; t < 3; ++t) {
-        terms[t][q] = upper_halves(a, b);
-        a -= __uint_as_float(__float_as_uint(a) & 0xFFFF0000u);
-        b -= __uint_as_float(__float_as_uint(b) & 0xFFFF0000u);
-    }
+    for (int t = 0; t < 3; ++t) terms[t][q] = take_nearest(a, b, t == 0);
 }
 
 template <int OP> __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_direct_fp32(const Product p) {

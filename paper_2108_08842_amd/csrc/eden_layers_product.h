@@ -16,7 +16,7 @@ template <int WIDTH> __device__ inline int piece_of_depth(int depth, int piece) 
     return depth * (WIDTH * 2) + ((WIDTH == 64 ? piece ^ (2 * (depth & 2)) : piece ^ (4 * (depth & 3))) << 4);
 }
 
-// x = term + rest, term = the upper 16 bits (exact; an infinity leaves nothing, a NaN a NaN)
+// Next to an operand of one term, where all products are taken: x = term + rest, term = the upper 16 bits (exact; an infinity leaves nothing, a NaN a NaN)
 __device__ inline float take_term(float &x) {
     const float term = __uint_as_float(__float_as_uint(x) & 0xFFFF0000u);
     const float rest = x - term;
@@ -24,6 +24,18 @@ __device__ inline float take_term(float &x) {
     return term;
 }
 __device__ inline uint32_t upper_halves(float lo, float hi) { return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u); }
+
+// Between two fp32 operands, where the products of second and third terms are left out: the next term of a and of b, side by side, and what they leave.  `first`: the
+// upper 16 bits (a number that rounds to an infinity keeps its size; of an infinity the other terms are NaN).  The others are the nearest bf16 numbers, so that the
+// third ones are at most 2^-16 of the power of two below |a| and of either sign: what is left out of a product is below 2^-22 of it, 2^-25.4 in the mean square (an
+// fp32 rounding: 2^-25.2).  All terms cut off: up to 2^-21.03, always towards zero.  The first one to the nearest as well: below 2^-24, but with the numbers next to fp32's largest
+// taken care of 4096 x 8192 x 4096 takes 6.4% longer.
+__device__ inline uint32_t take_nearest(float &a, float &b, bool first) {
+    const uint32_t pair = first ? upper_halves(a, b) : __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2));
+    a -= __uint_as_float(pair << 16);
+    b -= __uint_as_float(pair & 0xFFFF0000u);
+    return pair;
+}
 
 __device__ inline u32x4 code_values(uint32_t c0, uint32_t c1, float unit) {
     float a[4], b[4];

@@ -4,7 +4,7 @@
 // A workgroup of four waves has a tile of 128 x 128, a wave 64 x 64 of it; where such tiles would leave most of the device idle and each step
 // of a few workgroups would be waited for, 64 x 64 and 32 x 32.  Operands go through registers into the LDS, where
 // those that the matrix cores cannot take are turned into bf16 terms that add up to them exactly:
-//   fp32                three terms of 8 bits; fp16 next to a checkpoint: two.  With three on both sides the products below 2^-24 are left out.
+//   fp32                three terms of 8 bits; fp16 next to a checkpoint: two.  With three on both sides the smallest products are left out, below 2^-22 together.
 //   8-bit checkpoint    q 2^(t - 127) itself: seven bits.
 // The LDS holds an operand as memory does: rows of the depth (x, w, dz), or rows of columns at one depth (dy, checkpoints, w in the
 // input gradient), which the transposing reads of the LDS turn by the way.  16-byte pieces of a row are swapped so that neither kind of
@@ -25,6 +25,7 @@ constexpr int kThreads = 256;
 template <int OP, uint32_t DTYPE, int W> struct Plan {
     static constexpr int kTermsA = DTYPE == EDEN_F32 ? 3 : (OP == kWeightGrad && DTYPE == EDEN_F16) ? 2 : 1;
     static constexpr int kTermsB = OP == kWeightGrad ? 1 : DTYPE == EDEN_F32 ? 3 : 1;
+    static constexpr bool kNearest = kTermsB > 1;                              // not all products of terms are taken
     static constexpr bool kHalf = DTYPE == EDEN_F16 && OP != kWeightGrad;      // fp16 products
     static constexpr bool kStridedA = OP == kWeightGrad, kStridedB = OP != kForward;
     static constexpr int kSide = 64 * W;
@@ -64,7 +65,7 @@ template <class T> __device__ inline void select_near(Vec<T, 8> &v, const T *at,
     }
 }
 
-template <uint32_t DTYPE, int TERMS> __device__ inline void store_piece(char *lds, int plane, const Piece<DTYPE> &p) {
+template <uint32_t DTYPE, int TERMS, bool NEAREST> __device__ inline void store_piece(char *lds, int plane, const Piece<DTYPE> &p) {
     if constexpr (TERMS == 1) {
         static_assert(sizeof(p) == 16, "");
         __builtin_memcpy(__builtin_assume_aligned(lds, 16), &p, 16);
@@ -77,8 +78,12 @@ template <uint32_t DTYPE, int TERMS> __device__ inline void store_piece(char *ld
             u32x4 w;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float a = take_term(x[2 * i]), b = take_term(x[2 * i + 1]);
-                w[i] = upper_halves(a, b);
+                if constexpr (NEAREST) {
+                    w[i] = take_nearest(x[2 * i], x[2 * i + 1], t == 0);
+                } else {
+                    const float a = take_term(x[2 * i]), b = take_term(x[2 * i + 1]);
+                    w[i] = upper_halves(a, b);
+                }
             }
             *reinterpret_cast<u32x4 *>(lds + t * plane) = w;
         }
@@ -159,14 +164,14 @@ template <int OP, uint32_t DTYPE, int W> __global__ __launch_bounds__(kThreads, 
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int c = i * kThreads + tid;
-            store_piece<DTYPE, P::kTermsA>(stage + (P::kStridedA ? piece_of_depth<P::kSide>(c / kAcross, c % kAcross) : piece_of_row<D>(c / (D / 8), c % (D / 8))), P::kPlane, from.a[i]);
+            store_piece<DTYPE, P::kTermsA, P::kNearest>(stage + (P::kStridedA ? piece_of_depth<P::kSide>(c / kAcross, c % kAcross) : piece_of_row<D>(c / (D / 8), c % (D / 8))), P::kPlane, from.a[i]);
         }
         char *second = stage + P::kTermsA * P::kPlane;
         if constexpr (OP != kWeightGrad) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const int c = i * kThreads + tid;
-                store_piece<DTYPE, P::kTermsB>(second + (P::kStridedB ? piece_of_depth<P::kSide>(c / kAcross, c % kAcross) : piece_of_row<D>(c / (D / 8), c % (D / 8))), P::kPlane, from.b[i]);
+                store_piece<DTYPE, P::kTermsB, P::kNearest>(second + (P::kStridedB ? piece_of_depth<P::kSide>(c / kAcross, c % kAcross) : piece_of_row<D>(c / (D / 8), c % (D / 8))), P::kPlane, from.b[i]);
             }
         } else {
 #pragma unroll

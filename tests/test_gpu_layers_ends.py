@@ -72,3 +72,41 @@ def test_input_gradient_of_one_feature_at_any_distance(layers):
     assert size and layers.lib().eden_linear_input_grad(dz.data_ptr(), 1, w.data_ptr(), 0, None, 0, None, 0, dx.data_ptr(), k, m, 1, k, layers.BF16, ws.data_ptr(), size,
                                                         stream()) == 0
     assert torch.equal(dx, dz * w)                                 # 16 bits, rounded once
+
+
+# ---- precision
+
+# a launch of k_tiles (few products) and one of the kernel with loads straight into the LDS
+PAIRS = [(40, 72, 3), (2048, 2048, 128)]
+
+
+@pytest.mark.parametrize("m,n,k", PAIRS)
+def test_what_is_left_out_of_fp32_products(layers, m, n, k):
+    """One product in each sum, the other operands zero: what is left out is below 2^-22 of it, and the additions of its parts (the largest last: the others
+    are below 2^-6 of it) are off by 2^-23 of it at most."""
+    g = gen("pairs", m)
+    x, w = torch.zeros(m, k, device="cuda"), torch.zeros(n, k, device="cuda")
+    worst = torch.tensor([1 + 2.0 ** -7 - 2.0 ** -23, 1 + 2.0 ** -8 - 2.0 ** -17, 1 + 2.0 ** -8, 1 + 2.0 ** -7 - 2.0 ** -16, 2 - 2.0 ** -23, 1.0, 1 + 2.0 ** -23], device="cuda")
+    for t, at in ((x, 1), (w, 1)):
+        t[:, at] = torch.rand(t.shape[0], generator=g, device="cuda") + 1.0
+        t[:7, at] = worst
+    want = x[:, 1].double()[:, None] * w[:, 1].double()
+    v = w.t().contiguous()
+    for y in (layers.linear(x, w), layers.linear_input_grad(x, v)):
+        off = (y.double() - want) / want
+        assert float(off.abs().max()) <= 1.5 * 2.0 ** -22
+
+
+@pytest.mark.parametrize("m,n,k", PAIRS)
+def test_largest_fp32_operands(layers, m, n, k):
+    # numbers that round to an infinity in bf16
+    big = torch.finfo(torch.float32).max
+    x, w = torch.zeros(m, k, device="cuda"), torch.zeros(n, k, device="cuda")
+    x[:, 0], w[:, 0] = big, 2.0 ** -20
+    x[1::2, 0] = -big
+    want = x[:, 0].double()[:, None] * w[:, 0].double()
+    for y in (layers.linear(x, w), layers.linear_input_grad(x, w.t().contiguous()), layers.linear(w, x).t()):
+        assert y.shape == want.shape and bool(((y.double() - want).abs() <= 2.0 ** -22 * want.abs()).all())
+    x[0, 0] = float("inf")                                         # gives NaN, and in its own row only
+    y = layers.linear(x, w)
+    assert bool(y[0].isnan().all()) and bool(y[1:].isfinite().all())
