@@ -9,7 +9,7 @@ using namespace eden_layers;
 namespace {
 
 constexpr uint64_t kMostSize = 1ull << 30;
-constexpr uint64_t kMostGroups = 0x7FFFFFFFull;        // workgroups of a launch
+constexpr uint64_t kMostGroups = 0x7FFFFFFFull;        // workgroups of an element-wise call
 
 bool known_type(uint32_t dtype) { return dtype <= EDEN_BF16; }
 size_t bytes_of(uint32_t dtype) { return dtype == EDEN_F32 ? 4 : 2; }
@@ -141,7 +141,7 @@ int run(Op op, uint32_t dtype, Product &p, void *workspace, size_t workspace_byt
         if (e != hipSuccess) return EDEN_ERR_HIP;
     }
     const Shape shape = !direct ? tiles_shape(p.rows, p.cols, p.depth, op == kWeightGrad || dtype == EDEN_F32 ? 1024 : 512) : dtype == EDEN_F32 ? fp32_shape(p.rows, p.cols, p.depth) : direct_shape(p.rows, p.cols, p.depth);
-    if (tile_count(p.rows, p.cols, shape.side) > kMostGroups / 64) return EDEN_ERR_INVALID_ARG;
+    if (tile_count(p.rows, p.cols, shape.side) * shape.splits > most_groups(256)) return EDEN_ERR_INVALID_ARG;      // (one launch; such a result has 2^38 places)
     uint64_t splits = p.cols ? shape.splits : 1;                   // (row sums alone have no columns at which a join would find them)
     while (splits > 1 && partial_bytes(p.rows, p.cols, splits) > workspace_bytes) --splits;
     const uint64_t each = ((p.depth + splits - 1) / splits + kSplitUnit - 1) / kSplitUnit * kSplitUnit;

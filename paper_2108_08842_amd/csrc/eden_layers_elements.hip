@@ -8,6 +8,8 @@
 // 84% of the cycles.  17 x 1000: 2.6 us a launch, whatever it does.
 #include "eden_layers_kernels.h"
 
+#include <algorithm>
+
 namespace eden_layers {
 namespace {
 
@@ -28,17 +30,18 @@ Spread spread(uint32_t rows, uint32_t cols) {
 struct Place {
     uint32_t row, col;
 };
-__device__ inline Place place(uint32_t shift, uint32_t segments) {
-    const uint32_t group = blockIdx.x / segments, segment = blockIdx.x - group * segments;
+// `before`: workgroups of the call's launches before this one
+__device__ inline Place place(uint32_t shift, uint32_t segments, uint32_t before) {
+    const uint32_t number = before + blockIdx.x, group = number / segments, segment = number - group * segments;
     return {group * (kThreads >> shift) + (threadIdx.x >> shift), ((segment << shift) + (threadIdx.x & ((1u << shift) - 1))) * 8};
 }
 __device__ inline int valid_of(uint32_t col, uint32_t cols) { return col < cols ? (int)min(8u, cols - col) : 0; }
 
 template <uint32_t DTYPE>
 __global__ __launch_bounds__(kThreads) void k_save(const typename Elem<DTYPE>::type *x, size_t ldx, uint32_t rows, uint32_t cols, uint32_t blocks,
-                                                   uint8_t *codes, uint8_t *exps, uint32_t shift, uint32_t segments) {
+                                                   uint8_t *codes, uint8_t *exps, uint32_t shift, uint32_t segments, uint32_t before) {
     using T = typename Elem<DTYPE>::type;
-    const Place at = place(shift, segments);
+    const Place at = place(shift, segments, before);
     if (at.row >= rows || at.col >= blocks * kBlock) return;       // four threads of a block leave or stay together
     const auto v = load_some<T, 8>(x + (size_t)at.row * ldx + at.col, valid_of(at.col, cols));
     float lo[4], hi[4];
@@ -66,9 +69,9 @@ __device__ inline void read_values(const uint8_t *codes, const uint8_t *exps, ui
 
 template <uint32_t DTYPE>
 __global__ __launch_bounds__(kThreads) void k_restore(const uint8_t *codes, const uint8_t *exps, uint32_t rows, uint32_t cols, uint32_t blocks,
-                                                      typename Elem<DTYPE>::type *x, size_t ldx, uint32_t shift, uint32_t segments) {
+                                                      typename Elem<DTYPE>::type *x, size_t ldx, uint32_t shift, uint32_t segments, uint32_t before) {
     using T = typename Elem<DTYPE>::type;
-    const Place at = place(shift, segments);
+    const Place at = place(shift, segments, before);
     if (at.row >= rows || at.col >= cols) return;
     float lo[4], hi[4];
     read_values(codes, exps, blocks, at, lo, hi);
@@ -84,10 +87,10 @@ __global__ __launch_bounds__(kThreads) void k_restore(const uint8_t *codes, cons
 template <uint32_t DTYPE>
 __global__ __launch_bounds__(kThreads) void k_activation_grad(const typename Elem<DTYPE>::type *dy, size_t ldy, const uint8_t *codes, const uint8_t *exps,
                                                               uint32_t activation, typename Elem<DTYPE>::type *dz, size_t ldz, uint32_t rows,
-                                                              uint32_t cols, uint32_t blocks, uint32_t shift, uint32_t segments) {
+                                                              uint32_t cols, uint32_t blocks, uint32_t shift, uint32_t segments, uint32_t before) {
     using T = typename Elem<DTYPE>::type;
     constexpr bool FULL = DTYPE == EDEN_F32;
-    const Place at = place(shift, segments);
+    const Place at = place(shift, segments, before);
     if (at.row >= rows || at.col >= cols) return;
     const int valid = valid_of(at.col, cols);
     auto v = load_some<T, 8>(dy + (size_t)at.row * ldy + at.col, valid);
@@ -102,8 +105,8 @@ __global__ __launch_bounds__(kThreads) void k_activation_grad(const typename Ele
 }
 
 template <class T>
-__global__ __launch_bounds__(kThreads) void k_copy_rows(const T *from, size_t ld, uint32_t rows, uint32_t cols, T *to, uint32_t to_ld, uint32_t shift, uint32_t segments) {
-    const Place at = place(shift, segments);
+__global__ __launch_bounds__(kThreads) void k_copy_rows(const T *from, size_t ld, uint32_t rows, uint32_t cols, T *to, uint32_t to_ld, uint32_t shift, uint32_t segments, uint32_t before) {
+    const Place at = place(shift, segments, before);
     if (at.row >= rows || at.col >= to_ld) return;
     Vec<T, 8> v;
     const int valid = valid_of(at.col, cols);
@@ -117,49 +120,64 @@ __global__ __launch_bounds__(kThreads) void k_copy_rows(const T *from, size_t ld
     __builtin_memcpy(__builtin_assume_aligned(to + (size_t)at.row * to_ld + at.col, 16), &v, sizeof(v));
 }
 
-template <class F> hipError_t for_type(uint32_t dtype, F f) {
+template <class F> void for_type(uint32_t dtype, F f) {
     if (dtype == EDEN_F32) f(std::integral_constant<uint32_t, EDEN_F32>());
     else if (dtype == EDEN_F16) f(std::integral_constant<uint32_t, EDEN_F16>());
     else f(std::integral_constant<uint32_t, EDEN_BF16>());
-    return hipGetLastError();
+}
+// f(workgroups before a launch, workgroups of it) until all are launched
+template <class F> hipError_t launches(const Spread &s, F f) {
+    hipError_t e = hipSuccess;
+    for (uint64_t before = 0; before < s.groups && e == hipSuccess; before += most_groups(kThreads)) {
+        f((uint32_t)before, (uint32_t)std::min(s.groups - before, most_groups(kThreads)));
+        e = hipGetLastError();
+    }
+    return e;
 }
 
 }  // namespace
 
 hipError_t launch_save(uint32_t dtype, const void *x, size_t ldx, uint32_t rows, uint32_t cols, uint8_t *codes, uint8_t *exps, hipStream_t st) {
     const Spread s = spread(rows, cols);
-    return for_type(dtype, [&](auto t) {
-        using T = typename Elem<decltype(t)::value>::type;
-        k_save<decltype(t)::value><<<(uint32_t)s.groups, kThreads, 0, st>>>(static_cast<const T *>(x), ldx, rows, cols, (uint32_t)blocks_of(cols), codes, exps,
-                                                                           s.shift, s.segments);
+    return launches(s, [&](uint32_t before, uint32_t groups) {
+        for_type(dtype, [&](auto t) {
+            using T = typename Elem<decltype(t)::value>::type;
+            k_save<decltype(t)::value><<<groups, kThreads, 0, st>>>(static_cast<const T *>(x), ldx, rows, cols, (uint32_t)blocks_of(cols), codes, exps, s.shift, s.segments, before);
+        });
     });
 }
 
 hipError_t launch_copy_rows(uint32_t dtype, const void *from, size_t ld, uint32_t rows, uint32_t cols, void *to, uint32_t to_ld, hipStream_t st) {
     const Spread s = spread(rows, to_ld);
-    if (dtype == EDEN_F32)
-        k_copy_rows<<<(uint32_t)s.groups, kThreads, 0, st>>>(static_cast<const uint32_t *>(from), ld, rows, cols, static_cast<uint32_t *>(to), to_ld, s.shift, s.segments);
-    else k_copy_rows<<<(uint32_t)s.groups, kThreads, 0, st>>>(static_cast<const uint16_t *>(from), ld, rows, cols, static_cast<uint16_t *>(to), to_ld, s.shift, s.segments);
-    return hipGetLastError();
+    return launches(s, [&](uint32_t before, uint32_t groups) {
+        auto copy = [&](auto element) {
+            using T = decltype(element);
+            k_copy_rows<<<groups, kThreads, 0, st>>>(static_cast<const T *>(from), ld, rows, cols, static_cast<T *>(to), to_ld, s.shift, s.segments, before);
+        };
+        if (dtype == EDEN_F32) copy(uint32_t());
+        else copy(uint16_t());
+    });
 }
 
 hipError_t launch_restore(uint32_t dtype, const uint8_t *codes, const uint8_t *exps, uint32_t rows, uint32_t cols, void *x, size_t ldx, hipStream_t st) {
     const Spread s = spread(rows, cols);
-    return for_type(dtype, [&](auto t) {
-        using T = typename Elem<decltype(t)::value>::type;
-        k_restore<decltype(t)::value><<<(uint32_t)s.groups, kThreads, 0, st>>>(codes, exps, rows, cols, (uint32_t)blocks_of(cols), static_cast<T *>(x), ldx,
-                                                                              s.shift, s.segments);
+    return launches(s, [&](uint32_t before, uint32_t groups) {
+        for_type(dtype, [&](auto t) {
+            using T = typename Elem<decltype(t)::value>::type;
+            k_restore<decltype(t)::value><<<groups, kThreads, 0, st>>>(codes, exps, rows, cols, (uint32_t)blocks_of(cols), static_cast<T *>(x), ldx, s.shift, s.segments, before);
+        });
     });
 }
 
 hipError_t launch_activation_grad(uint32_t dtype, const void *dy, size_t ldy, const uint8_t *codes, const uint8_t *exps, uint32_t activation,
                                   void *dz, size_t ldz, uint32_t rows, uint32_t cols, hipStream_t st) {
     const Spread s = spread(rows, cols);
-    return for_type(dtype, [&](auto t) {
-        using T = typename Elem<decltype(t)::value>::type;
-        k_activation_grad<decltype(t)::value><<<(uint32_t)s.groups, kThreads, 0, st>>>(static_cast<const T *>(dy), ldy, codes, exps, activation,
-                                                                                      static_cast<T *>(dz), ldz, rows, cols, (uint32_t)blocks_of(cols), s.shift,
-                                                                                      s.segments);
+    return launches(s, [&](uint32_t before, uint32_t groups) {
+        for_type(dtype, [&](auto t) {
+            using T = typename Elem<decltype(t)::value>::type;
+            k_activation_grad<decltype(t)::value><<<groups, kThreads, 0, st>>>(static_cast<const T *>(dy), ldy, codes, exps, activation, static_cast<T *>(dz), ldz, rows, cols,
+                                                                              (uint32_t)blocks_of(cols), s.shift, s.segments, before);
+        });
     });
 }
 

@@ -22,8 +22,11 @@ struct Product {
     float *partial;                // splits > 1: splits x rows x partial_ld sums, then splits x rows of row_sums
     uint32_t partial_ld;
     uint32_t splits, split_depth;  // of a split, a multiple of kSplitUnit
+    uint32_t before;               // eden_linear of few rows: workgroups of the launches before this one
 };
 
+// Workgroups of a launch: it has less than 2^32 threads.
+constexpr uint64_t most_groups(uint32_t threads) { return 0xFFFFFFFFull / threads; }
 constexpr uint32_t kSplitUnit = 64;   // the depth is split at multiples of this
 // (a result without columns still has row sums: one tile)
 __host__ __device__ inline uint32_t tiles_of(uint32_t n, uint32_t side) { return n ? (n + side - 1) / side : 1; }

@@ -62,7 +62,7 @@ template <uint32_t DTYPE, int COLS> __global__ __launch_bounds__(kWaves * 64) vo
     __shared__ f32x4 sums[kWaves][COLS][64];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const uint32_t col0 = blockIdx.x * (16 * COLS);
+    const uint32_t col0 = (p.before + blockIdx.x) * (16 * COLS);
     const T *w[COLS];
     bool has_w[COLS];
 #pragma unroll
@@ -167,7 +167,7 @@ template <uint32_t DTYPE, int EACH, int ROWS> __global__ __launch_bounds__(kWave
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t pieces = (p.depth + kPiece * 64 - 1) / (kPiece * 64) * 64;                     // a lane has one of every 64
     const uint32_t part = min(pieces, part_of<ROWS>());                                           // of x in the LDS at a time
-    const uint32_t col0 = blockIdx.x * kCols, first = col0 + wave * EACH;
+    const uint32_t col0 = (p.before + blockIdx.x) * kCols, first = col0 + wave * EACH;
     const T *w[EACH];
     bool has[EACH];
 #pragma unroll
@@ -239,16 +239,28 @@ template <uint32_t DTYPE, int EACH, int ROWS> __global__ __launch_bounds__(kWave
     }
 }
 
-template <uint32_t DTYPE, int COLS> void launch(const Product &p, hipStream_t st) {
-    k_rows<DTYPE, COLS><<<(p.cols + 16 * COLS - 1) / (16 * COLS), kWaves * 64, 0, st>>>(p);
+// f(the product, workgroups of a launch) until all `groups` are launched
+template <class F> hipError_t launches(Product p, uint32_t groups, F f) {
+    constexpr uint32_t kMost = (uint32_t)most_groups(kWaves * 64);
+    hipError_t e = hipSuccess;
+    for (p.before = 0; p.before < groups && e == hipSuccess; p.before += kMost) {
+        f(p, groups - p.before < kMost ? groups - p.before : kMost);
+        e = hipGetLastError();
+    }
+    return e;
 }
-template <uint32_t DTYPE, int EACH> void launch_dots(const Product &p, hipStream_t st) {
+template <uint32_t DTYPE, int COLS> hipError_t launch(const Product &p, hipStream_t st) {
+    return launches(p, (p.cols + 16 * COLS - 1) / (16 * COLS), [&](const Product &q, uint32_t groups) { k_rows<DTYPE, COLS><<<groups, kWaves * 64, 0, st>>>(q); });
+}
+template <uint32_t DTYPE, int EACH> hipError_t launch_dots(const Product &p, hipStream_t st) {
     constexpr uint32_t kRun = 1024 / Elem<DTYPE>::kBytes;          // elements of a wave's load
-    const uint32_t grid = (p.cols + kWaves * EACH - 1) / (kWaves * EACH), pieces = (p.depth + kRun - 1) / kRun * 64;
+    const uint32_t all = (p.cols + kWaves * EACH - 1) / (kWaves * EACH), pieces = (p.depth + kRun - 1) / kRun * 64;
     auto with_rows = [&](auto rows) {
         constexpr int ROWS = decltype(rows)::value;
         const uint32_t part = pieces < part_of<ROWS>() ? pieces : part_of<ROWS>();
-        k_dots<DTYPE, EACH, ROWS><<<grid, kWaves * 64, ROWS * (part * 16 + kWaves * EACH * sizeof(float)), st>>>(p);
+        return launches(p, all, [&](const Product &q, uint32_t groups) {
+            k_dots<DTYPE, EACH, ROWS><<<groups, kWaves * 64, ROWS * (part * 16 + kWaves * EACH * sizeof(float)), st>>>(q);
+        });
     };
     constexpr bool kFull = DTYPE == EDEN_F32;
     if constexpr (EACH != 2) {                                     // (two rows of w are for more rows of x)
@@ -257,8 +269,10 @@ template <uint32_t DTYPE, int EACH> void launch_dots(const Product &p, hipStream
     if constexpr (EACH != 2 || !kFull) {
         if (p.rows <= 2) return with_rows(std::integral_constant<int, 2>());
     }
-    if (!kFull || p.rows <= 4) with_rows(std::integral_constant<int, 4>());
-    else if constexpr (kFull) with_rows(std::integral_constant<int, 8>());
+    if constexpr (kFull) {
+        if (p.rows > 4) return with_rows(std::integral_constant<int, 8>());
+    }
+    return with_rows(std::integral_constant<int, 4>());
 }
 template <uint32_t DTYPE> hipError_t launch_type(const Product &p, hipStream_t st) {
     // k_dots in us, w of 16384 x 4096: 4 rows of bf16 28.5 (k_rows 34), 5 rows 40 (35); fp32, 8 rows 67 (72) and at 1024 x 1024 5.9 (6.3).
@@ -268,14 +282,11 @@ template <uint32_t DTYPE> hipError_t launch_type(const Product &p, hipStream_t s
     const bool keeps = p.finish.codes_out != nullptr;
     constexpr bool kFull = DTYPE == EDEN_F32;
     if (p.rows <= (kFull ? 8 : 4)) {
-        if (keeps || (!kFull && p.depth <= 1024)) launch_dots<DTYPE, 4>(p, st);
-        else if (p.cols >= 512 * 16 && p.rows > (kFull ? 2 : 1)) launch_dots<DTYPE, 2>(p, st);
-        else launch_dots<DTYPE, 1>(p, st);
-    } else {
-        if (keeps) launch<DTYPE, 2>(p, st);
-        else launch<DTYPE, 1>(p, st);
+        if (keeps || (!kFull && p.depth <= 1024)) return launch_dots<DTYPE, 4>(p, st);
+        if (p.cols >= 512 * 16 && p.rows > (kFull ? 2 : 1)) return launch_dots<DTYPE, 2>(p, st);
+        return launch_dots<DTYPE, 1>(p, st);
     }
-    return hipGetLastError();
+    return keeps ? launch<DTYPE, 2>(p, st) : launch<DTYPE, 1>(p, st);
 }
 
 }  // namespace

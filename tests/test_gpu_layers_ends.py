@@ -1,10 +1,13 @@
 """The layer operators at the ends of their range, in part through the C entry points themselves."""
 import zlib
 
+import numpy as np
 import pytest
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
+
+from tests import layers_reference as ref                          # noqa: E402
 
 TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
 
@@ -110,3 +113,29 @@ def test_largest_fp32_operands(layers, m, n, k):
     x[0, 0] = float("inf")                                         # gives NaN, and in its own row only
     y = layers.linear(x, w)
     assert bool(y[0].isnan().all()) and bool(y[1:].isfinite().all())
+
+
+# ---- more threads than a launch can have (2^32)
+
+def test_few_rows_next_to_more_columns_than_a_launch_has_threads_for(layers):
+    # whole numbers: exact.  fp32, one row: 64 threads a column; bf16, eight rows of odd length: 32
+    for m, n, k, t in ((1, 2 ** 26 + 44, 8, torch.float32), (8, 2 ** 27 + 20, 7, torch.bfloat16)):
+        g = gen("wide", m)
+        x, w = torch.randint(-3, 4, (m, k), generator=g, device="cuda").to(t), torch.randint(-3, 4, (4099, k), generator=g, device="cuda").to(t)
+        want, w = (x.float() @ w.float().t()).to(t), w.repeat(n // 4099 + 1, 1)[:n]
+        y = layers.linear(x, w)
+        whole = n // 4099 * 4099
+        assert torch.equal(y[:, :whole].reshape(m, -1, 4099), want[:, None].expand(m, whole // 4099, 4099)) and torch.equal(y[:, whole:], want[:, :n - whole])
+        del w, y
+
+
+def test_more_rows_than_a_launch_has_threads_for(layers):
+    # 2^30 rows of one column take four threads each; every value fills its block's seven bits or less
+    rows = 2 ** 30
+    x = (torch.arange(2 ** 20 + 3, device="cuda") % 251 - 125).half().repeat(1024)[:rows].view(rows, 1)
+    c = layers.save_checkpoint(x)
+    assert torch.equal(c.restore(torch.float16), x)
+    codes, exps = ref.encode(x[-100:].float().cpu().numpy())
+    assert np.array_equal(c.buffer[(rows - 100) * 32:rows * 32].cpu().numpy().view(np.int8).reshape(100, 32), codes)
+    assert np.array_equal(c.buffer[rows * 33 - 100:].cpu().numpy().reshape(100, 1), exps)
+    assert torch.equal(layers.activation_grad(x, c, "relu"), x.clamp(min=0.0))
