@@ -115,17 +115,18 @@ constexpr float kTanhCubic = 0.044715f;
 template <bool FULL> __device__ inline float exp_of(float x) { return FULL ? expf(x) : __expf(x); }
 template <bool FULL> __device__ inline float over(float a, float b) { return FULL ? a / b : a * __builtin_amdgcn_rcpf(b); }
 
-// Phi(-|z|) = erfc(|z| / sqrt 2) / 2 for results of at most 11 bits, without a branch: erfc(x) = exp(-x^2) t P(t), t = 1 / (1 + x/2), P of degree 6
-// fitted to exp(x^2) erfc(x) / t in the largest relative error (2.7e-6 on 0 .. 14; 3.1e-6 in fp32).  bell: exp(-z^2 / 2).
+// Phi(-|z|) = erfc(|z| / sqrt 2) / 2 for results of at most 11 bits, without a branch: erfc(x) = exp(-x^2) t P(t), t = 1 / (1 + x/2), P of degree 6 fitted to
+// exp(x^2) erfc(x) / t in the largest relative error on 0 .. 14, and exact where gelu's slope is zero (z = -0.7518: its two terms cancel there, and a fit without this is
+// off by 5.7e-7 at z = -0.75, more than half a unit of fp16): 3.0e-6, in place of 2.7e-6.  bell: exp(-z^2 / 2).
 __device__ inline float normal_tail(float z, float bell) {
     const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.5f * kSqrtHalf, fabsf(z), 1.0f));
-    float p = 0.0410626493f;
-    p = __builtin_fmaf(p, t, -0.167846605f);
-    p = __builtin_fmaf(p, t, 0.180191427f);
-    p = __builtin_fmaf(p, t, 0.0288821887f);
-    p = __builtin_fmaf(p, t, 0.137151808f);
-    p = __builtin_fmaf(p, t, 0.139435709f);
-    p = __builtin_fmaf(p, t, 0.141121447f);
+    float p = 0.041804079f;
+    p = __builtin_fmaf(p, t, -0.170242995f);
+    p = __builtin_fmaf(p, t, 0.183163226f);
+    p = __builtin_fmaf(p, t, 0.0270974953f);
+    p = __builtin_fmaf(p, t, 0.137693584f);
+    p = __builtin_fmaf(p, t, 0.139357433f);
+    p = __builtin_fmaf(p, t, 0.141125649f);
     return p * t * bell;
 }
 

@@ -115,6 +115,25 @@ def test_largest_fp32_operands(layers, m, n, k):
     assert bool(y[0].isnan().all()) and bool(y[1:].isfinite().all())
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_slope_of_gelu_is_rounded_once_next_to_its_zero_too(layers, dtype):
+    """Every code in four units, -0.75 among them, next to which (-0.7518) the two terms of the slope cancel.  In 32 bits the slope is off by less than 2^-17 of
+    itself (its polynomial 2^-18.3, exp and a quotient 2^-23 each of the terms); then half a unit of the result's type."""
+    bits, least = {"f16": (11, -24), "bf16": (8, -133)}[dtype]
+    for unit in (2.0 ** -8, 2.0 ** -7, 2.0 ** -6, 2.0 ** -5):
+        z = torch.zeros(8, 256, device="cuda")
+        codes = (torch.arange(8 * 31, device="cuda").float() - 127).view(8, 31)
+        z[:, 1:32], z[:, 32:39] = codes, torch.arange(121, 128, device="cuda").float()
+        z[:, ::32] = 127.0                                         # every block's largest value
+        z *= unit
+        c = layers.save_checkpoint(z)
+        assert torch.equal(c.restore(torch.float32), z)
+        got = layers.activation_grad(torch.ones(8, 256, dtype=TYPES[dtype], device="cuda"), c, "gelu").double().cpu()
+        want = ref.slope(z.double().cpu(), "gelu")
+        half = torch.exp2((torch.frexp(want)[1] - bits).clamp(min=least).double() - 1)
+        assert bool(((got - want).abs() <= half * 1.001 + 2.0 ** -17 * want.abs()).all()), float(((got - want).abs() - half).max())
+
+
 # ---- more threads than a launch can have (2^32)
 
 def test_few_rows_next_to_more_columns_than_a_launch_has_threads_for(layers):
