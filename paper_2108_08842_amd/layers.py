@@ -9,6 +9,10 @@
 Tensors are torch CUDA(HIP) tensors of float32, float16 or bfloat16 with unit distance between the last dimension's elements; dimensions
 in front of it are rows.  Argument checks, allocation and marshalling only: every step runs in the HIP kernels, on the current
 stream or the one given.  What does not fit raises EdenError (ERR_INVALID_ARG) before anything is launched.
+
+The calls record nothing for autograd: the backward pass is made of calls as above, by hand or in the two halves of a torch.autograd.Function.
+Where autograd records, an operand or an `out` that requires a gradient is refused, since the gradient would be lost (`torch.no_grad()` or `detach()` says
+that none is expected); save_checkpoint takes it.
 """
 from __future__ import annotations
 
@@ -94,9 +98,17 @@ def _rows(t, what):
     return t.data_ptr(), ld if rows > 1 else cols, rows, cols
 
 
+def _gradient_lost(what):
+    """For a tensor that requires a gradient: refused where autograd records."""
+    if torch.is_grad_enabled():
+        _refuse(f"{what} requires a gradient, but nothing is recorded for autograd (torch.no_grad() or detach() where none is expected)")
+
+
 def _same(t, like, what):
     if t.dtype is not like.dtype or t.device != like.device:
         _refuse(f"{what}: {t.dtype} on {t.device}, expected {like.dtype} on {like.device}")
+    if t.requires_grad:
+        _gradient_lost(what)
 
 
 def _output(out, shape, like, what, dtype=None):
@@ -107,6 +119,8 @@ def _output(out, shape, like, what, dtype=None):
     dtype = dtype or like.dtype
     if tuple(out.shape) != tuple(shape) or out.dtype is not dtype or out.device != like.device:
         _refuse(f"{what}: {tuple(out.shape)} of {out.dtype} on {out.device}, expected {tuple(shape)} of {dtype} on {like.device}")
+    if out.requires_grad:
+        _gradient_lost(what)
     address, ld, _, _ = _rows(out, what)
     return out, address, ld
 
@@ -234,6 +248,8 @@ def linear(x, w, bias=None, activation: str = "none", residual=None, checkpoint=
         with _On(device, stream):
             return linear(x, w, bias, activation, residual, checkpoint, out)
     L = _lib or lib()
+    if x.requires_grad:
+        _gradient_lost("linear: x")
     act = _act(activation, "linear")
     xp, ldx, m, k = _rows(x, "linear: x")
     _same(w, x, "linear: w")
@@ -274,6 +290,8 @@ def linear_weight_grad(dy, saved: Checkpoint, bias: bool = False, out=None, bias
         with _On(device, stream):
             return linear_weight_grad(dy, saved, bias, out, bias_out, accumulate)
     L = _lib or lib()
+    if dy.requires_grad:
+        _gradient_lost("linear_weight_grad: dy")
     dp, ldy, m, n = _rows(dy, "linear_weight_grad: dy")
     k = saved.cols
     sp = _saved(saved, m, k, device, "linear_weight_grad")
@@ -296,6 +314,8 @@ def linear_input_grad(dz, w, activation: str = "none", checkpoint: Checkpoint = 
         with _On(device, stream):
             return linear_input_grad(dz, w, activation, checkpoint, residual, out)
     L = _lib or lib()
+    if dz.requires_grad:
+        _gradient_lost("linear_input_grad: dz")
     act = _act(activation, "linear_input_grad")
     dp, ldz, m, n = _rows(dz, "linear_input_grad: dz")
     _same(w, dz, "linear_input_grad: w")
@@ -325,6 +345,8 @@ def activation_grad(dy, saved: Checkpoint, activation: str, out=None, stream=Non
     if _elsewhere(device, stream):
         with _On(device, stream):
             return activation_grad(dy, saved, activation, out)
+    if dy.requires_grad:
+        _gradient_lost("activation_grad: dy")
     act = _act(activation, "activation_grad")
     dp, ldy, rows, cols = _rows(dy, "activation_grad: dy")
     sp = _saved(saved, rows, cols, device, "activation_grad")

@@ -158,3 +158,29 @@ def test_more_rows_than_a_launch_has_threads_for(layers):
     assert np.array_equal(c.buffer[(rows - 100) * 32:rows * 32].cpu().numpy().view(np.int8).reshape(100, 32), codes)
     assert np.array_equal(c.buffer[rows * 33 - 100:].cpu().numpy().reshape(100, 1), exps)
     assert torch.equal(layers.activation_grad(x, c, "relu"), x.clamp(min=0.0))
+
+
+# ---- operands that require a gradient
+
+def test_operands_that_require_a_gradient_are_refused_where_it_would_be_lost(layers):
+    from paper_2108_08842_amd.eden import EdenError
+    g = gen("autograd")
+    x, w, b, r, dy, dw = randn(g, 6, 40), randn(g, 24, 40), randn(g, 24), randn(g, 6, 24), randn(g, 6, 24), torch.zeros(24, 40, device="cuda")
+    kept, z = layers.save_checkpoint(x), layers.save_checkpoint(dy)
+
+    def calls(x, w, b, r, dy, dw):
+        return [lambda: layers.linear(x, w, b, residual=r), lambda: layers.save_checkpoint(x).restore(torch.float32), lambda: layers.linear_weight_grad(dy, kept),
+                lambda: layers.linear_input_grad(dy, w), lambda: layers.linear_input_grad(r, w, residual=x), lambda: layers.activation_grad(dy, z, "gelu"),
+                lambda: layers.linear_weight_grad(r, kept, out=dw), lambda: layers.linear(x, w, stream=torch.cuda.current_stream())]
+
+    plain = {"x": x, "w": w, "b": b, "r": r, "dy": dy, "dw": dw}
+    want = [f().clone() for f in calls(**plain)]
+    for which, refused in (("x", {0, 4, 7}), ("w", {0, 3, 4, 7}), ("b", {0}), ("r", {0, 4, 6}), ("dy", {2, 3, 5}), ("dw", {6})):
+        for number, f in enumerate(calls(**{**plain, which: plain[which].clone().requires_grad_(True)})):
+            if number in refused:
+                with pytest.raises(EdenError):
+                    f()
+            else:
+                assert torch.equal(f(), want[number])
+            with torch.no_grad():                                  # nobody expects one
+                assert torch.equal(f(), want[number])
