@@ -184,3 +184,158 @@ def test_operands_that_require_a_gradient_are_refused_where_it_would_be_lost(lay
                 assert torch.equal(f(), want[number])
             with torch.no_grad():                                  # nobody expects one
                 assert torch.equal(f(), want[number])
+
+
+# ---- subnormal and non-finite operands, in every kernel that has a product
+
+# rows, features out, features in: few rows (dots; matrix cores), tiles, a split sum, tiles with loads straight into the LDS, the same with copies
+# (fp32: 2^29 products, two bytes: 2^30)
+PLACES = [(1, 40, 24), (3, 70, 520), (9, 40, 264), (14, 40, 24), (40, 72, 33), (40, 72, 3000), (40, 72, 3008), (2048, 2048, 136), (1500, 1501, 499)]
+
+
+@pytest.mark.parametrize("m,n,k", PLACES)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_subnormal_operands(layers, dtype, m, n, k):
+    """Whole numbers of the smallest unit next to powers of two that bring the products back into the range: every sum is exact."""
+    t = TYPES[dtype]
+    unit, up = {"f32": (2.0 ** -133, 2.0 ** 110), "f16": (2.0 ** -24, 2.0 ** 10), "bf16": (2.0 ** -133, 2.0 ** 110)}[dtype]
+    small = torch.zeros(m, k, dtype=torch.float64, device="cuda")
+    small[:, ::7] = ((torch.arange(m, device="cuda")[:, None] + torch.arange(0, k, 7, device="cuda")) % 3).double() - 1.0      # -1, 0, 1
+    small[:, k - 1] = torch.arange(m, device="cuda") % 100 + 5
+    small, big = (small * unit).to(t), torch.full((n, k), up, dtype=torch.float64, device="cuda").to(t)
+    want = (small.double() @ big.double().t().contiguous()).to(t)
+    assert bool((want != 0).any())
+    assert torch.equal(layers.linear(small, big), want)
+    assert torch.equal(layers.linear_input_grad(small, big.t().contiguous()), want)
+    flipped = layers.linear(big, small)                            # the weights are the small ones
+    assert torch.equal(flipped, want.t())
+    # the weight gradient's dy, and its sums
+    c = layers.save_checkpoint(torch.full((k, m), up, dtype=torch.float32, device="cuda"))
+    dy = torch.zeros(k, n, dtype=torch.float64, device="cuda")
+    dy[:] = (torch.arange(k, device="cuda")[:, None] + torch.arange(n, device="cuda")) % 3 * unit
+    dy = dy.to(t)
+    dw, db = layers.linear_weight_grad(dy, c, bias=True)
+    sums = dy.double().sum(0)
+    assert torch.equal(dw.double(), (sums[:, None] * up).expand(n, m)) and torch.equal(db.double(), sums)
+
+
+@pytest.mark.parametrize("m,n,k", PLACES)
+def test_fp32_operands_whose_terms_are_subnormal(layers, m, n, k):
+    # what an operand holds below 2^-133 may be left out: at 2^-120 some 2^-13 of it
+    g = gen("tiny", m, k)
+    x, w = randn(g, m, k, scale=2.0 ** -120), randn(g, n, k, scale=2.0 ** 100)
+    X, W = x.double(), w.double()
+    for y in (layers.linear(x, w), layers.linear_input_grad(x, w.t().contiguous()), layers.linear(w, x).t()):
+        near = ref.product_bound(X, W, k) + 2.0 ** -133 * W.abs().sum(1)
+        assert bool(((y.double() - X @ W.t().contiguous()).abs() <= near).all())
+    c = layers.save_checkpoint(randn(g, m, k, scale=2.0 ** 100))
+    dy, held = randn(g, m, n, scale=2.0 ** -120), c.restore(torch.float32).double()
+    dw, db = layers.linear_weight_grad(dy, c, bias=True)
+    Y = dy.double()
+    near = ref.product_bound(Y.t().contiguous(), held.t().contiguous(), m) + 2.0 ** -133 * held.abs().sum(0)
+    assert bool(((dw.double() - Y.t().contiguous() @ held).abs() <= near).all())
+    assert bool(((db.double() - Y.sum(0)).abs() <= (m + 8) * 2.0 ** -23 * Y.abs().sum(0) + m * 2.0 ** -133).all())
+
+
+@pytest.mark.parametrize("m,n,k", PLACES)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_infinities_and_nan_reach_their_own_rows_and_columns(layers, dtype, m, n, k):
+    t = TYPES[dtype]
+    x, w = torch.ones(m, k, dtype=t, device="cuda"), torch.ones(n, k, dtype=t, device="cuda")
+    r, c = m // 2, n - 1
+    x[r, k - 1], w[c, k // 2], w[3, 0] = float("inf"), float("nan"), -float("inf")
+    want = x.double() @ w.double().t().contiguous()
+    finite = torch.ones(m, n, dtype=torch.bool, device="cuda")
+    finite[r], finite[:, c], finite[:, 3] = False, False, False
+    y, z = layers.linear(x, w, checkpoint=True)
+    values = z.restore(torch.float32)
+    dx = layers.linear_input_grad(x, w.t().contiguous())
+    for got in (y, dx):
+        assert torch.equal(got.isfinite(), finite) and torch.equal(got[finite], want[finite].to(t))
+        if t != torch.float32 or (m <= 16 and got is y):           # (products of fp32 terms: an infinity gives NaN)
+            assert torch.equal(got.nan_to_num(nan=7.0), want.to(t).nan_to_num(nan=7.0))
+    blocks = torch.nn.functional.pad(~finite, (0, -n % 32)).view(m, -1, 32).any(2).repeat_interleave(32, 1)[:, :n]
+    assert torch.equal(values.isnan(), blocks)
+    dy = torch.ones(m, n, dtype=t, device="cuda")
+    dy[r, 0], dy[0, n - 1] = float("inf"), float("nan")
+    dw, db = layers.linear_weight_grad(dy, layers.save_checkpoint(torch.ones(m, k, device="cuda")), bias=True)
+    assert bool((dw[0] == float("inf")).all()) and bool(dw[n - 1].isnan().all()) and bool((dw[1:n - 1] == m).all())
+    assert float(db[0]) == float("inf") and bool(db[n - 1].isnan()) and bool((db[1:n - 1] == m).all())
+    kept = torch.ones(m, k, device="cuda")
+    kept[r, k - 1] = float("nan")
+    dw = layers.linear_weight_grad(torch.ones(m, n, dtype=t, device="cuda"), layers.save_checkpoint(kept))
+    bad = torch.zeros(k, dtype=torch.bool, device="cuda")
+    bad[(k - 1) // 32 * 32:] = True
+    assert bool(dw[:, bad].isnan().all()) and bool((dw[:, ~bad] == m).all())
+
+
+# ---- the general kernel's tiles of 128 x 128: from 256 of them on
+
+@pytest.mark.parametrize("n,k,m,pad", [(2056, 2051, 333, 0), (2050, 2056, 64, 3), (2177, 1930, 33, 1)])
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+def test_weight_grad_in_large_tiles(layers, dtype, n, k, m, pad):
+    g = gen("tiles", n, m)
+    dy = torch.full((m, n + pad), float("nan"), dtype=TYPES[dtype], device="cuda")[:, :n]
+    dy.copy_(randn(g, m, n))
+    c = layers.save_checkpoint(randn(g, m, k, scale=10.0))
+    X, Y = c.restore(torch.float32).double(), dy.double()
+    flat = torch.full((1 + n * k + 2 + n,), 4.0, device="cuda")
+    out, bias_out = flat[1:1 + n * k].view(n, k), flat[1 + n * k + 2:]
+    layers.linear_weight_grad(dy, c, out=out, bias_out=bias_out)
+    want, want_b = Y.t().contiguous() @ X, Y.sum(0)
+    assert bool(((out.double() - want).abs() <= ref.product_bound(Y.t().contiguous(), X.t().contiguous(), m) + 2.0 ** -24 * want.abs()).all())
+    assert ref.rel(out, want) <= ref.norm_bound(m, torch.float32)
+    assert bool(((bias_out.double() - want_b).abs() <= (m + 8) * 2.0 ** -23 * Y.abs().sum(0)).all())
+    first, first_b = out.clone(), bias_out.clone()
+    layers.linear_weight_grad(dy, c, out=out, bias_out=bias_out, accumulate=True)
+    assert torch.equal(out, first + first) and torch.equal(bias_out, first_b + first_b)
+    assert bool((flat[:1] == 4.0).all()) and bool((flat[1 + n * k:3 + n * k] == 4.0).all())
+
+
+@pytest.mark.parametrize("m,n,k,pad", [(2100, 2051, 100, 0), (2051, 2100, 333, 3), (2305, 1801, 31, 1)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_products_in_large_tiles_without_a_workspace(layers, dtype, m, n, k, pad):
+    # rows that begin anywhere and no room for copies of them
+    t, g = TYPES[dtype], gen("anywhere", m)
+
+    def apart(rows, cols, scale=1.0):
+        return torch.full((rows, cols + pad), float("nan"), dtype=t, device="cuda")[:, :cols].copy_(randn(g, rows, cols, scale=scale))
+
+    x, w, r, L, code = apart(m, k), apart(n, k, k ** -0.5), apart(m, n), layers.lib(), layers._DTYPES[t]
+    y, z = torch.full((m, n + pad), 5.0, dtype=t, device="cuda"), layers.Checkpoint(torch.empty(layers.checkpoint_bytes(m, n), dtype=torch.uint8, device="cuda"), m, n)
+    assert L.eden_linear(x.data_ptr(), k + pad, w.data_ptr(), k + pad, None, r.data_ptr(), n + pad, y.data_ptr(), n + pad, z.buffer.data_ptr(), z.buffer.numel(), m, n, k, code, 0,
+                         None, 0, stream()) == 0
+    product = x.double() @ w.double().t().contiguous()
+    want, dz = product + r.double(), ref.product_bound(x.double(), w.double(), k)
+    assert bool(((y[:, :n].double() - want).abs() <= dz + (4 * ref.EPS + ref.ROUND[t]) * want.abs() + ref.TINY[t]).all()) and bool((y[:, n:] == 5.0).all())
+    codes, exps = ref.unpack(z.buffer, m, n)
+    unit = torch.from_numpy(np.repeat(np.exp2(exps.astype(np.float64) - 127), 32, axis=1)[:, :n])
+    held = torch.from_numpy(ref.decode(codes, exps, n))
+    assert bool(((held - product.cpu()).abs() <= unit * torch.where(held.abs() == 127 * unit, 1.0, 0.5) + dz.cpu()).all()) and not codes[:, n:].any()
+    # dx of that size: dz is m x k, w k x n
+    v, dx = apart(k, n, k ** -0.5), torch.full((m, n + pad), 5.0, dtype=t, device="cuda")
+    assert L.eden_linear_input_grad(x.data_ptr(), k + pad, v.data_ptr(), n + pad, z.buffer.data_ptr(), 4, None, 0, dx.data_ptr(), n + pad, m, k, n, code, None, 0, stream()) == 0
+    product = x.double() @ v.double()
+    want = product * ref.slope(held, "silu").cuda()
+    near = 1.13 * ref.product_bound(x.double(), v.double().t().contiguous(), k) + 2.0 ** -19 * product.abs() + (4 * ref.EPS + ref.ROUND[t]) * want.abs() + ref.TINY[t]
+    assert bool(((dx[:, :n].double() - want).abs() <= near).all()) and bool((dx[:, n:] == 5.0).all())
+
+
+# ---- the same bits every time
+
+def test_checkpoints_ends_and_joined_sums_give_the_same_bits_every_time(layers):
+    g = gen("again")
+    bf = torch.bfloat16
+    x, w, b, r = randn(g, 2304, 1024, dtype=bf), randn(g, 4096, 1024, dtype=bf, scale=2.0 ** -5), randn(g, 4096, dtype=bf), randn(g, 2304, 4096, dtype=bf)
+    x32, w32 = randn(g, 40, 3000), randn(g, 72, 3000)
+
+    def calls():
+        y, z = layers.linear(x, w, b, activation="gelu", residual=r, checkpoint=True)
+        s, q = layers.linear(x32, w32, activation="silu", checkpoint=True)
+        dx = layers.linear_input_grad(y, w, activation="gelu", checkpoint=layers.save_checkpoint(x))
+        return y, z.buffer, s, q.buffer, dx, *layers.linear_weight_grad(r, z, bias=True)
+
+    first = calls()
+    for _ in range(10):
+        for got, want in zip(calls(), first):
+            assert torch.equal(got, want)
