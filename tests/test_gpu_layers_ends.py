@@ -134,6 +134,21 @@ def test_slope_of_gelu_is_rounded_once_next_to_its_zero_too(layers, dtype):
         assert bool(((got - want).abs() <= half * 1.001 + 2.0 ** -17 * want.abs()).all()), float(((got - want).abs() - half).max())
 
 
+@pytest.mark.parametrize("m", [3, 40])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_gelu_under_a_residual_that_nearly_cancels_it(layers, dtype, m):
+    """In 32 bits gelu is off by 2^-20 + 2^-23 |z| of itself (exp of z^2 / 2, its argument rounded twice; polynomial, quotient and products 2^-21); then one
+    rounding of the sum.  z is an operand itself: one product by 1."""
+    t, bits, least = TYPES[dtype], {"f16": 11, "bf16": 8}[dtype], {"f16": -24, "bf16": -133}[dtype]
+    z = (torch.arange(m * 40, device="cuda").double() / (m * 40) * 8 - 4).to(t).view(m, 40)
+    act = ref.act(z.double(), "gelu")
+    residual = (-act).to(t)
+    got = layers.linear(z, torch.eye(40, dtype=t, device="cuda"), activation="gelu", residual=residual).double()
+    want = act + residual.double()
+    half = torch.exp2((torch.frexp(want)[1] - bits).clamp(min=least).double() - 1)
+    assert bool(((got - want).abs() <= (2.0 ** -20 + 2.0 ** -23 * z.double().abs()) * act.abs() + 1.001 * half).all())
+
+
 # ---- more threads than a launch can have (2^32)
 
 def test_few_rows_next_to_more_columns_than_a_launch_has_threads_for(layers):
