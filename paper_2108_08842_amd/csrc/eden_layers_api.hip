@@ -80,8 +80,8 @@ bool direct_type(Op op, uint32_t dtype, const Product &p) {
 }
 // ... and whether that is the faster one: it has a long way to its first product.  2 bytes: two steps deep and up to 2^20 results the general kernel is (1024 x
 // 1024 x 128 bf16 5.0 us against 5.6; 1024 x 1024 x 256 12.5 against 6.3, 2048 x 2048 x 128 8.9 against 6.8).  With a checkpoint below 2^28 products (512 x 512 x 768
-// 11.5 against 14.1; 1024 x 1024 x 256 12.8 against 8.6).  fp32 below 1.5 * 2^28 (1024 x 1024 x 256 15.2 against 17.3; 768 x 768 x 768 23.3 against 22.3,
-// 2048 x 2048 x 512 43 against 34).
+// 11.5 against 14.1; 1024 x 1024 x 256 12.8 against 8.6).  fp32 below 1.5 * 2^28 (1024 x 1024 x 256 14.6 against 17.0; 768 x 768 x 768 20.6 against 20.8,
+// 2048 x 2048 x 512 35.7 against 31.6).
 bool direct_pays(Op op, uint32_t dtype, const Product &p) {
     const double results = (double)p.rows * p.cols, products = results * p.depth;
     if (dtype == EDEN_F32) return products >= 1.5 * (1u << 28);
@@ -97,12 +97,12 @@ bool many_columns(uint32_t dtype, const Product &p, uint64_t room) {
            partial_bytes(p.rows, p.cols, direct_shape(p.rows, p.cols, p.depth).splits) <= room;
 }
 
-// Copies cost two passes over an operand and are worth it from about 2^30 products on in 2 bytes (1501 x 1501 x 1501: 40 -> 31 us, 1021 x 1001 x 2047: 31 -> 27; 801 x 1001 x
-// 1335: no difference), from 2^29 in fp32 (1235 x 7079 x 2681: 513 -> 361 us, 301 x 2001 x 1001: 54 -> 34, 831 x 831 x 831: 33 -> 31), but not for a
-// narrow result (fp32, 2318 x 192 x 3081: 52 us in place of 43).
+// Copies cost two passes over an operand and are worth it from about 2^30 products on: in 2 bytes 1501 x 1501 x 1501 38 -> 30 us, 1021 x 1001 x 2047 28 -> 26.5, 801 x 1001 x 1335 between
+// 20 -> 22 (eden_linear) and 23 -> 20 (input gradient), 831 x 831 x 831 14 -> 18; in fp32 1235 x 7079 x 2681 446 -> 353, 1235 x 1235 x 1235 53 -> 46, 801 x 1001 x 1335 35 -> 37,
+// 831 x 831 x 831 22 -> 30, 301 x 2001 x 1001 24 -> 32.  Not for a narrow result (fp32, 2318 x 192 x 3081: 35 -> 47).
 uint64_t copy_bytes(uint64_t a, uint64_t b, uint32_t dtype) { return (a + 63) / 64 * 64 * ((b + 63) / 64 * 64) * bytes_of(dtype); }
-bool worth_copies(uint64_t rows, uint64_t cols, uint64_t depth, uint32_t dtype) {
-    const uint64_t most = 1u << 21, least = dtype == EDEN_F32 ? 1u << 29 : 1u << 30;
+bool worth_copies(uint64_t rows, uint64_t cols, uint64_t depth) {
+    const uint64_t most = 1u << 21, least = 1u << 30;
     return rows >= 256 && cols >= 256 && rows < most && cols < most && depth < most && rows * cols >= least / std::max<uint64_t>(depth, 1);
 }
 // Replaces an operand by a copy in the workspace.
@@ -128,7 +128,7 @@ int run(Op op, uint32_t dtype, Product &p, void *workspace, size_t workspace_byt
         // rows along the depth that do not end with a piece need zeros behind it in both operands
         const bool a = !whole_a(op, dtype, p), b = !whole_b(op, dtype, p);
         const uint64_t need = (a ? copy_bytes(p.rows, p.depth, dtype) : 0) + (b ? copy_bytes(p.cols, p.depth, dtype) : 0);
-        direct = worth_copies(p.rows, p.cols, p.depth, dtype) && need <= workspace_bytes;
+        direct = worth_copies(p.rows, p.cols, p.depth) && need <= workspace_bytes;
         hipError_t e = hipSuccess;
         if (direct && a) {
             e = op == kWeightGrad ? copy_operand(dtype, p.a, p.lda, p.depth, p.rows, space, workspace_bytes, st) : copy_operand(dtype, p.a, p.lda, p.rows, p.depth, space, workspace_bytes, st);
@@ -191,7 +191,7 @@ size_t eden_layers_workspace_bytes(uint64_t rows, uint64_t cols, uint64_t depth,
 size_t eden_layers_copying_bytes(uint64_t rows, uint64_t cols, uint64_t depth, uint32_t dtype) {
     if (!known_type(dtype) || rows > kMostSize || cols > kMostSize || depth > kMostSize) return 0;
     const size_t plain = eden_layers_workspace_bytes(rows, cols, depth, dtype);
-    if (!worth_copies(rows, cols, depth, dtype)) return plain;
+    if (!worth_copies(rows, cols, depth)) return plain;
     return plain + copy_bytes(rows, depth, dtype) + copy_bytes(cols, depth, dtype);
 }
 

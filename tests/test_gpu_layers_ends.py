@@ -204,7 +204,7 @@ def test_operands_that_require_a_gradient_are_refused_where_it_would_be_lost(lay
 # ---- subnormal and non-finite operands, in every kernel that has a product
 
 # rows, features out, features in: few rows (dots; matrix cores), tiles, a split sum, tiles with loads straight into the LDS, the same with copies
-# (fp32: 2^29 products, two bytes: 2^30)
+# (from 2^30 products on)
 PLACES = [(1, 40, 24), (3, 70, 520), (9, 40, 264), (14, 40, 24), (40, 72, 33), (40, 72, 3000), (40, 72, 3008), (2048, 2048, 136), (1500, 1501, 499)]
 
 

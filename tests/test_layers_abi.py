@@ -118,3 +118,12 @@ def test_tensors_that_are_not_on_the_gpu_are_refused(layers):
                  lambda: layers.Checkpoint(torch.zeros(66, dtype=torch.uint8), 2, 8)):
         with pytest.raises(EdenError):
             call()
+
+
+@pytest.mark.parametrize("dtype", [0, 1, 2])
+def test_no_room_for_copies_below_two_to_the_30_products(layers, dtype):
+    plain, copying = layers.lib().eden_layers_workspace_bytes, layers.lib().eden_layers_copying_bytes
+    for size in ((831, 831, 831), (301, 2001, 1001), (1023, 1024, 1024), (255, 8192, 8192), (8192, 255, 8192)):
+        assert copying(*size, dtype) == plain(*size, dtype)
+    for size in ((1025, 1024, 1024), (1235, 1235, 1235), (256, 8192, 8192)):
+        assert copying(*size, dtype) > plain(*size, dtype)
