@@ -58,9 +58,10 @@ Shape direct_shape(uint64_t rows, uint64_t cols, uint64_t depth) {
     const uint64_t splits = rows * cols <= 40000 ? splits_of(small, depth, 512, 128) : splits_of(small, depth, 256, 512);
     return {128, rows <= 128 ? std::max(splits, splits_of(small, depth, 512, 1024)) : splits};
 }
-// Through registers: 128 x 128 where those fill the device (fp16 weight gradient 2048 x 4096, 1024 deep: 60 us against 75 with 64 x 64), else 64 x 64, three or more to
-// a CU.  `slots`: as many workgroups as split a sum together: 512 where each product has one term (512 x 1001 x 1003 bf16: 17 us against 21 with 1024), else 1024
-// (fp16 weight gradient 568 x 696, 2624 deep: 25 against 27.5 with 512).
+// Through registers: 128 x 128 where those fill the device (fp16 weight gradient 2048 x 4096, 1024 deep: 52 us against 63 with 64 x 64), else 64 x 64, three or more to
+// a CU.  `slots`: as many workgroups as split a sum together: 512 (512 x 1001 x 1003 bf16: 13.3 us against 18 with 1024; weight gradients 1001 x 1024, 555 deep, fp32 17.5
+// against 19.9; 256 x 256, 8192 deep, 16.3 against 20.8; 568 x 696, 2624 deep, fp16 21.3 against 21.9), between two fp32 operands, with six products of terms, 1024 (2318 x
+// 192, 3081 deep: 36 against 39 with 512; 3405 x 128, 1193 deep, 20.5 against 19.6).
 Shape tiles_shape(uint64_t rows, uint64_t cols, uint64_t depth, uint64_t slots) {
     if (tile_count(rows, cols, 128) >= 256) return {128, 1};
     return {64, splits_of(tile_count(rows, cols, 64), depth, slots, 96)};
@@ -79,8 +80,8 @@ bool direct_type(Op op, uint32_t dtype, const Product &p) {
     return !(op == kWeightGrad && dtype != EDEN_BF16) && p.depth != 0 && p.cols != 0 && (op != kWeightGrad || p.ldb < (1u << 24));
 }
 // ... and whether that is the faster one: it has a long way to its first product.  2 bytes: two steps deep and up to 2^20 results the general kernel is (1024 x
-// 1024 x 128 bf16 5.0 us against 5.6; 1024 x 1024 x 256 12.5 against 6.3, 2048 x 2048 x 128 8.9 against 6.8).  With a checkpoint below 2^28 products (512 x 512 x 768
-// 11.5 against 14.1; 1024 x 1024 x 256 12.8 against 8.6).  fp32 below 1.5 * 2^28 (1024 x 1024 x 256 14.6 against 17.0; 768 x 768 x 768 20.6 against 20.8,
+// 1024 x 128 bf16 4.1 us against 5.6; 1024 x 1024 x 256 11.8 against 6.4, 2048 x 2048 x 128 7.4 against 6.7).  With a checkpoint below 2^28 products (512 x 512 x 768
+// 11.0 against 14.0; 1024 x 1024 x 256 12.5 against 8.6).  fp32 below 1.5 * 2^28 (1024 x 1024 x 256 14.6 against 17.0; 768 x 768 x 768 20.6 against 20.8,
 // 2048 x 2048 x 512 35.7 against 31.6).
 bool direct_pays(Op op, uint32_t dtype, const Product &p) {
     const double results = (double)p.rows * p.cols, products = results * p.depth;
@@ -140,7 +141,7 @@ int run(Op op, uint32_t dtype, Product &p, void *workspace, size_t workspace_byt
         }
         if (e != hipSuccess) return EDEN_ERR_HIP;
     }
-    const Shape shape = !direct ? tiles_shape(p.rows, p.cols, p.depth, op == kWeightGrad || dtype == EDEN_F32 ? 1024 : 512) : dtype == EDEN_F32 ? fp32_shape(p.rows, p.cols, p.depth) : direct_shape(p.rows, p.cols, p.depth);
+    const Shape shape = !direct ? tiles_shape(p.rows, p.cols, p.depth, op != kWeightGrad && dtype == EDEN_F32 ? 1024 : 512) : dtype == EDEN_F32 ? fp32_shape(p.rows, p.cols, p.depth) : direct_shape(p.rows, p.cols, p.depth);
     if (tile_count(p.rows, p.cols, shape.side) * shape.splits > most_groups(256)) return EDEN_ERR_INVALID_ARG;      // (one launch; such a result has 2^38 places)
     uint64_t splits = p.cols ? shape.splits : 1;                   // (row sums alone have no columns at which a join would find them)
     while (splits > 1 && partial_bytes(p.rows, p.cols, splits) > workspace_bytes) --splits;
