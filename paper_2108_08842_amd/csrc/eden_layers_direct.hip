@@ -13,10 +13,11 @@
 //
 // Where 256 x 256 would leave CUs idle, tiles of 128 x 128 with waves of 64 x 64, two workgroups to a CU.
 //
-// Bound by the card's power: bf16, 8192 x 16384 with 4096 products each takes 806 to 845 us without an end (1300 to 1365 TFLOP/s; a matrix product alone 726 to
-// 808), the matrix cores are busy 86% of the cycles at 1.5 GHz, and the clock falls where they are busier.  Bias, gelu, residual and checkpoint, 0.4 GB to be
-// written, add 140 to 170 us that the one workgroup of a CU has nothing to hide behind.  Input gradient of these sizes with gelu's slope 970, weight gradient
-// 4096 x 8192 from a checkpoint, 8192 deep, 480 (1140 TFLOP/s; decoding takes the vector unit).  Tiles of 128: 1021 x 5000, 2048 deep, fp16 33 us (640 TFLOP/s).
+// The product alone is bound by the card's power: bf16, 8192 x 16384 with 4096 products each takes 820 to 845 us without an end (1300 to 1340 TFLOP/s; a library's product 726 to
+// 808), with the matrix cores busy 73% of the cycles at a clock of 1.44 GHz (six launches under a profiler; counters_layers.txt).  Bias, gelu and checkpoint, 0.4 GB to be
+// written, make it 960 to 975, a residual 1040: the one workgroup of a CU has nothing to hide its end behind, and the matrix cores are busy 60% of the cycles at 1.6 GHz.
+// Input gradient of these sizes with gelu's slope 950 to 970 (59%, 1.67 GHz).  Weight gradient 4096 x 8192 from a checkpoint, 8192 deep, 475 to 495 (1110 to 1160 TFLOP/s): the vector unit, which decodes the
+// codes, and the waits for them leave the matrix cores 54% of the cycles at 1.7 to 1.85 GHz.  Tiles of 128: 1021 x 5000, 2048 deep, fp16 33 us (640 TFLOP/s).
 // Not faster: nine tiles in the LDS in place of five for tiles of 128 (four steps ahead; a CU's loads bound them, 0.4 to 0.5 us for 64 deep), a second set of
 // registers for the codes, tiles of 256 x 128, loads 32 deep (half a line each: twice the requests).
 #include "eden_layers_fetch.h"

@@ -6,7 +6,9 @@
 // A workgroup has a tile of 128 x 128, two to a CU, a wave 64 x 64.  Operands' tiles are 32 deep (128-byte lines) and go straight into the LDS as fp32; the LDS
 // holds five, in turns as in the kernel for two-byte types: the two in use, the next two, the first of the two after that.  A wave reads the
 // operands of the next 16 deep and takes them apart in registers while it multiplies those of the last: 5.5 vector instructions an element,
-// 176 in the time of 24 products.  Bound by the card's power: 4096 x 8192 x 4096 takes 1320 us = 208 TFLOP/s with the matrix cores busy 68% of the cycles at 1.5 GHz.
+// 176 in the time of 24 products.  Bound by the card's power and the vector unit: 4096 x 8192 x 4096 takes 1380 to 1390 us = 198 TFLOP/s (input gradient 1390 to
+// 1400), with the matrix cores busy 65% of the cycles at 1.47 GHz (six launches under a profiler).  Two workgroups fit a CU, but a sum is split over 256 of them only: 3654 x 320, 11904 deep, is 87 tiles in
+// two parts and takes 266 us with the matrix cores busy 34% of the cycles.
 #include "eden_layers_fetch.h"
 
 namespace eden_layers {

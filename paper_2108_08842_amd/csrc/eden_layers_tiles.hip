@@ -12,8 +12,9 @@
 // columns of the result: the end of the product works on vectors, and a checkpoint's block of 32 columns is 16 values in each of two lanes.
 //
 // Takes what the kernels with loads straight into the LDS do not: rows that begin anywhere, small products, fp32 and fp16 next to a checkpoint.  Bound by the way
-// through the registers: a step's loads are as far ahead as its registers reach, and its vector instructions (terms) stand between products.  Weight gradient of
-// 4096 x 4096, 4096 deep: fp16 417 us (329 TFLOP/s, twice that in terms), fp32 460 us; 555 x 1001, 1024 deep, fp32: 16 us and 4.5 for the join, most of it waiting.
+// through the registers: a step's loads are as far ahead as its registers reach, and with more than one term there is one stage, so that a step has two barriers and takes its operands
+// apart between them, when no product runs: weight gradient of 4096 x 4096, 4096 deep, fp16 345 us (400 TFLOP/s, twice that in terms; matrix cores busy 34% of the
+// cycles), fp32 460 us (300 TFLOP/s; 40%).  1001 x 1024, 555 deep, fp32: 256 tiles in two parts, 14.5 us and 4.4 for the join, most of it waiting.
 #include "eden_layers_product.h"
 
 namespace eden_layers {

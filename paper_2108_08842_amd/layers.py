@@ -10,6 +10,9 @@ Tensors are torch CUDA(HIP) tensors of float32, float16 or bfloat16 with unit di
 in front of it are rows.  Argument checks, allocation and marshalling only: every step runs in the HIP kernels, on the current
 stream or the one given.  What does not fit raises EdenError (ERR_INVALID_ARG) before anything is launched.
 
+An `out` must not overlap an operand, except that linear's and linear_input_grad's may be the residual itself and activation_grad's dy itself.  With `stream` the operands have
+to be ready on that stream and to stay until its work is done; results and workspaces are allocated on it.
+
 The calls record nothing for autograd: the backward pass is made of calls as above, by hand or in the two halves of a torch.autograd.Function.
 Where autograd records, an operand or an `out` that requires a gradient is refused, since the gradient would be lost (`torch.no_grad()` or `detach()` says
 that none is expected); save_checkpoint takes it.
