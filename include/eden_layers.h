@@ -13,7 +13,8 @@
  * Matrices are row-major with unit distance between the columns; ld* is the distance between rows in elements, at least the
  * number of columns (any value if there is at most one row).  Pointers are aligned to their element type; rows that start at
  * multiples of 16 bytes are read fastest.  Every size may be 0 (nothing is written where there is no output; a sum over nothing is 0), and
- * is at most 2^30.  Outputs must not overlap inputs, except that eden_linear's y and eden_linear_input_grad's dx may be the
+ * is at most 2^30; a product's result has less than 2^24 tiles of 128 x 128, and rows (cols / 2048 + 1) of an element-wise call
+ * is below 2^31 (beyond any device's memory, and refused).  Outputs must not overlap inputs, except that eden_linear's y and eden_linear_input_grad's dx may be the
  * residual itself and eden_activation_grad's dz may be dy itself (same pointer, same distance).
  *
  * Sums are held in fp32 and results rounded once, to nearest even.  The products of fp16 and bf16 operands are exact.  fp32
