@@ -11,7 +11,8 @@ ROOT = os.path.dirname(PKG)
 LIB = os.path.join(PKG, "libeden_hip.so")
 OBJ_DIR = os.path.join(ROOT, "_build")
 SOURCES = ["eden_tables.cpp", "eden_kernels.hip", "eden_kernels_small.hip", "eden_kernels_sparse.hip", "eden_kernels_wg.hip", "eden_kernels_wg_dec.hip", "eden_kernels_lo14.hip", "eden_kernels_lo15.hip", "eden_api.hip",
-           "eden_layers_tiles.hip", "eden_layers_direct.hip", "eden_layers_direct_fp32.hip", "eden_layers_rows.hip", "eden_layers_elements.hip", "eden_layers_api.hip"]
+           "eden_layers_tiles.hip", "eden_layers_direct.hip", "eden_layers_direct_fp32.hip", "eden_layers_rows.hip", "eden_layers_elements.hip", "eden_layers_api.hip",
+           "eden_blocks_grad_f32.hip", "eden_blocks_grad_f16.hip", "eden_blocks_grad_bf16.hip", "eden_blocks_join.hip", "eden_blocks_sums.hip", "eden_blocks_api.hip"]
 
 
 def hipcc_path() -> str:
@@ -35,12 +36,15 @@ def _stale(src: str, obj: str) -> bool:
     if not os.path.exists(obj):
         return True
     csrc = os.path.join(PKG, "csrc")
-    # the layer operators share no header with the rest but eden.h
-    layers = os.path.basename(src).startswith("eden_layers")
-    deps = [src, os.path.join(ROOT, "include", "eden.h")] + [os.path.join(csrc, f) for f in os.listdir(csrc)
-                                                             if f.endswith(".h") and f.startswith("eden_layers") == layers]
-    if layers:
-        deps.append(os.path.join(ROOT, "include", "eden_layers.h"))
+    # the encoder's sources and those of the layers share no header but eden.h and the hash; the block operators build on the layers
+    families = ["eden_layers", "eden_blocks", "eden_mx4"]
+
+    def family(name):
+        return next((f for f in families if name.startswith(f)), "eden")
+    own = {"eden_layers": families[:1], "eden_blocks": families[:2], "eden_mx4": families, "eden": ["eden"]}[family(os.path.basename(src))]
+    deps = [src, os.path.join(ROOT, "include", "eden.h"), os.path.join(csrc, "eden_hash.h")]
+    deps += [os.path.join(csrc, f) for f in os.listdir(csrc) if f.endswith(".h") and family(f) in own]
+    deps += [p for p in (os.path.join(ROOT, "include", f + ".h") for f in own) if os.path.exists(p)]
     return any(os.path.getmtime(dep) > os.path.getmtime(obj) for dep in deps)
 
 

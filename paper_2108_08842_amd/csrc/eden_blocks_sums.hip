@@ -1,0 +1,51 @@
+// Adds parts of sums over rows, in their order: out[row][col] (+)= sum over p of from[row * parts + p][col].
+//
+// A workgroup has 64 neighbouring columns of one result; its sixteen waves take a sixteenth of the parts each, eight reads on their way at a time, and meet in the LDS.
+#include "eden_blocks_kernels.h"
+
+namespace eden_layers {
+namespace {
+
+constexpr int kWaves = 16;
+
+__global__ __launch_bounds__(kWaves * 64) void k_sums(const SumsArgs a) {
+    __shared__ float shared[kWaves][64];
+    uint32_t which = 0;
+    while (blockIdx.x >= a.first[which + 1]) ++which;
+    const uint32_t segments = (a.cols + 63) / 64, number = blockIdx.x - a.first[which], row = number / segments;
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = (number - row * segments) * 64 + lane;
+    const uint32_t parts = a.parts[which], each = (parts + kWaves - 1) / kWaves, begin = min(wave * each, parts), end = min(begin + each, parts);
+    float sum = 0.0f;
+    if (col < a.cols) {
+        const float *from = a.of[which].from + (uint64_t)row * parts * a.ld_from + col;
+        uint32_t p = begin;
+        for (; p + 8 <= end; p += 8) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = from[(uint64_t)(p + i) * a.ld_from];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += v[i];
+        }
+        for (; p < end; ++p) sum += from[(uint64_t)p * a.ld_from];
+    }
+    shared[wave][lane] = sum;
+    __syncthreads();
+    if (wave || col >= a.cols) return;
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) sum += shared[w][lane];
+    float *to = a.of[which].to + row * a.ld_to[which] + col;
+    *to = a.accumulate ? *to + sum : sum;
+}
+
+}  // namespace
+
+hipError_t launch_sums(const SumsArgs &args, hipStream_t st) {
+    SumsArgs a = args;
+    const uint32_t segments = (a.cols + 63) / 64;
+    a.first[0] = 0;
+    for (uint32_t i = 0; i < a.count; ++i) a.first[i + 1] = a.first[i] + segments * a.rows[i];
+    k_sums<<<a.first[a.count], kWaves * 64, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace eden_layers

@@ -9,6 +9,7 @@
 #include <stdint.h>
 
 #include "eden.h"                    // status bits, packet size
+#include "eden_hash.h"
 
 namespace eden {
 
@@ -16,22 +17,6 @@ constexpr int kMaxBatch = 32;            // senders handled by one launch; large
 constexpr uint32_t kEncCounterStride = 32;  // words between the arrival counters of two senders: a memory line each (see enc_last_tail)
 constexpr uint32_t kDecCounters = 8;     // arrival counters of the small decode launches, used in turn (see k_dec_small)
 constexpr int kLoBits = 12;              // index bits transformed by the contiguous pass up to D = 2^18
-
-// ---- shared randomness (Sec. 2.1): counter hash = splitmix64 stream started at a per-(seed,stream,client) key
-constexpr uint64_t kPhi = 0x9E3779B97F4A7C15ull;
-enum : uint32_t { kStreamSign = 0, kStreamSubsample = 1, kStreamLoss = 2, kStreamMix = 3, kStreamSparse = 4 };
-
-__host__ __device__ inline uint64_t mix64(uint64_t z) {
-    z ^= z >> 30; z *= 0xBF58476D1CE4E5B9ull;
-    z ^= z >> 27; z *= 0x94D049BB133111EBull;
-    z ^= z >> 31;
-    return z;
-}
-__host__ __device__ inline uint64_t stream_key(uint64_t seed, uint32_t stream, uint32_t client) {
-    const uint64_t tag = ((uint64_t)stream << 32) | (uint64_t)client;
-    return mix64(mix64(seed + kPhi) + kPhi * tag + kPhi);
-}
-__host__ __device__ inline uint64_t hash_word(uint64_t key, uint64_t j) { return mix64(key + kPhi * (j + 1)); }
 
 // ---- bit budgets (Sec. 4.1): b_q8 = 256 b -> bits per transmitted index, keep one coordinate in k.
 // b = 1.5, 2.5, 3.5 ("mixed"): every coordinate has floor(b) bits in the first part of the payload and one

@@ -6,36 +6,12 @@
 //
 // 8192 x 8192 bf16: save 38 us = 5.3 TB/s, restore 37 us = 5.4 TB/s.  Gradient through gelu_tanh, 8192 x 16384 bf16: 143 us = 4.7 TB/s, with vector instructions in
 // 84% of the cycles.  17 x 1000: 2.6 us a launch, whatever it does.
-#include "eden_layers_kernels.h"
-
-#include <algorithm>
+#include "eden_layers_spread.h"
 
 namespace eden_layers {
 namespace {
 
-constexpr uint32_t kThreads = 256;
-
-// threads of a row (a power of two, 4 at least: a block's) and workgroups along it
-struct Spread {
-    uint32_t shift, segments;
-    uint64_t groups;
-};
-Spread spread(uint32_t rows, uint32_t cols) {
-    const uint32_t units = (uint32_t)blocks_of(cols) * 4;
-    uint32_t shift = 2;
-    while (shift < 8 && (1u << shift) < units) ++shift;
-    const uint32_t segments = (units + (1u << shift) - 1) >> shift, rows_each = kThreads >> shift;
-    return {shift, segments, (uint64_t)((rows + rows_each - 1) / rows_each) * segments};
-}
-struct Place {
-    uint32_t row, col;
-};
-// `before`: workgroups of the call's launches before this one
-__device__ inline Place place(uint32_t shift, uint32_t segments, uint32_t before) {
-    const uint32_t number = before + blockIdx.x, group = number / segments, segment = number - group * segments;
-    return {group * (kThreads >> shift) + (threadIdx.x >> shift), ((segment << shift) + (threadIdx.x & ((1u << shift) - 1))) * 8};
-}
-__device__ inline int valid_of(uint32_t col, uint32_t cols) { return col < cols ? (int)min(8u, cols - col) : 0; }
+constexpr uint32_t kThreads = kSpreadThreads;
 
 template <uint32_t DTYPE>
 __global__ __launch_bounds__(kThreads) void k_save(const typename Elem<DTYPE>::type *x, size_t ldx, uint32_t rows, uint32_t cols, uint32_t blocks,
@@ -118,21 +94,6 @@ __global__ __launch_bounds__(kThreads) void k_copy_rows(const T *from, size_t ld
         for (int i = 0; i < 8; ++i) v.v[i] = i < valid ? p[i] : (T)0;
     }
     __builtin_memcpy(__builtin_assume_aligned(to + (size_t)at.row * to_ld + at.col, 16), &v, sizeof(v));
-}
-
-template <class F> void for_type(uint32_t dtype, F f) {
-    if (dtype == EDEN_F32) f(std::integral_constant<uint32_t, EDEN_F32>());
-    else if (dtype == EDEN_F16) f(std::integral_constant<uint32_t, EDEN_F16>());
-    else f(std::integral_constant<uint32_t, EDEN_BF16>());
-}
-// f(workgroups before a launch, workgroups of it) until all are launched
-template <class F> hipError_t launches(const Spread &s, F f) {
-    hipError_t e = hipSuccess;
-    for (uint64_t before = 0; before < s.groups && e == hipSuccess; before += most_groups(kThreads)) {
-        f((uint32_t)before, (uint32_t)std::min(s.groups - before, most_groups(kThreads)));
-        e = hipGetLastError();
-    }
-    return e;
 }
 
 }  // namespace
