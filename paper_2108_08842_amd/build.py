@@ -12,7 +12,8 @@ LIB = os.path.join(PKG, "libeden_hip.so")
 OBJ_DIR = os.path.join(ROOT, "_build")
 SOURCES = ["eden_tables.cpp", "eden_kernels.hip", "eden_kernels_small.hip", "eden_kernels_sparse.hip", "eden_kernels_wg.hip", "eden_kernels_wg_dec.hip", "eden_kernels_lo14.hip", "eden_kernels_lo15.hip", "eden_api.hip",
            "eden_layers_tiles.hip", "eden_layers_direct.hip", "eden_layers_direct_fp32.hip", "eden_layers_rows.hip", "eden_layers_elements.hip", "eden_layers_api.hip",
-           "eden_blocks_grad_f32.hip", "eden_blocks_grad_f16.hip", "eden_blocks_grad_bf16.hip", "eden_blocks_join.hip", "eden_blocks_sums.hip", "eden_blocks_api.hip"]
+           "eden_blocks_grad_f32.hip", "eden_blocks_grad_f16.hip", "eden_blocks_grad_bf16.hip", "eden_blocks_join.hip", "eden_blocks_sums.hip", "eden_blocks_api.hip",
+           "eden_mx4_quantize.hip", "eden_mx4_tiles.hip", "eden_mx4_few.hip", "eden_mx4_api.hip"]
 
 
 def hipcc_path() -> str:

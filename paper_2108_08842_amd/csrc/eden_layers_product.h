@@ -144,6 +144,30 @@ __device__ inline void finish_wave(const Product &p, const f32x16 (&acc)[T][T], 
     }
 }
 
+// The end of four neighbouring columns; BLOCK: eight lanes side by side have the 32 columns from col0 on.
+template <bool BLOCK, uint32_t DTYPE> __device__ inline void finish_quad(const Product &p, uint32_t row, uint32_t col0, uint32_t col, int valid, float (&v)[4]) {
+    if (valid) finish_bias<kForward, DTYPE>(p.finish, col, valid, v);
+    if constexpr (BLOCK)
+        if (p.finish.codes_out) {
+            uint32_t largest = 0;
+            float z[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                z[e] = e < valid ? v[e] : 0.0f;
+                largest = max(largest, magnitude_bits(z[e]));
+            }
+            largest = largest_of_quad(largest);
+            largest = max(largest, (uint32_t)__shfl_xor((int)largest, 4));
+            const uint32_t t = block_exponent(largest);
+            if (row < p.rows) {                                    // (the workgroup has a column: its block exists)
+                const size_t block = (size_t)row * p.finish.blocks + col0 / kBlock;
+                if (col == col0) p.finish.exps_out[block] = (uint8_t)t;
+                *reinterpret_cast<uint32_t *>(p.finish.codes_out + block * kBlock + (col - col0)) = codes4(z, t);
+            }
+        }
+    if (valid) finish_store<kForward, DTYPE>(p.finish, row, col, valid, v);
+}
+
 // Row sums (sums: the product with ones, any of its rows) of row `row`, for one lane of each.
 __device__ inline void finish_row_sum(const Product &p, float sum, uint32_t row, uint32_t split) {
     if (row >= p.rows) return;

@@ -10,7 +10,7 @@
 // One row of bf16 next to 16384 x 4096: 26 us = 5.2 TB/s, what a copy reaches.  7 x 1024 next to 1001 x 1024 in fp32: 6.3 us, a launch, the way of x into the LDS and one
 // of w's rows a wave, one after the other.  16 rows next to 4096 x 4096: 11.1 us = 3.0 TB/s (x comes from the L2 once for every 16 columns: as many bytes as w).
 // 8 rows of fp32 next to 16384 x 4096: 71 us = 3.8 TB/s (x from the LDS for every piece of w; a library's product of 5 to 16 rows takes 52).
-#include "eden_layers_kernels.h"
+#include "eden_layers_product.h"
 
 namespace eden_layers {
 namespace {
@@ -30,30 +30,6 @@ template <uint32_t DTYPE> __device__ inline f32x4 multiply16(u32x4 a, u32x4 b, f
     } else {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
     }
-}
-
-// The end of four neighbouring columns; BLOCK: eight lanes side by side have the 32 columns from col0 on.
-template <bool BLOCK, uint32_t DTYPE> __device__ inline void finish_quad(const Product &p, uint32_t row, uint32_t col0, uint32_t col, int valid, float (&v)[4]) {
-    if (valid) finish_bias<kForward, DTYPE>(p.finish, col, valid, v);
-    if constexpr (BLOCK)
-        if (p.finish.codes_out) {
-            uint32_t largest = 0;
-            float z[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                z[e] = e < valid ? v[e] : 0.0f;
-                largest = max(largest, magnitude_bits(z[e]));
-            }
-            largest = largest_of_quad(largest);
-            largest = max(largest, (uint32_t)__shfl_xor((int)largest, 4));
-            const uint32_t t = block_exponent(largest);
-            if (row < p.rows) {                                    // (the workgroup has a column: its block exists)
-                const size_t block = (size_t)row * p.finish.blocks + col0 / kBlock;
-                if (col == col0) p.finish.exps_out[block] = (uint8_t)t;
-                *reinterpret_cast<uint32_t *>(p.finish.codes_out + block * kBlock + (col - col0)) = codes4(z, t);
-            }
-        }
-    if (valid) finish_store<kForward, DTYPE>(p.finish, row, col, valid, v);
 }
 
 // COLS: sixteens of columns
