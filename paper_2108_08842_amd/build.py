@@ -12,8 +12,9 @@ LIB = os.path.join(PKG, "libeden_hip.so")
 OBJ_DIR = os.path.join(ROOT, "_build")
 SOURCES = ["eden_tables.cpp", "eden_kernels.hip", "eden_kernels_small.hip", "eden_kernels_sparse.hip", "eden_kernels_wg.hip", "eden_kernels_wg_dec.hip", "eden_kernels_lo14.hip", "eden_kernels_lo15.hip", "eden_api.hip",
            "eden_layers_tiles.hip", "eden_layers_direct.hip", "eden_layers_direct_fp32.hip", "eden_layers_rows.hip", "eden_layers_elements.hip", "eden_layers_api.hip",
-           "eden_blocks_grad_f32.hip", "eden_blocks_grad_f16.hip", "eden_blocks_grad_bf16.hip", "eden_blocks_join.hip", "eden_blocks_sums.hip", "eden_blocks_api.hip",
+           "eden_blocks_join.hip", "eden_blocks_sums.hip", "eden_blocks_api.hip",
            "eden_mx4_quantize.hip", "eden_mx4_tiles.hip", "eden_mx4_few.hip", "eden_mx4_api.hip"]
+SOURCES += [f"eden_blocks_grad_{post}_{dtype}.hip" for post in ("norm", "bare", "rms", "layer") for dtype in ("f32", "f16", "bf16")]
 
 
 def hipcc_path() -> str:
@@ -116,7 +117,7 @@ def build(verbose: bool = True, incremental: bool = False) -> str:
     # the .hip sources also leave their device assembly beside the objects (checked below)
     cmds = [common + (["-save-temps=obj"] if s.endswith(".hip") else []) + ["-c", os.path.join(PKG, "csrc", s), "-o", o]
             for s, o in zip(SOURCES, objs) if not incremental or _stale(os.path.join(PKG, "csrc", s), o)]
-    with ThreadPoolExecutor(max(1, len(cmds))) as pool:
+    with ThreadPoolExecutor(max(1, min(len(cmds), 2 * (os.cpu_count() or 1)))) as pool:
         outs = list(pool.map(lambda c: _run(c, verbose), cmds))
     bad = wide_stores_with_scalar_offset()
     if bad:

@@ -33,11 +33,11 @@ bool gates_ok(const void *gate, const void *gate_grad, uint64_t gates, uint64_t 
 }
 
 uint64_t sums_distance(uint64_t cols) { return (cols + 7) / 8 * 8; }
-// Workgroups that share the rows of a gradient: at most `most`, those that the device holds together, and each with some rows.
-Share share_of(uint64_t rows, uint64_t cols, uint64_t gates, uint64_t most) {
-    const int lanes = row_shape((uint32_t)cols).lanes, threads = std::max(64, lanes);
+// Workgroups that share the rows of a gradient: at most `most`, those that the device holds together, and each with some rows.  full: with a branch, post: and a norm behind it.
+Share share_of(uint64_t rows, uint64_t cols, uint64_t gates, bool full, bool post, uint64_t most) {
+    const int lanes = full ? FullGradShape((uint32_t)cols).lanes : GradShape((uint32_t)cols).lanes, threads = std::max(64, lanes);
     const uint64_t rows_each = 4 * (uint64_t)(threads / lanes);
-    uint64_t wanted = std::min<uint64_t>(256 * 1024 / threads, most);
+    const uint64_t wanted = std::min<uint64_t>(256 * (full && (post || cols > 4096) ? lanes == 512 ? 512 : 768 : 1024) / threads, most);
     Share s = {(uint32_t)gates, (uint32_t)(rows / gates), 1, 1, 1};
     if (gates >= wanted || s.group_rows == 0) {
         s.groups_each = (uint32_t)((gates + wanted - 1) / std::max<uint64_t>(wanted, 1));
@@ -47,6 +47,16 @@ Share share_of(uint64_t rows, uint64_t cols, uint64_t gates, uint64_t most) {
         s.workers = s.gates * s.splits;
     }
     return s;
+}
+
+template <uint32_t DTYPE> hipError_t launch_typed(const GradArgs &g, hipStream_t st) {
+    if (!g.a.branch) return launch_block_grad<DTYPE, -1>(g, st);
+    if (g.a.post.kind == EDEN_NORM_NONE) return launch_block_grad<DTYPE, EDEN_NORM_NONE>(g, st);
+    return g.a.post.kind == EDEN_NORM_RMS ? launch_block_grad<DTYPE, EDEN_NORM_RMS>(g, st) : launch_block_grad<DTYPE, EDEN_NORM_LAYER>(g, st);
+}
+hipError_t launch_grad(const GradArgs &g, hipStream_t st) {
+    if (!g.a.branch && g.a.dh == nullptr) return hipSuccess;
+    return g.a.dtype == EDEN_F32 ? launch_typed<EDEN_F32>(g, st) : g.a.dtype == EDEN_F16 ? launch_typed<EDEN_F16>(g, st) : launch_typed<EDEN_BF16>(g, st);
 }
 
 }  // namespace
@@ -81,7 +91,7 @@ size_t eden_join_workspace_bytes(uint64_t rows, uint64_t cols, uint64_t gates, u
     if (!known_type(dtype) || !sizes_ok(rows, cols) || rows == 0 || cols == 0) return 0;
     if (gates < 1) gates = 1;
     if (gates > rows || rows % gates) return 0;
-    const uint64_t workers = share_of(rows, cols, gates, ~0ull).workers;
+    const uint64_t workers = std::max(share_of(rows, cols, gates, false, false, ~0ull).workers, share_of(rows, cols, gates, true, false, ~0ull).workers);
     return workers > 1 ? workers * kAllSums * sums_distance(cols) * sizeof(float) : 0;
 }
 
@@ -118,7 +128,7 @@ int eden_join_grad(const eden_join_grad_args *args, void *stream) {
     }
     if (!a.dx && !a.df && count == 0) return EDEN_OK;
     const uint64_t ld = sums_distance(a.cols), room = a.workspace ? a.workspace_bytes / (sizeof(float) * ld) : 0;
-    g.share = share_of(a.rows, a.cols, a.gates, count ? std::max<uint64_t>(1, room / count) : ~0ull);
+    g.share = share_of(a.rows, a.cols, a.gates, a.branch, post, count ? std::max<uint64_t>(1, room / count) : ~0ull);
     g.ld_sums = ld;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const bool parts = g.share.workers > 1;
@@ -127,6 +137,14 @@ int eden_join_grad(const eden_join_grad_args *args, void *stream) {
     float *space = static_cast<float *>(a.workspace);
     for (int s = 0; s < kAllSums; ++s) {
         g.sums[s] = sums[s];
+        if (sums[s] && (s == kPreWeight || s == kPreBias) && a.dh == nullptr) {
+            // without dh they are sums over nothing, and the kernel has no place for them
+            g.sums[s] = nullptr;
+            add.of[add.count] = {space, sums[s]};
+            add.rows[add.count] = 1;
+            ++add.count;
+            continue;
+        }
         if (!sums[s] || !parts || (s == kGateSum && g.share.splits == 1)) continue;
         g.sums[s] = space;
         const bool gate = s == kGateSum;
@@ -137,7 +155,7 @@ int eden_join_grad(const eden_join_grad_args *args, void *stream) {
         ++add.count;
         space += g.share.workers * ld;
     }
-    hipError_t err = a.dtype == EDEN_F32 ? launch_block_grad<EDEN_F32>(g, st) : a.dtype == EDEN_F16 ? launch_block_grad<EDEN_F16>(g, st) : launch_block_grad<EDEN_BF16>(g, st);
+    hipError_t err = launch_grad(g, st);
     if (err == hipSuccess && add.count) err = launch_sums(add, st);
     return status(err);
 }

@@ -1,4 +1,4 @@
-// The gradients of a residual block's join (included by one source for each type).
+// The gradients of a residual block's join (included by one source for each type and kind of norm behind the branch).
 //
 //   d = dr + rho_r (g - [mean g] - n mean(g n)), g = dh w_pre, n = (r - [mean r]) rho_r               brackets: layer norms
 //   dx = x_scale d
@@ -14,34 +14,58 @@
 namespace eden_layers {
 namespace {
 
-constexpr int bit(int sum) { return 1 << sum; }
+// waves of a SIMD that the registers are shared out to
+constexpr int waves_of(int lanes, int chunks, int post) { return post < 0 || (post == 0 && chunks == 1) ? 4 : lanes == 512 ? 2 : 3; }
 
-template <uint32_t DTYPE, int LANES, int CHUNKS, int SUMS>
-__global__ __launch_bounds__(LANES > 64 ? LANES : 64) void k_block_grad(const GradArgs args) {
+// The operands of a row as they lie in memory
+template <uint32_t DTYPE, int CHUNKS> struct RowOperands {
+    Eight<DTYPE> r[CHUNKS], f[CHUNKS], dh[CHUNKS], dr[CHUNKS];
+};
+
+// PRE, POST: kinds of the norms; POST -1: no branch
+template <uint32_t DTYPE, int LANES, int CHUNKS, bool RAGGED, int PRE, int POST>
+__global__ __launch_bounds__(LANES > 64 ? LANES : 64) __attribute__((amdgpu_waves_per_eu(waves_of(LANES, CHUNKS, POST)))) void k_block_grad(const GradArgs args) {
     constexpr int kThreads = LANES > 64 ? LANES : 64, kRows = kThreads / LANES;
+    constexpr bool kHeld = CHUNKS * sizeof(typename Elem<DTYPE>::type) <= (POST == EDEN_NORM_LAYER ? 2 : 4);       // weights stay in registers, and the next row's operands come while one is worked on
+    constexpr bool kPacked = sizeof(typename Elem<DTYPE>::type) == 2 && (waves_of(LANES, CHUNKS, POST) == 4 || (CHUNKS == 2 && POST == EDEN_NORM_LAYER));
+    constexpr bool kPre = PRE != EDEN_NORM_NONE, kPreLayer = PRE == EDEN_NORM_LAYER, kBranch = POST >= 0, kPost = POST > 0, kPostLayer = POST == EDEN_NORM_LAYER;
+    constexpr bool kHas[kAllSums] = {kBranch, kPost, kPostLayer, kPre, kPreLayer};
     __shared__ float shared[kSumFloats<LANES>];
     int turn = 0;
     const eden_join_grad_args &a = args.a;
+    typedef const __attribute__((address_space(4))) GradArgs *Arguments;
     const Share &share = args.share;
-    const uint32_t cols = (uint32_t)a.cols, lane = threadIdx.x % LANES, worker = blockIdx.x;
-    const uint64_t key = a.random.threshold ? key_of(a.random, eden::kStreamDropout) : 0;
-    const float each = 1.0f / (float)cols, kept = kept_scale(a.random.threshold);
-    const bool pre = a.dh != nullptr, post = a.post.kind != EDEN_NORM_NONE, pre_layer = a.pre.kind == EDEN_NORM_LAYER, post_layer = a.post.kind == EDEN_NORM_LAYER;
+    const uint32_t cols = (uint32_t)a.cols, worker = blockIdx.x, sub = row_in_group<LANES>();
+    const RowPlace<DTYPE, LANES, CHUNKS, RAGGED> place(cols, threadIdx.x % LANES);
+    const uint64_t key = kBranch && a.random.threshold ? key_of(a.random, eden::kStreamDropout) : 0;
+    const float each = 1.0f / (float)cols, scale = a.scale * kept_scale(a.random.threshold);
 
-    uint32_t columns[CHUNKS];                                      // valid ones
-    Eight<DTYPE> pre_weight[CHUNKS], post_weight[CHUNKS], post_bias[CHUNKS];
+    // The arguments again, from memory: kept, all of them would take more scalar registers than there are
+    auto again = [] {
+        Arguments k = (Arguments)__builtin_amdgcn_kernarg_segment_ptr();
+        asm volatile("" : "+s"(k));
+        return k;
+    };
+    auto weights_of = [&](const void *p, int c, float fill) {
+        Eight<DTYPE> w;
+        w.fill(fill);
+        if (p) place.load(w, p, c), place.settle(w, c, true);
+        return w;
+    };
+    Eight<DTYPE> held_pre[CHUNKS], held_post[CHUNKS], held_post_bias[CHUNKS], held_gate[CHUNKS];
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
-        const uint32_t col = (c * LANES + lane) * 8;
-        columns[c] = col < cols ? min(8u, cols - col) : 0;
-        if (a.pre.weight) pre_weight[c].load(a.pre.weight, col, columns[c]);
-        if (a.post.weight) post_weight[c].load(a.post.weight, col, columns[c]);
-        if (a.post.bias) post_bias[c].load(a.post.bias, col, columns[c]);
+        if constexpr (kHeld && kPre) held_pre[c] = weights_of(a.pre.weight, c, 1.0f);
+        if constexpr (kHeld && kPost) held_post[c] = weights_of(a.post.weight, c, 1.0f);
+        if constexpr (kHeld && kPostLayer) held_post_bias[c] = weights_of(a.post.bias, c, 0.0f);
     }
+    auto pre_weight = [&](int c) { return kHeld ? held_pre[c] : weights_of(a.pre.weight, c, 1.0f); };
+    auto post_weight = [&](int c) { return kHeld ? held_post[c] : weights_of(a.post.weight, c, 1.0f); };
+    auto post_bias = [&](int c) { return kHeld ? held_post_bias[c] : weights_of(a.post.bias, c, 0.0f); };
     float sums[kAllSums][CHUNKS][8] = {};
 
     // one result's or one part's sums
-    auto put = [&](int which, float (&v)[CHUNKS][8], float *to, bool add) {
+    auto put = [&](float (&v)[CHUNKS][8], float *to, bool add) {
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
 #pragma unroll
@@ -49,13 +73,13 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) void k_block_grad(const Gr
 #pragma unroll
                 for (int d = LANES; d < 64; d *= 2) v[c][i] += __shfl_xor(v[c][i], d);
             }
-            if (threadIdx.x < LANES && columns[c]) {
-                float *at = to + (c * LANES + lane) * 8;
+            if (threadIdx.x < LANES && place.valid[c]) {
+                float *at = to + place.col[c];
                 Vec<float, 8> out;
-                if (add) out = load_some<float, 8>(at, columns[c]);
+                if (add) out = load_some<float, 8>(at, place.valid[c]);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) out.v[i] = add ? out.v[i] + v[c][i] : v[c][i];
-                store_some<float, 8>(at, out, columns[c]);
+                store_some<float, 8>(at, out, place.valid[c]);
             }
         }
     };
@@ -63,138 +87,191 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) void k_block_grad(const Gr
     const uint32_t first_group = share.splits > 1 ? worker / share.splits : worker * share.groups_each;
     const uint32_t end_group = share.splits > 1 ? first_group + 1 : min(share.gates, first_group + share.groups_each);
     const uint32_t split = share.splits > 1 ? worker % share.splits : 0, split_rows = (share.group_rows + share.splits - 1) / share.splits;
+    const uint32_t from = min(split * split_rows, share.group_rows), to = min(from + split_rows, share.group_rows);
     for (uint32_t group = first_group; group < end_group; ++group) {
-        const uint32_t from = min(split * split_rows, share.group_rows), to = min(from + split_rows, share.group_rows);
         const uint64_t group_row = (uint64_t)group * share.group_rows;
-        Eight<DTYPE> gate[CHUNKS];
-        if (a.gate) {
+        auto gate_of = [&](int c) { return weights_of(a.gate ? row_of<DTYPE, LANES>(a.gate, group, a.ld_gate) : nullptr, c, 1.0f); };
+        auto gate = [&](int c) { return kHeld ? held_gate[c] : gate_of(c); };
 #pragma unroll
-            for (int c = 0; c < CHUNKS; ++c) gate[c].load(row_of<DTYPE>(a.gate, group, a.ld_gate), (c * LANES + lane) * 8, columns[c]);
-        }
-        for (uint32_t at = from; at < to; at += kRows) {
-            const bool has = at + threadIdx.x / LANES < to;
-            const uint64_t row = group_row + at + (has ? threadIdx.x / LANES : 0);
-            Eight<DTYPE> r8[CHUNKS], f8[CHUNKS], dh8[CHUNKS], dr8[CHUNKS];
-            int valid[CHUNKS];
+        for (int c = 0; c < CHUNKS; ++c)
+            if constexpr (kHeld && kBranch) held_gate[c] = gate_of(c);
+        auto row_at = [&](uint32_t at) { return group_row + (kRows == 1 || at + sub < to ? at + sub : from); };
+        auto load = [&](RowOperands<DTYPE, CHUNKS> &row8, uint32_t at) {
+            const Arguments k = again();
+            const uint64_t row = row_at(at);
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c) {
-                const uint32_t col = (c * LANES + lane) * 8;
-                valid[c] = has ? columns[c] : 0;
-                if (pre) r8[c].load(row_of<DTYPE>(a.r, row, a.ldr), col, valid[c]);
-                if (pre) dh8[c].load(row_of<DTYPE>(a.dh, row, a.lddh), col, valid[c]);
-                if (a.dr) dr8[c].load(row_of<DTYPE>(a.dr, row, a.lddr), col, valid[c]);
-                if (args.needs_f) f8[c].load(row_of<DTYPE>(a.f, row, a.ldf), col, valid[c]);
+                if constexpr (kPre) {
+                    place.load(row8.r[c], row_of<DTYPE, LANES>(k->a.r, row, k->a.ldr), c);
+                    place.load(row8.dh[c], row_of<DTYPE, LANES>(k->a.dh, row, k->a.lddh), c);
+                }
+                if (k->a.dr) place.load(row8.dr[c], row_of<DTYPE, LANES>(k->a.dr, row, k->a.lddr), c);
+                if (kBranch && k->needs_f) place.load(row8.f[c], row_of<DTYPE, LANES>(k->a.f, row, k->a.ldf), c);
             }
-            float n[CHUNKS][8], u[CHUNKS][8], d[CHUNKS][8];
+        };
+        RowOperands<DTYPE, CHUNKS> now = {}, next = {};
+        if (kHeld && from < to) load(now, from);
+        for (uint32_t at = from; at < to; at += kRows) {
+            if constexpr (kHeld) {
+                if (at + kRows < to) load(next, at + kRows);
+            } else {
+                load(now, at);
+            }
+            const bool has = kRows == 1 || at + sub < to;
+            const Arguments k = again();
+            const uint64_t row = row_at(at);
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c) {
+                if constexpr (kPre) place.settle(now.r[c], c, has), place.settle(now.dh[c], c, has);
+                if (k->a.dr) place.settle(now.dr[c], c, has);
+                if (kBranch && k->needs_f) place.settle(now.f[c], c, has);
+            }
+            auto stay_packed = [&] {
+                if constexpr (kPacked) {
+#pragma unroll
+                    for (int c = 0; c < CHUNKS; ++c) {
+                        if constexpr (kPre) now.r[c].stay_packed(), now.dh[c].stay_packed();
+                        if constexpr (kBranch) now.f[c].stay_packed();
+                        if constexpr (kPre && kHeld) held_pre[c].stay_packed();
+                        if constexpr (kPost && kHeld) held_post[c].stay_packed();
+                        if constexpr (kPostLayer && kHeld) held_post_bias[c].stay_packed();
+                        if constexpr (kBranch && kHeld) held_gate[c].stay_packed();
+                    }
+                }
+            };
+            stay_packed();
+            auto inside = [&](int c, int i) { return has && place.inside(c, i); };
+            // means of layer norms, then sums of squares and of products with r around them
+            float three[3], mean_r = 0.0f, mean_f = 0.0f, mean_g = 0.0f;
+            if constexpr (kPreLayer || kPostLayer) {
+                three[0] = three[1] = three[2] = 0.0f;
+#pragma unroll
+                for (int c = 0; c < CHUNKS; ++c) {
+                    Eight<DTYPE> w;
+                    if constexpr (kPreLayer) w = pre_weight(c);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        if constexpr (kPreLayer) three[0] += now.r[c][i], three[2] = __builtin_fmaf(now.dh[c][i], w[i], three[2]);
+                        if constexpr (kPostLayer) three[1] += now.f[c][i];
+                    }
+                }
+                stay_packed();
+                sum_in_row<LANES>(three, shared, turn);
+                if constexpr (kPreLayer) mean_r = three[0] * each, mean_g = three[2] * each;
+                if constexpr (kPostLayer) mean_f = three[1] * each;
+            }
+            float rho_r = 0.0f, rho_f = 0.0f, inner = 0.0f;
+            if constexpr (kPre || kPost) {
+                three[0] = three[1] = three[2] = 0.0f;
+#pragma unroll
+                for (int c = 0; c < CHUNKS; ++c) {
+                    Eight<DTYPE> w;
+                    if constexpr (kPre) w = pre_weight(c);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        if constexpr (kPre) {
+                            const float n = kPreLayer && !inside(c, i) ? 0.0f : now.r[c][i] - mean_r;
+                            three[0] = __builtin_fmaf(n, n, three[0]);
+                            three[2] = __builtin_fmaf(now.dh[c][i] * w[i], n, three[2]);
+                        }
+                        if constexpr (kPost) {
+                            const float u = kPostLayer && !inside(c, i) ? 0.0f : now.f[c][i] - mean_f;
+                            three[1] = __builtin_fmaf(u, u, three[1]);
+                        }
+                    }
+                }
+                stay_packed();
+                sum_in_row<LANES>(three, shared, turn);
+                if (has) rho_r = rsqrtf(three[0] * each + k->a.pre.eps), rho_f = rsqrtf(three[1] * each + k->a.post.eps);       // (of rows that are none, 0 times 0 and not times 1 / 0)
+                inner = three[2] * rho_r * each;
+            }
+            float d[CHUNKS][8];
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    n[c][i] = pre ? r8[c][i] : 0.0f;
-                    u[c][i] = args.needs_f ? f8[c][i] : 0.0f;
-                    d[c][i] = a.dr ? dr8[c][i] : 0.0f;
+                for (int i = 0; i < 8; ++i) d[c][i] = now.dr[c][i];
+            if constexpr (kPre) {
+                // rho (g - mean_g - n rho inner), n = r - mean_r
+                const float c0 = -rho_r * mean_g, c1 = -rho_r * rho_r * inner;
+#pragma unroll
+                for (int c = 0; c < CHUNKS; ++c) {
+                    const Eight<DTYPE> w = pre_weight(c);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float dh = now.dh[c][i], n = now.r[c][i] - mean_r;
+                        sums[kPreWeight][c][i] = __builtin_fmaf(dh, n * rho_r, sums[kPreWeight][c][i]);
+                        if constexpr (kPreLayer) sums[kPreBias][c][i] += dh;
+                        d[c][i] += __builtin_fmaf(rho_r, dh * w[i], kPreLayer ? __builtin_fmaf(c1, n, c0) : c1 * n);
+                        if (kPacked && i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+                    }
                 }
-            float two[2];
-            if (pre_layer || post_layer) {
-                two[0] = two[1] = 0.0f;
-#pragma unroll
-                for (int c = 0; c < CHUNKS; ++c)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) two[0] += n[c][i], two[1] += u[c][i];
-                sum_in_row<LANES>(two, shared, turn);
-                const float mean_r = pre_layer ? two[0] * each : 0.0f, mean_f = post_layer ? two[1] * each : 0.0f;
-#pragma unroll
-                for (int c = 0; c < CHUNKS; ++c)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        n[c][i] = i < valid[c] ? n[c][i] - mean_r : 0.0f;
-                        u[c][i] = i < valid[c] ? u[c][i] - mean_f : 0.0f;
-                    }
             }
-            float rho_r = 0.0f, rho_f = 0.0f;
-            if (pre || post) {
-                two[0] = two[1] = 0.0f;
-#pragma unroll
-                for (int c = 0; c < CHUNKS; ++c)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) two[0] = __builtin_fmaf(n[c][i], n[c][i], two[0]), two[1] = __builtin_fmaf(u[c][i], u[c][i], two[1]);
-                sum_in_row<LANES>(two, shared, turn);
-                if (has) rho_r = rsqrtf(two[0] * each + a.pre.eps), rho_f = rsqrtf(two[1] * each + a.post.eps);       // (of rows that are none, 0 times 0 and not times 1 / 0)
-            }
-            if (pre) {
-                float g[CHUNKS][8];
-                two[0] = two[1] = 0.0f;
-#pragma unroll
-                for (int c = 0; c < CHUNKS; ++c)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float dh = dh8[c][i];
-                        n[c][i] *= rho_r;
-                        if constexpr (SUMS & bit(kPreWeight)) sums[kPreWeight][c][i] = __builtin_fmaf(dh, n[c][i], sums[kPreWeight][c][i]);
-                        if constexpr (SUMS & bit(kPreBias)) sums[kPreBias][c][i] += dh;
-                        g[c][i] = a.pre.weight ? dh * pre_weight[c][i] : dh;
-                        two[0] += g[c][i], two[1] = __builtin_fmaf(g[c][i], n[c][i], two[1]);
-                    }
-                sum_in_row<LANES>(two, shared, turn);
-                const float c0 = pre_layer ? -rho_r * (two[0] * each) : 0.0f, c1 = -rho_r * (two[1] * each);
-#pragma unroll
-                for (int c = 0; c < CHUNKS; ++c)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) d[c][i] += __builtin_fmaf(rho_r, g[c][i], __builtin_fmaf(c1, n[c][i], c0));
-            }
-            if (a.dx) {
+            if (k->a.dx) {
 #pragma unroll
                 for (int c = 0; c < CHUNKS; ++c) {
                     float to8[8];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) to8[i] = a.x_scale * d[c][i];
-                    if (valid[c]) store_eight<DTYPE>(row_of<DTYPE>(a.dx, row, a.lddx), (c * LANES + lane) * 8, to8, valid[c]);
+                    for (int i = 0; i < 8; ++i) to8[i] = k->a.x_scale * d[c][i];
+                    if (has) place.store(row_of<DTYPE, LANES>(k->a.dx, row, k->a.lddx), c, to8);
                 }
             }
-            if (!a.branch) continue;
-            const float scale = a.scale * kept;
-            two[0] = two[1] = 0.0f;
+            if constexpr (kBranch) {
+                float two[2] = {0.0f, 0.0f};
+                {
+                    constexpr bool DROP = true;
 #pragma unroll
-            for (int c = 0; c < CHUNKS; ++c) {
-                const uint32_t col = (c * LANES + lane) * 8;
-                Bits8 bits = {};
-                if (a.random.threshold) bits = bits_of(key, row * words_of(cols) + col / 4);
+                    for (int c = 0; c < CHUNKS; ++c) {
+                        Bits8 bits = {};
+                        if (k->a.random.threshold) bits = bits_of(key, row * words_of(cols) + place.col[c] / 4);
+                        Eight<DTYPE> w, b;
+                        if constexpr (kPost) w = post_weight(c);
+                        if constexpr (kPostLayer) b = post_bias(c);
+                        const Eight<DTYPE> g = gate(c);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const bool keep = i < valid[c] && bits.of(i) >= a.random.threshold;      // (behind a row's end d is what a layer norm took out)
-                    if (post) u[c][i] *= rho_f;
-                    d[c][i] = keep ? scale * d[c][i] : 0.0f;
-                    if constexpr (SUMS & bit(kGateSum)) {
-                        float v = u[c][i];
-                        if (a.post.weight) v *= post_weight[c][i];
-                        if (a.post.bias) v += post_bias[c][i];
-                        sums[kGateSum][c][i] += keep ? d[c][i] * v : 0.0f;       // (what is dropped may be anything)
+                        for (int i = 0; i < 8; ++i) {
+                            // behind a row's end d is what a layer norm took out; what is dropped may be anything
+                            const bool keep = (!kPreLayer || inside(c, i)) && (!DROP || bits.of(i) >= k->a.random.threshold);
+                            const float u = kPost ? (now.f[c][i] - mean_f) * rho_f : now.f[c][i];
+                            const float v = kPostLayer ? __builtin_fmaf(u, w[i], b[i]) : kPost ? u * w[i] : u;
+                            const float back = !DROP && !kPreLayer ? scale * d[c][i] : keep ? scale * d[c][i] : 0.0f;
+                            sums[kGateSum][c][i] = __builtin_fmaf(back, DROP && !keep ? 0.0f : v, sums[kGateSum][c][i]);
+                            const float du = DROP && !keep ? 0.0f : back * g[i];
+                            if constexpr (kPost) {
+                                sums[kPostWeight][c][i] = __builtin_fmaf(du, u, sums[kPostWeight][c][i]);
+                                if constexpr (kPostLayer) sums[kPostBias][c][i] += du;
+                                d[c][i] = du * w[i];
+                                if constexpr (kPostLayer) two[0] += d[c][i];
+                                two[1] = __builtin_fmaf(d[c][i], u, two[1]);
+                            } else {
+                                d[c][i] = du;
+                            }
+                            if (kPacked && i % 2 == 1) __builtin_amdgcn_sched_barrier(0);       // (all eight side by side would take too many registers)
+                        }
                     }
-                    if (a.gate) d[c][i] = keep ? d[c][i] * gate[c][i] : 0.0f;
-                    if constexpr (SUMS & bit(kPostWeight)) sums[kPostWeight][c][i] = __builtin_fmaf(d[c][i], u[c][i], sums[kPostWeight][c][i]);
-                    if constexpr (SUMS & bit(kPostBias)) sums[kPostBias][c][i] += d[c][i];
-                    if (a.post.weight) d[c][i] *= post_weight[c][i];
-                    two[0] += d[c][i], two[1] = __builtin_fmaf(d[c][i], u[c][i], two[1]);
+                }
+                if (k->a.df) {
+                    if constexpr (kPost) {
+                        stay_packed();
+                        sum_in_row<LANES>(two, shared, turn);
+                        const float c0 = -rho_f * (two[0] * each), c1 = -rho_f * rho_f * (two[1] * each);
+#pragma unroll
+                        for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                const float u = now.f[c][i] - mean_f;
+                                d[c][i] = __builtin_fmaf(rho_f, d[c][i], kPostLayer ? __builtin_fmaf(c1, u, c0) : c1 * u);
+                            }
+                    }
+#pragma unroll
+                    for (int c = 0; c < CHUNKS; ++c)
+                        if (has) place.store(row_of<DTYPE, LANES>(k->a.df, row, k->a.lddf), c, d[c]);
                 }
             }
-            if (!a.df) continue;
-            float c0 = 0.0f, c1 = 0.0f;
-            if (post) {
-                sum_in_row<LANES>(two, shared, turn);
-                c0 = post_layer ? -rho_f * (two[0] * each) : 0.0f, c1 = -rho_f * (two[1] * each);
-            }
-#pragma unroll
-            for (int c = 0; c < CHUNKS; ++c) {
-                if (post) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) d[c][i] = __builtin_fmaf(rho_f, d[c][i], __builtin_fmaf(c1, u[c][i], c0));
-                }
-                if (valid[c]) store_eight<DTYPE>(row_of<DTYPE>(a.df, row, a.lddf), (c * LANES + lane) * 8, d[c], valid[c]);
-            }
+            if constexpr (kHeld) now = next;
         }
-        if constexpr (SUMS & bit(kGateSum))
+        if constexpr (kBranch)
             if (args.sums[kGateSum] && share.splits == 1) {
-                put(kGateSum, sums[kGateSum], args.sums[kGateSum] + group * a.ld_gate_grad, a.accumulate);
+                put(sums[kGateSum], args.sums[kGateSum] + group * a.ld_gate_grad, a.accumulate);
 #pragma unroll
                 for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
@@ -204,25 +281,24 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) void k_block_grad(const Gr
     const bool parts = share.workers > 1;
 #pragma unroll
     for (int s = 0; s < kAllSums; ++s) {
-        if (!(SUMS >> s & 1) || !args.sums[s] || (s == kGateSum && share.splits == 1)) continue;
-        put(s, sums[s], args.sums[s] + (parts ? worker * args.ld_sums : 0), !parts && a.accumulate);
+        if (!kHas[s] || !args.sums[s] || (s == kGateSum && share.splits == 1)) continue;
+        put(sums[s], args.sums[s] + (parts ? worker * args.ld_sums : 0), !parts && a.accumulate);
     }
 }
 
 }  // namespace
 
-template <uint32_t DTYPE> hipError_t launch_block_grad(const GradArgs &args, hipStream_t st) {
-    int wanted = 0;
-    for (int s = 0; s < kAllSums; ++s) wanted |= args.sums[s] ? bit(s) : 0;
-    for_shape(row_shape((uint32_t)args.a.cols), [&](auto lanes, auto chunks) {
-        constexpr int LANES = decltype(lanes)::value, CHUNKS = decltype(chunks)::value;
-        auto with = [&](auto sums) { k_block_grad<DTYPE, LANES, CHUNKS, decltype(sums)::value><<<args.share.workers, LANES > 64 ? LANES : 64, 0, st>>>(args); };
-        constexpr int kPre = bit(kPreWeight), kPreBoth = kPre | bit(kPreBias), kGates = kPre | bit(kGateSum), kRms = kGates | bit(kPostWeight), kAll = bit(kAllSums) - 1;
-        if ((wanted & ~kPre) == 0) with(std::integral_constant<int, kPre>());
-        else if ((wanted & ~kPreBoth) == 0) with(std::integral_constant<int, kPreBoth>());
-        else if ((wanted & ~kGates) == 0) with(std::integral_constant<int, kGates>());
-        else if ((wanted & ~kRms) == 0) with(std::integral_constant<int, kRms>());
-        else with(std::integral_constant<int, kAll>());
+template <uint32_t DTYPE, int POST> hipError_t launch_block_grad(const GradArgs &args, hipStream_t st) {
+    std::conditional_t<(POST >= 0), FullGradShape, GradShape>((uint32_t)args.a.cols).use((uint32_t)args.a.cols, [&](auto lanes, auto chunks, auto ragged) {
+        constexpr int LANES = decltype(lanes)::value, CHUNKS = decltype(chunks)::value, kThreads = LANES > 64 ? LANES : 64;
+        constexpr bool RAGGED = decltype(ragged)::value;
+        if (args.a.dh == nullptr) {
+            if constexpr (POST >= 0) k_block_grad<DTYPE, LANES, CHUNKS, RAGGED, EDEN_NORM_NONE, POST><<<args.share.workers, kThreads, 0, st>>>(args);
+        } else if (args.a.pre.kind == EDEN_NORM_RMS) {
+            k_block_grad<DTYPE, LANES, CHUNKS, RAGGED, EDEN_NORM_RMS, POST><<<args.share.workers, kThreads, 0, st>>>(args);
+        } else {
+            k_block_grad<DTYPE, LANES, CHUNKS, RAGGED, EDEN_NORM_LAYER, POST><<<args.share.workers, kThreads, 0, st>>>(args);
+        }
     });
     return hipGetLastError();
 }

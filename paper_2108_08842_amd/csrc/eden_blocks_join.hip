@@ -26,8 +26,8 @@ __global__ __launch_bounds__(kSpreadThreads) void k_dropout(const typename Elem<
 }
 
 // Takes the mean (layer) and the size out of a row.  Behind the row's end its values are zeros, and stay so.
-template <int LANES, int CHUNKS>
-__device__ inline void standardise(float (&v)[CHUNKS][8], const eden_norm &norm, uint32_t cols, const int (&valid)[CHUNKS], float *shared, int &turn) {
+template <int LANES, int CHUNKS, class P>
+__device__ inline void standardise(float (&v)[CHUNKS][8], const eden_norm &norm, uint32_t cols, const P &place, float *shared, int &turn) {
     const float each = 1.0f / (float)cols;
     if (norm.kind == EDEN_NORM_LAYER) {
         float sum[1] = {0.0f};
@@ -40,7 +40,7 @@ __device__ inline void standardise(float (&v)[CHUNKS][8], const eden_norm &norm,
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[c][i] = i < valid[c] ? v[c][i] - mean : 0.0f;
+            for (int i = 0; i < 8; ++i) v[c][i] = place.inside(c, i) ? v[c][i] - mean : 0.0f;
     }
     float sum[1] = {0.0f};
 #pragma unroll
@@ -54,85 +54,111 @@ __device__ inline void standardise(float (&v)[CHUNKS][8], const eden_norm &norm,
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[c][i] *= scale;
 }
-template <uint32_t DTYPE> __device__ inline void weigh(float (&v)[8], const eden_norm &norm, uint32_t col, int valid) {
-    Eight<DTYPE> w;
-    if (norm.weight) {
-        w.load(norm.weight, col, valid);
+
+// A norm's weights and biases in the lane's columns
+template <uint32_t DTYPE, int CHUNKS> struct Weights {
+    Eight<DTYPE> weight[CHUNKS], bias[CHUNKS];
+    template <class P> __device__ void load(const eden_norm &norm, const P &place) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] *= w[i];
+        for (int c = 0; c < CHUNKS; ++c) {
+            if (norm.weight) place.load(weight[c], norm.weight, c);
+            if (norm.bias) place.load(bias[c], norm.bias, c);
+        }
     }
-    if (norm.bias) {
-        w.load(norm.bias, col, valid);
+    template <class P> __device__ void apply(float (&v)[CHUNKS][8], const eden_norm &norm, const P &place) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += w[i];
+        for (int c = 0; c < CHUNKS; ++c) {
+            if (norm.weight) {
+                place.settle(weight[c], c, true);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[c][i] *= weight[c][i];
+            }
+            if (norm.bias) {
+                place.settle(bias[c], c, true);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[c][i] += bias[c][i];
+            }
+        }
     }
+};
+
+// Waves of a SIMD: rows of up to a wave's eights need few registers, and nothing but other waves hides their loads
+template <uint32_t DTYPE> constexpr int waves_of(int lanes, int chunks, bool branch) {
+    return lanes == 1024 ? 4 : (DTYPE == EDEN_F32 ? 4 : branch ? 6 : 8) / (chunks == 2 ? 2 : 1);
 }
 
-template <uint32_t DTYPE, int LANES, int CHUNKS> __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void k_block_join(const eden_join_args a) {
+template <uint32_t DTYPE, int LANES, int CHUNKS, bool RAGGED, bool BRANCH>
+__global__ __launch_bounds__(LANES > 64 ? LANES : 256) __attribute__((amdgpu_waves_per_eu(waves_of<DTYPE>(LANES, CHUNKS, BRANCH)))) void k_block_join(const eden_join_args a) {
     constexpr int kThreads = LANES > 64 ? LANES : 256, kRows = kThreads / LANES;          // (rows of up to a wave: their waves do not meet)
     __shared__ float shared[kSumFloats<LANES>];
     int turn = 0;
-    const uint32_t rows = (uint32_t)a.rows, cols = (uint32_t)a.cols, lane = threadIdx.x % LANES, step = gridDim.x * kRows;
-    const uint64_t key = a.random.threshold ? key_of(a.random, eden::kStreamDropout) : 0;
+    const uint32_t rows = (uint32_t)a.rows, cols = (uint32_t)a.cols, step = gridDim.x * kRows, sub = row_in_group<LANES>();
+    const RowPlace<DTYPE, LANES, CHUNKS, RAGGED> place(cols, threadIdx.x % LANES);
+    const uint64_t key = BRANCH && a.random.threshold ? key_of(a.random, eden::kStreamDropout) : 0;
     const uint32_t gate_rows = a.gates > 1 ? rows / (uint32_t)a.gates : rows;
+    const float scale = a.scale * kept_scale(a.random.threshold);
+    const bool post = a.post.kind != EDEN_NORM_NONE, pre = a.pre.kind != EDEN_NORM_NONE;
     for (uint64_t first = (uint64_t)blockIdx.x * kRows; first < rows; first += step) {
-        const uint32_t row = (uint32_t)first + threadIdx.x / LANES;
-        int valid[CHUNKS];
-        float r[CHUNKS][8], f[CHUNKS][8];
-        Eight<DTYPE> x8[CHUNKS], f8[CHUNKS];
+        const bool has = first + sub < rows;
+        const uint32_t row = (uint32_t)(has ? first + sub : first);
+        float r[CHUNKS][8];
+        Eight<DTYPE> x8[CHUNKS], f8[CHUNKS], gate8[CHUNKS];
+        Weights<DTYPE, CHUNKS> weights;
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
-            const uint32_t col = (c * LANES + lane) * 8;
-            valid[c] = row < rows && col < cols ? (int)min(8u, cols - col) : 0;
-            x8[c].load(row_of<DTYPE>(a.x, row, a.ldx), col, valid[c]);
-            if (a.f) f8[c].load(row_of<DTYPE>(a.f, row, a.ldf), col, valid[c]);
+            if constexpr (BRANCH) place.load(f8[c], row_of<DTYPE, LANES>(a.f, row, a.ldf), c);
+            place.load(x8[c], row_of<DTYPE, LANES>(a.x, row, a.ldx), c);
         }
-#pragma unroll
-        for (int c = 0; c < CHUNKS; ++c)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) r[c][i] = x8[c][i];
-        if (a.f) {
-#pragma unroll
-            for (int c = 0; c < CHUNKS; ++c)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) f[c][i] = f8[c][i];
-            if (a.post.kind != EDEN_NORM_NONE) {
-                standardise<LANES>(f, a.post, cols, valid, shared, turn);
-#pragma unroll
-                for (int c = 0; c < CHUNKS; ++c) weigh<DTYPE>(f[c], a.post, (c * LANES + lane) * 8, valid[c]);
-            }
-            if (a.gate) {
-                const void *gate = row_of<DTYPE>(a.gate, row < rows ? row / gate_rows : 0, a.ld_gate);
-#pragma unroll
-                for (int c = 0; c < CHUNKS; ++c) {
-                    Eight<DTYPE> g;
-                    g.load(gate, (c * LANES + lane) * 8, valid[c]);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) f[c][i] *= g[i];
-                }
-            }
-            const float scale = a.scale * kept_scale(a.random.threshold);
+        if constexpr (!BRANCH) {
+            weights.load(a.pre, place);
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c) {
-                const uint32_t col = (c * LANES + lane) * 8;
+                place.settle(x8[c], c, has);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) r[c][i] = x8[c][i];
+            }
+        } else {
+            float f[CHUNKS][8];
+            if (post) weights.load(a.post, place);
+            if (a.gate) {
+#pragma unroll
+                for (int c = 0; c < CHUNKS; ++c) place.load(gate8[c], row_of<DTYPE, LANES>(a.gate, row / gate_rows, a.ld_gate), c);
+            }
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c) {
+                place.settle(f8[c], c, has);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[c][i] = f8[c][i];
+            }
+            if (post) {
+                standardise<LANES, CHUNKS>(f, a.post, cols, place, shared, turn);
+                weights.apply(f, a.post, place);
+            }
+            if (pre) weights.load(a.pre, place);                   // (on their way during what follows)
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c) {
                 if (a.random.threshold) {
-                    const Bits8 bits = bits_of(key, row * words_of(cols) + col / 4);
+                    const Bits8 bits = bits_of(key, row * words_of(cols) + place.col[c] / 4);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) f[c][i] = bits.of(i) >= a.random.threshold ? f[c][i] : 0.0f;
                 }
+                if (a.gate) {
+                    place.settle(gate8[c], c, has);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) r[c][i] = __builtin_fmaf(scale, f[c][i], a.x_scale * r[c][i]);
-                if (a.r && valid[c]) store_eight<DTYPE>(row_of<DTYPE>(a.r, row, a.ldr), col, r[c], valid[c]);
+                    for (int i = 0; i < 8; ++i) f[c][i] *= gate8[c][i];
+                }
+                place.settle(x8[c], c, has);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) r[c][i] = __builtin_fmaf(scale, f[c][i], a.x_scale * x8[c][i]);
+                if (a.r && has) place.store(row_of<DTYPE, LANES>(a.r, row, a.ldr), c, r[c]);
             }
         }
-        if (a.pre.kind != EDEN_NORM_NONE) {
-            standardise<LANES>(r, a.pre, cols, valid, shared, turn);
+        if (!BRANCH || pre) {
+            standardise<LANES, CHUNKS>(r, a.pre, cols, place, shared, turn);
+            weights.apply(r, a.pre, place);
 #pragma unroll
-            for (int c = 0; c < CHUNKS; ++c) {
-                const uint32_t col = (c * LANES + lane) * 8;
-                weigh<DTYPE>(r[c], a.pre, col, valid[c]);
-                if (valid[c]) store_eight<DTYPE>(row_of<DTYPE>(a.h, row, a.ldh), col, r[c], valid[c]);
-            }
+            for (int c = 0; c < CHUNKS; ++c)
+                if (has) place.store(row_of<DTYPE, LANES>(a.h, row, a.ldh), c, r[c]);
         }
     }
 }
@@ -151,10 +177,13 @@ hipError_t launch_dropout(uint32_t dtype, const void *x, size_t ldx, void *y, si
 
 hipError_t launch_block_join(const eden_join_args &args, hipStream_t st) {
     for_type(args.dtype, [&](auto t) {
-        for_shape(row_shape((uint32_t)args.cols), [&](auto lanes, auto chunks) {
-            constexpr int LANES = decltype(lanes)::value, kThreads = LANES > 64 ? LANES : 256, kRows = kThreads / LANES;
-            const uint64_t groups = std::min<uint64_t>((args.rows + kRows - 1) / kRows, 1u << 16);
-            k_block_join<decltype(t)::value, LANES, decltype(chunks)::value><<<(uint32_t)groups, kThreads, 0, st>>>(args);
+        JoinShape((uint32_t)args.cols).use((uint32_t)args.cols, [&](auto lanes, auto chunks, auto ragged) {
+            constexpr uint32_t DTYPE = decltype(t)::value;
+            constexpr int LANES = decltype(lanes)::value, CHUNKS = decltype(chunks)::value, kThreads = LANES > 64 ? LANES : 256, kRows = kThreads / LANES;
+            constexpr bool RAGGED = decltype(ragged)::value;
+            const uint32_t groups = (uint32_t)std::min<uint64_t>((args.rows + kRows - 1) / kRows, 1u << 16);
+            if (args.f) k_block_join<DTYPE, LANES, CHUNKS, RAGGED, true><<<groups, kThreads, 0, st>>>(args);
+            else k_block_join<DTYPE, LANES, CHUNKS, RAGGED, false><<<groups, kThreads, 0, st>>>(args);
         });
     });
     return hipGetLastError();

@@ -7,30 +7,45 @@
 
 namespace eden_layers {
 
-// Lanes that share a row and chunks of eight columns each of them has: LANES * CHUNKS * 8 columns at least
-struct RowShape {
+// Lanes that share a row and chunks of eight columns each of them has: LANES * CHUNKS * 8 columns at least (rows of less than eight: one lane).  Two chunks a lane where a row takes
+// more than a wave's eights: what a wave does once for a row (sums over its lanes, addresses) then serves twice as many values.
+// WIDE: lanes of the longest rows; FROM: lanes from which on a lane has two chunks before a row gets more lanes
+template <int WIDE, int FROM> struct RowShape {
     int lanes, chunks;
+    explicit RowShape(uint32_t cols) {
+        const int eights = (int)((cols + 7) / 8);
+        if (cols < 8) {
+            lanes = 1, chunks = 1;
+            return;
+        }
+        for (lanes = 8; lanes < eights && lanes < FROM; lanes *= 2) {}
+        for (; lanes < WIDE && lanes * 2 < eights; lanes *= 2) {}
+        for (chunks = 1; lanes * chunks < eights; chunks *= 2) {}
+    }
+    // f(LANES, CHUNKS, RAGGED), integral constants
+    template <class F> void use(uint32_t cols, F f) const {
+        auto with = [&](auto n, auto c) {
+            constexpr int LANES = decltype(n)::value, CHUNKS = decltype(c)::value;
+            if constexpr ((CHUNKS == 1 ? LANES <= FROM : LANES >= FROM && LANES <= WIDE) && LANES * (CHUNKS / 2) * 8 < EDEN_MOST_COLUMNS) {
+                if (lanes != LANES || chunks != CHUNKS) return;
+                if (cols % 8) f(n, c, std::true_type());
+                else f(n, c, std::false_type());
+            }
+        };
+        auto one = [&](auto n) { with(n, std::integral_constant<int, 1>()); };
+        auto two = [&](auto n) { with(n, std::integral_constant<int, 2>()); };
+        if (lanes == 1) f(std::integral_constant<int, 1>(), std::integral_constant<int, 1>(), std::true_type());
+        one(std::integral_constant<int, 8>()), one(std::integral_constant<int, 16>()), one(std::integral_constant<int, 32>()), one(std::integral_constant<int, 64>());
+        one(std::integral_constant<int, 128>()), one(std::integral_constant<int, 256>()), one(std::integral_constant<int, 512>()), one(std::integral_constant<int, 1024>());
+        two(std::integral_constant<int, 64>()), two(std::integral_constant<int, 128>()), two(std::integral_constant<int, 256>()), two(std::integral_constant<int, 512>());
+        two(std::integral_constant<int, 1024>());
+        if constexpr (WIDE < 1024) with(std::integral_constant<int, WIDE>(), std::integral_constant<int, 4>());
+    }
 };
-inline RowShape row_shape(uint32_t cols) {
-    const uint32_t eights = (cols + 7) / 8;
-    if (eights > 1024) return {1024, 2};
-    int lanes = 8;
-    while ((uint32_t)lanes < eights) lanes *= 2;
-    return {lanes, 1};
-}
-// f(integral constants LANES, CHUNKS)
-template <class F> inline void for_shape(RowShape s, F f) {
-    auto with = [&](auto lanes) { f(lanes, std::integral_constant<int, 1>()); };
-    if (s.chunks == 2) f(std::integral_constant<int, 1024>(), std::integral_constant<int, 2>());
-    else if (s.lanes == 8) with(std::integral_constant<int, 8>());
-    else if (s.lanes == 16) with(std::integral_constant<int, 16>());
-    else if (s.lanes == 32) with(std::integral_constant<int, 32>());
-    else if (s.lanes == 64) with(std::integral_constant<int, 64>());
-    else if (s.lanes == 128) with(std::integral_constant<int, 128>());
-    else if (s.lanes == 256) with(std::integral_constant<int, 256>());
-    else if (s.lanes == 512) with(std::integral_constant<int, 512>());
-    else with(std::integral_constant<int, 1024>());
-}
+using JoinShape = RowShape<1024, 64>;
+// A gradient with the sums of the gate and of two norms takes more registers than 1024 lanes have (128 each).
+using GradShape = RowShape<1024, 1024>;
+using FullGradShape = RowShape<512, 512>;
 
 // How the rows of a gradient are shared out: `gates` groups of `group_rows` rows.  Either splits workgroups share a group, or a workgroup has
 // `groups_each` whole ones.
@@ -48,11 +63,8 @@ struct GradArgs {
 
 hipError_t launch_dropout(uint32_t dtype, const void *x, size_t ldx, void *y, size_t ldy, uint32_t rows, uint32_t cols, const eden_random &random, hipStream_t st);
 hipError_t launch_block_join(const eden_join_args &args, hipStream_t st);
-// one for each type, so that they are compiled side by side
-template <uint32_t DTYPE> hipError_t launch_block_grad(const GradArgs &args, hipStream_t st);
-extern template hipError_t launch_block_grad<EDEN_F32>(const GradArgs &, hipStream_t);
-extern template hipError_t launch_block_grad<EDEN_F16>(const GradArgs &, hipStream_t);
-extern template hipError_t launch_block_grad<EDEN_BF16>(const GradArgs &, hipStream_t);
+// one for each type and kind of norm behind the branch (-1: no branch), so that they are compiled side by side
+template <uint32_t DTYPE, int POST> hipError_t launch_block_grad(const GradArgs &args, hipStream_t st);
 
 // out[c] (+)= sum of parts x cols partial sums in their order, for several sums at once
 struct SumsOf {
