@@ -20,6 +20,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+import struct
 from typing import NamedTuple, Optional
 
 import torch
@@ -57,6 +58,13 @@ class JoinGradArgs(ctypes.Structure):
                 + _fields(ctypes.c_void_p, "workspace") + _fields(ctypes.c_size_t, "workspace_bytes"))
 
 
+# The same structures as strings of bytes: a call packs its arguments at once (a ctypes field at a time takes the longer part of a short call)
+_RANDOM, _NORM = "QPII", "IfPP"
+_RANDOM_ARGS = struct.Struct(_RANDOM)
+_JOIN_ARGS = struct.Struct("QQ5P6Q" + 2 * _NORM + _RANDOM + "ffI4x")
+_JOIN_GRAD_ARGS = struct.Struct("QQ7P8Q5PQ" + 2 * _NORM + _RANDOM + "ffIII4xPN")
+
+
 def lib():
     """The built library with this header's entry points declared."""
     global _lib
@@ -65,8 +73,8 @@ def lib():
     L = eden.lib()
     vp, u64, u32 = ctypes.c_void_p, ctypes.c_uint64, ctypes.c_uint32
     L.eden_join_workspace_bytes.argtypes, L.eden_join_workspace_bytes.restype = [u64, u64, u64, u32], ctypes.c_size_t
-    for name, args in (("eden_dropout", [vp, u64, vp, u64, u64, u64, u32, ctypes.POINTER(RandomArgs), vp]), ("eden_join", [ctypes.POINTER(JoinArgs), vp]),
-                       ("eden_join_grad", [ctypes.POINTER(JoinGradArgs), vp])):
+    for name, args in (("eden_dropout", [vp, u64, vp, u64, u64, u64, u32, ctypes.c_char_p, vp]), ("eden_join", [ctypes.c_char_p, vp]),
+                       ("eden_join_grad", [ctypes.c_char_p, vp])):
         f = getattr(L, name)
         f.argtypes, f.restype = args, ctypes.c_int
     _lib = L
@@ -74,14 +82,14 @@ def lib():
 
 
 def _random(seed, number, threshold, device, what):
-    """RandomArgs of a seed that is a number, or an int64 tensor on the device."""
+    """The fields of RandomArgs for a seed that is a number, or an int64 tensor on the device."""
     if not 0 <= number < 2 ** 32:
         _refuse(f"{what}: id {number} is not in 0 .. 2^32 - 1")
     if not isinstance(seed, torch.Tensor):
-        return RandomArgs(seed & (2 ** 64 - 1), None, number, threshold)
+        return seed & (2 ** 64 - 1), 0, number, threshold
     if seed.dtype is not torch.int64 or seed.numel() != 1 or (device is not None and seed.device != device) or not seed.is_cuda:
         _refuse(f"{what}: a seed tensor is one int64 on the operands' device, got {seed.numel()} of {seed.dtype} on {seed.device}")
-    return RandomArgs(0, seed.data_ptr(), number, threshold)
+    return 0, seed.data_ptr(), number, threshold
 
 
 class Dropout:
@@ -113,40 +121,38 @@ class Norm:
         if not (eps >= 0.0 and math.isfinite(eps)):
             _refuse(f"Norm: eps = {eps}")
 
-    def _args(self, to, like, cols, what):
-        to.kind, to.eps = self.code, self.eps
-        if self.weight is not None:
-            to.weight = _vector(self.weight, like, cols, what + " weight")
-        if self.bias is not None:
-            to.bias = _vector(self.bias, like, cols, what + " bias")
+    def _args(self, like, cols, what):
+        weight, bias = self.weight, self.bias
+        return self.code, self.eps, 0 if weight is None else _vector(weight, like, cols, what, "weight"), 0 if bias is None else _vector(bias, like, cols, what, "bias")
 
 
-def _vector(v, like, cols, what):
+_NO_NORM, _NO_RANDOM = (0, 0.0, 0, 0), (0, 0, 0, 0)
+
+
+def _vector(v, like, cols, what, name):
     _same(v, like, what)
     if v.dim() != 1 or v.shape[0] != cols or (cols > 1 and v.stride(0) != 1):
-        _refuse(f"{what} is {tuple(v.shape)} with stride {v.stride()}, expected {cols} neighbours")
+        _refuse(f"{what}: {name} is {tuple(v.shape)} with stride {v.stride()}, expected {cols} neighbours")
     return v.data_ptr()
 
 
-def _matrix(args, name, ld, t, like, shape, what):
-    """Sets the address and distance of an operand of the shape of `like`."""
-    _same(t, like, f"{what}: {name}")
+def _matrix(t, like, shape, what):
+    """(address, distance between rows) of an operand of that shape."""
+    _same(t, like, what)
     if t.shape != shape:
-        _refuse(f"{what}: {name} is {tuple(t.shape)}, expected {tuple(shape)}")
-    address, distance, _, _ = _rows(t, f"{what}: {name}")
-    setattr(args, name, address)
-    setattr(args, ld, distance)
+        _refuse(f"{what} is {tuple(t.shape)}, expected {tuple(shape)}")
+    return _rows(t, what)[:2]
 
 
-def _gate(args, gate, like, rows, cols, what):
-    _same(gate, like, f"{what}: gate")
+def _gate(gate, like, rows, cols, what):
+    """(address, distance between rows, rows) of a gate."""
     if gate.dim() == 1:
-        args.gate, args.ld_gate, args.gates = _vector(gate, like, cols, f"{what}: gate"), cols, 1
-        return
-    address, ld, groups, width = _rows(gate, f"{what}: gate")
+        return _vector(gate, like, cols, what, "gate"), cols, 1
+    _same(gate, like, what)
+    address, ld, groups, width = _rows(gate, what)
     if width != cols or groups < 1 or rows % groups:
         _refuse(f"{what}: gate is {tuple(gate.shape)}, expected {cols} columns and a number of rows that divides {rows}")
-    args.gate, args.ld_gate, args.gates = address, ld, groups
+    return address, ld, groups
 
 
 def _narrow(cols, what):
@@ -156,7 +162,7 @@ def _narrow(cols, what):
 
 def _finite(what, *numbers):
     for n in numbers:
-        if not (math.isfinite(n) and abs(n) <= 3.4028234e38):
+        if not -3.4028234e38 <= n <= 3.4028234e38:
             _refuse(f"{what}: a scale of {n}")
 
 
@@ -171,9 +177,9 @@ def dropout(x, drop: Optional[Dropout], out=None, stream=None):
         _gradient_lost("dropout: x")
     xp, ldx, rows, cols = _rows(x, "dropout: x")
     _narrow(cols, "dropout")
-    random = drop._args(device, "dropout") if drop is not None else RandomArgs()
+    random = drop._args(device, "dropout") if drop is not None else _NO_RANDOM
     y, yp, ldy = _output(out, x.shape, x, "dropout: out")
-    _check((_lib or lib()).eden_dropout(xp, ldx, yp, ldy, rows, cols, dtype, random, _stream(device)), "eden_dropout")
+    _check((_lib or lib()).eden_dropout(xp, ldx, yp, ldy, rows, cols, dtype, _RANDOM_ARGS.pack(*random), _stream(device)), "eden_dropout")
     return y
 
 
@@ -201,28 +207,33 @@ def _join(what, x, f, gate, scale, x_scale, drop, post, pre, out, norm_out, stre
     if x.requires_grad:
         _gradient_lost(f"{what}: x")
     _finite(what, scale, x_scale)
-    a = JoinArgs()
-    a.x, a.ldx, rows, cols = _rows(x, f"{what}: x")
+    xp, ldx, rows, cols = _rows(x, f"{what}: x")
     _narrow(cols, what)
-    a.rows, a.cols, a.dtype, a.x_scale, a.scale = rows, cols, dtype, x_scale, scale
+    shape = x.shape
     r = h = None
+    fp = gp = rp = hp = 0
+    ldf = ldg = ldr = ldh = cols
+    gates, random, post_args = 1, _NO_RANDOM, _NO_NORM
     if f is not None:
-        _matrix(a, "f", "ldf", f, x, x.shape, what)
+        fp, ldf = _matrix(f, x, shape, f"{what}: f")
         if gate is not None:
-            _gate(a, gate, x, rows, cols, what)
+            gp, ldg, gates = _gate(gate, x, rows, cols, f"{what}: gate")
         if drop is not None:
-            a.random = drop._args(device, what)
+            random = drop._args(device, what)
         if post is not None:
-            post._args(a.post, x, cols, f"{what}: post")
-        r, a.r, a.ldr = _output(out, x.shape, x, f"{what}: out")
+            post_args = post._args(x, cols, f"{what}: post")
+        r, rp, ldr = _output(out, shape, x, f"{what}: out")
     if pre is not None:
-        pre._args(a.pre, x, cols, f"{what}: pre")
-        h, a.h, a.ldh = _output(norm_out, x.shape, x, f"{what}: norm_out" if f is not None else f"{what}: out")
+        pre_args = pre._args(x, cols, f"{what}: pre")
+        h, hp, ldh = _output(norm_out, shape, x, f"{what}: norm_out" if f is not None else f"{what}: out")
     elif f is None:
         _refuse("norm: without a norm")
     elif norm_out is not None:
         _refuse("join: norm_out without pre")
-    _check(L.eden_join(a, _stream(device)), "eden_join")
+    else:
+        pre_args = _NO_NORM
+    args = _JOIN_ARGS.pack(rows, cols, xp, fp, gp, rp, hp, ldx, ldf, ldg, ldr, ldh, gates, *post_args, *pre_args, *random, x_scale, scale, dtype)
+    _check(L.eden_join(args, _stream(device)), "eden_join")
     return r, h
 
 
@@ -261,56 +272,67 @@ def _join_grad(what, dr, f, dh, r, gate, scale, x_scale, drop, post, pre, into, 
             return _join_grad(what, dr, f, dh, r, gate, scale, x_scale, drop, post, pre, into, accumulate, branch, None)
     L = _lib or lib()
     _finite(what, scale, x_scale)
-    a = JoinGradArgs()
     shape = like.shape
     _, _, rows, cols = _rows(like, f"{what}: the gradient")
     _narrow(cols, what)
-    a.rows, a.cols, a.dtype, a.x_scale, a.scale, a.branch, a.accumulate = rows, cols, dtype, x_scale, scale, branch, 1 if accumulate else 0
+    df = None
+    drp = dhp = rp = fp = gp = dfp = 0
+    lddr = lddh = ldr = ldf = ldg = lddf = cols
+    gates, random, post_args, pre_args = 1, _NO_RANDOM, _NO_NORM, _NO_NORM
     if dr is not None:
-        _matrix(a, "dr", "lddr", dr, like, shape, what)
+        drp, lddr = _matrix(dr, like, shape, f"{what}: dr")
     if pre is not None:
-        pre._args(a.pre, like, cols, f"{what}: pre")
+        pre_args = pre._args(like, cols, f"{what}: pre")
         if dh is not None:
             if r is None:
                 _refuse(f"{what}: dh without r")
-            _matrix(a, "dh", "lddh", dh, like, shape, what)
-            _matrix(a, "r", "ldr", r, like, shape, what)
+            dhp, lddh = _matrix(dh, like, shape, f"{what}: dh")
+            rp, ldr = _matrix(r, like, shape, f"{what}: r")
     elif dh is not None:
         _refuse(f"{what}: dh without pre")
     if gate is not None:
-        _gate(a, gate, like, rows, cols, what)
+        gp, ldg, gates = _gate(gate, like, rows, cols, f"{what}: gate")
     if drop is not None:
-        a.random = drop._args(device, what)
+        random = drop._args(device, what)
     if post is not None:
-        post._args(a.post, like, cols, f"{what}: post")
+        post_args = post._args(like, cols, f"{what}: post")
     if gate is not None or post is not None:
         if f is None:
             _refuse(f"{what}: f is needed with a gate or post")
-        _matrix(a, "f", "ldf", f, like, shape, what)
-    dx, a.dx, a.lddx = _output(into.dx, shape, like, f"{what}: into.dx")
-    df = None
+        fp, ldf = _matrix(f, like, shape, f"{what}: f")
+    dx, dxp, lddx = _output(into.dx, shape, like, f"{what}: into.dx")
     if branch:
-        df, a.df, a.lddf = _output(into.df, shape, like, f"{what}: into.df")
-    sums = {}
-    for name, there, size in (("gate", gate is not None, None if gate is None else gate.shape), ("post_weight", post is not None and post.weight is not None, (cols,)),
-                              ("post_bias", post is not None and post.bias is not None, (cols,)), ("pre_weight", pre is not None and pre.weight is not None, (cols,)),
-                              ("pre_bias", pre is not None and pre.bias is not None, (cols,))):
-        given = getattr(into, name)
+        df, dfp, lddf = _output(into.df, shape, like, f"{what}: into.df")
+    elif into.df is not None:
+        _refuse(f"{what}: into.df without a branch")
+    sums, addresses, ld_gate_grad, fresh = [None] * 5, [0] * 5, cols, []
+    for i, (name, there) in enumerate((("gate", gate is not None), ("post_weight", post is not None and post.weight is not None), ("post_bias", post is not None and post.bias is not None),
+                                       ("pre_weight", pre is not None and pre.weight is not None), ("pre_bias", pre is not None and pre.bias is not None))):
+        given = into[2 + i]
         if not there:
             if given is not None:
                 _refuse(f"{what}: into.{name} without one")
-            continue
-        if accumulate and given is None:
+        elif given is not None:
+            sums[i], addresses[i], ld = _output(given, gate.shape if i == 0 else (cols,), like, f"{what}: into.{name}", torch.float32)
+            if i == 0:
+                ld_gate_grad = ld
+        elif accumulate:
             _refuse(f"{what}: nothing to accumulate in for {name}")
-        sums[name], address, ld = _output(given, size, like, f"{what}: into.{name}", torch.float32)
-        setattr(a, name + "_grad", address)
-        if name == "gate":
-            a.ld_gate_grad = ld
-    ws = None
-    if sums:
-        size = L.eden_join_workspace_bytes(rows, cols, max(1, a.gates), dtype)
+        else:
+            fresh.append(i)
+    if fresh:
+        # new ones are parts of one allocation, each of whole 64-byte pieces
+        sizes = [gates * cols if i == 0 else cols for i in fresh]
+        parts = like.new_empty(sum((n + 15) // 16 * 16 for n in sizes), dtype=torch.float32).split([(n + 15) // 16 * 16 for n in sizes]) if len(fresh) > 1 else [like.new_empty(sizes[0], dtype=torch.float32)]
+        for i, n, part in zip(fresh, sizes, parts):
+            part = part if part.shape[0] == n else part[:n]
+            sums[i], addresses[i] = part if i or gate.dim() == 1 else part.view(gate.shape), part.data_ptr()
+    ws, size = None, 0
+    if any(addresses):
+        size = L.eden_join_workspace_bytes(rows, cols, gates, dtype)
         if size:
             ws = torch.empty(size, dtype=torch.uint8, device=device)
-            a.workspace, a.workspace_bytes = ws.data_ptr(), size
-    _check(L.eden_join_grad(a, _stream(device)), "eden_join_grad")
-    return JoinGrads(dx=dx, df=df, **sums)
+    args = _JOIN_GRAD_ARGS.pack(rows, cols, drp, dhp, rp, fp, gp, dxp, dfp, lddr, lddh, ldr, ldf, ldg, lddx, lddf, gates, *addresses, ld_gate_grad, *post_args, *pre_args, *random, x_scale, scale,
+                                dtype, 1 if branch else 0, 1 if accumulate else 0, 0 if ws is None else ws.data_ptr(), size)
+    _check(L.eden_join_grad(args, _stream(device)), "eden_join_grad")
+    return JoinGrads(dx, df, *sums)

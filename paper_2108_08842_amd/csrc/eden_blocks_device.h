@@ -20,10 +20,13 @@ struct Bits8 {
     uint32_t pair[4];
     __device__ uint32_t of(int i) const { return i & 1 ? pair[i >> 1] >> 16 : pair[i >> 1] & 0xFFFFu; }
 };
-__device__ inline Bits8 bits_of(uint64_t key, uint64_t word) {
-    const uint64_t a = eden::hash_word(key, word), b = eden::hash_word(key, word + 1);
+// (the hash's 64-bit products are most of it: `state` is what a word is mixed from, key + phi (word + 1), and the next word's is phi more)
+__device__ inline uint64_t state_of(uint64_t key, uint64_t word) { return key + eden::kPhi * (word + 1); }
+__device__ inline Bits8 bits_of(uint64_t state) {
+    const uint64_t a = eden::mix64(state), b = eden::mix64(state + eden::kPhi);
     return {{(uint32_t)a, (uint32_t)(a >> 32), (uint32_t)b, (uint32_t)(b >> 32)}};
 }
+__device__ inline Bits8 bits_of(uint64_t key, uint64_t word) { return bits_of(state_of(key, word)); }
 // What kept values are multiplied by
 __host__ __device__ inline float kept_scale(uint32_t threshold) { return 65536.0f / (float)(65536u - threshold); }
 

@@ -20,8 +20,10 @@ bool matrix_ok(const void *p, uint64_t ld, uint64_t rows, uint64_t cols, size_t 
 }
 bool packed_ok(const void *p, uint64_t rows, uint64_t cols) { return rows == 0 || cols == 0 || (p != nullptr && aligned(p, 16)); }
 bool operand_sizes_ok(uint64_t rows, uint64_t cols) { return rows <= kMostRows && cols <= kMostDepth; }
-// Workgroups of eight rows and a chunk
-bool launchable(uint64_t rows, uint64_t cols) { return (rows / 8 + 1) * chunks_of(cols) <= kMostGroups; }
+// Workgroups of eight chunks, two rows' at least
+bool launchable(uint64_t rows, uint64_t cols) { return (rows / 2 + 1) * (chunks_of(cols) / 4 + 1) <= kMostGroups; }
+// Workgroups of 512 threads for 128 rows (of the transpose) and a chunk
+bool transposable(uint64_t rows, uint64_t cols) { return ((rows + 127) / 128) * chunks_of(cols) <= most_groups(512); }
 
 uint64_t tile_count(uint64_t rows, uint64_t cols, uint32_t side) { return ((rows + side - 1) / side) * ((cols + side - 1) / side); }
 size_t partial_bytes(uint64_t rows, uint64_t cols, uint64_t splits) { return splits * rows * ((cols + 3) / 4 * 4) * sizeof(float); }
@@ -78,6 +80,7 @@ int eden_mx4_quantize(const void *x, uint64_t ldx, uint64_t rows, uint64_t cols,
                       int accumulate, void *workspace, size_t workspace_bytes, void *stream) {
     const uint64_t r = transpose ? cols : rows, c = transpose ? rows : cols;
     if (!known_type(dtype) || !operand_sizes_ok(r, c) || !launchable(r, c) || !matrix_ok(x, ldx, rows, cols, bytes_of(dtype)) || !packed_ok(packed, r, c)) return EDEN_ERR_INVALID_ARG;
+    if (transpose && !transposable(r, c)) return EDEN_ERR_INVALID_ARG;
     if ((sums && !transpose) || !aligned(sums, 4) || !aligned(workspace, 16) || (rounding && !aligned(rounding->seed_at, 8))) return EDEN_ERR_INVALID_ARG;
     if (capacity < mx4_bytes(r, c)) return EDEN_ERR_CAPACITY;
     const hipStream_t st = static_cast<hipStream_t>(stream);

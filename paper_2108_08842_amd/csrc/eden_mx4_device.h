@@ -40,17 +40,26 @@ __device__ inline uint32_t mx4_codes(const float (&x)[8], uint32_t t) {
     w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6] * inverse, x[7] * inverse, 1.0f, 3);
     return t == 255u ? 0u : w;
 }
+// 2 times a half of w more than v
+template <bool UPPER> __device__ inline uint32_t add_half_twice(uint32_t w, uint32_t v) {
+    uint32_t r;
+    if constexpr (UPPER) asm("v_mad_u32_u16 %0, %1, 2, %2 op_sel:[1,0,0,0]" : "=v"(r) : "v"(w), "v"(v));
+    else asm("v_mad_u32_u16 %0, %1, 2, %2" : "=v"(r) : "v"(w), "v"(v));
+    return r;
+}
 // Eight values' codes, stochastically.  v = |x| 2^(127 - t) lies between codes 2 e + floor(f) and the next, f = v 2^(1 - e), e = max(exponent of v, 0).  Its share is
-// f - floor(f), and d + 1/2 < 65536 share iff ceil(2^17 f) + 2 (65535 - d) reaches the next multiple of 2^17: whole numbers, so nothing is rounded on the way.
+// f - floor(f), and d + 1/2 < 65536 share iff ceil(2^17 f) + 2 (65535 - d) reaches the next multiple of 2^17: whole numbers, so nothing is rounded on the way.  With e at 2^18 (127 more,
+// which makes 254 = -2 mod 256 codes) the code is three bits of one sum.
 __device__ inline uint32_t mx4_codes(const float (&x)[8], uint32_t t, const Bits8 &bits) {
     const float inverse = mx4_inverse(t);
     uint32_t w = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const float v = fabsf(x[i]) * inverse;
-        const int e = max((int)(__float_as_uint(v) >> 23), 127) - 127;
-        const uint32_t steps = (uint32_t)ceilf(__builtin_amdgcn_ldexpf(v, 18 - e));
-        const uint32_t code = ((steps + 2u * (65535u - bits.of(i))) >> 17) + 2u * (uint32_t)e;
+        const uint32_t e = __float_as_uint(fmaxf(v, 1.0f)) >> 23;
+        const uint32_t steps = (uint32_t)ceilf(__builtin_amdgcn_ldexpf(v, 145 - (int)e));
+        const uint32_t others = ~bits.pair[i >> 1], sum = (e << 18) + steps;
+        const uint32_t code = ((i & 1 ? add_half_twice<true>(others, sum) : add_half_twice<false>(others, sum)) + (2u << 17)) >> 17 & 7u;
         w |= (code | ((__float_as_uint(x[i]) >> 28) & 8u)) << (4 * i);
     }
     return t == 255u ? 0u : w;

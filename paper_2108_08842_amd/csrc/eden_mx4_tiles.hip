@@ -11,10 +11,13 @@
 #include "eden_layers_fetch.h"
 #include "eden_mx4_kernels.h"
 
+#include <algorithm>
+
 namespace eden_layers {
 namespace {
 
 constexpr int kThreads = 256, kSteps = 4;
+constexpr uint32_t kResident = 256;                                // CUs
 template <int T> struct Tile4 {
     static constexpr int kSide = 64 * T;
     static constexpr int kOperand = kSide * (int)kChunkBytes;      // bytes of an operand's chunk in the LDS
@@ -69,7 +72,7 @@ template <int T> struct Exps4 {
         reach = reach > step ? reach - step : 0;
     }
     __device__ void fetch(uint32_t stage) const {
-        if (offset != kNowhere) load_to_lds(stage + to, offset, now);
+        if (T == 4 || offset != kNowhere) load_to_lds(stage + to, offset, now);       // (a wave that has none would write zeros behind them)
     }
 };
 
@@ -80,18 +83,12 @@ template <int S> __device__ inline f32x16 multiply4(u32x4 a, uint32_t exp_a, u32
 
 template <int OP, uint32_t DTYPE, int T> __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(T == 4 ? 1 : 2, T == 4 ? 1 : 2))) void k_mx4_tiles(const Product p) {
     constexpr int kSide = Tile4<T>::kSide, kOperand = Tile4<T>::kOperand, kLoads = Tile4<T>::kLoads, kStage = Tile4<T>::kStage, N = T * T;
-    static_assert(4 * 32 * kRowFloats<T> * 4 <= 2 * kStage, "the end's sums");
+    static_assert(4 * 32 * kRowFloats<T> * 4 <= kStage, "the end's sums");
     __shared__ __attribute__((aligned(1024))) char lds[2 * kStage];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wave_row = wave >> 1, wave_col = wave & 1;
-    const uint32_t row_tiles = (p.rows + kSide - 1) / kSide, col_tiles = (p.cols + kSide - 1) / kSide;
-    uint32_t split, row_tile, col_tile;
-    place_of(blockIdx.x, gridDim.x, row_tiles, col_tiles, split, row_tile, col_tile);
-    const uint32_t row0 = row_tile * kSide, col0 = col_tile * kSide;
-    const uint32_t chunks = chunks_of(p.depth), first = split * (p.split_depth / kChunk), steps = min(chunks, first + p.split_depth / kChunk) - first;      // (at least one)
-
-    Codes4<T> a(p.a, chunks, row0, p.rows, first, wave, lane), b(p.b, chunks, col0, p.cols, first, wave, lane);
-    Exps4<T> exps(p, chunks, row0, col0, first, wave, lane);
+    const uint32_t row_tiles = (p.rows + kSide - 1) / kSide, col_tiles = (p.cols + kSide - 1) / kSide, total = row_tiles * col_tiles * p.splits;
+    const uint32_t chunks = chunks_of(p.depth), split_chunks = p.split_depth / kChunk;
 
     // where a lane reads: step s at piece 4 (lane / 32) + s; tiles of 32 are whole rows apart
     uint32_t at_a[kSteps], at_b[kSteps];
@@ -103,10 +100,32 @@ template <int OP, uint32_t DTYPE, int T> __global__ __launch_bounds__(kThreads) 
     const uint32_t exp_a = 2 * kOperand + (wave_row * (kSide / 2) + (lane & 31)) * kChunkBlocks + 4 * (lane >> 5);
     const uint32_t exp_b = 2 * kOperand + Tile4<T>::kExps + (wave_col * (kSide / 2) + (lane & 31)) * kChunkBlocks + 4 * (lane >> 5);
 
-    f32x16 acc[T][T] = {};
+    // a tile of the result, or a split of one, and where its operands come from
+    struct Work {
+        uint32_t split, row0, col0, steps;
+        Codes4<T> a, b;
+        Exps4<T> exps;
+    };
+    auto work_of = [&](uint32_t id) {
+        uint32_t split, row_tile, col_tile;
+        place_of(id, total, row_tiles, col_tiles, split, row_tile, col_tile);
+        const uint32_t row0 = row_tile * kSide, col0 = col_tile * kSide, first = split * split_chunks;
+        return Work{split, row0, col0, min(chunks, first + split_chunks) - first, Codes4<T>(p.a, chunks, row0, p.rows, first, wave, lane), Codes4<T>(p.b, chunks, col0, p.cols, first, wave, lane),
+                    Exps4<T>(p, chunks, row0, col0, first, wave, lane)};
+    };
+    auto start = [](Work &w, uint32_t step) { w.a.start(step < w.steps), w.b.start(step < w.steps), w.exps.start(step < w.steps); };
+    const uint32_t lds0 = (uint32_t)(size_t)(lds_char *)lds;
+    auto first_chunk = [&](Work &w, uint32_t to) {
+        start(w, 0);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) w.a.fetch(lds0 + to, wave, i);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) w.b.fetch(lds0 + to + kOperand, wave, i);
+        w.exps.fetch(lds0 + to);
+    };
+
     u32x4 fa[2][T], fb[2][T];
     uint32_t ea[T], eb[T], next_ea[T], next_eb[T];
-    const uint32_t lds0 = (uint32_t)(size_t)(lds_char *)lds;
     auto read = [&](const char *stage, int s, int set, int i) {    // one operand of 2 T
         if (i < T) fb[set][i] = *reinterpret_cast<const u32x4 *>(stage + at_b[s] + i * (32 * (int)kChunkBytes));
         else fa[set][i - T] = *reinterpret_cast<const u32x4 *>(stage + at_a[s] + (i - T) * (32 * (int)kChunkBytes));
@@ -119,61 +138,68 @@ template <int OP, uint32_t DTYPE, int T> __global__ __launch_bounds__(kThreads) 
 #pragma unroll
         for (int i = 0; i < T; ++i) ea[i] = next_ea[i], eb[i] = next_eb[i];
     };
-    // T x T products 64 deep: S = 0 .. 3 of a chunk.  The operands of the following ones are read; S = 3: those of the next chunk, behind a barrier since when nobody needs
-    // the present one, into whose place the chunk after the next goes: one operand during S = 3, the other one and the exponents during S = 0.
-    auto deep64 = [&](auto step64, const char *stage, uint32_t to) {
-        constexpr int S = decltype(step64)::value, set = S & 1, kReads = 2 * T;
-        each<N>([&](auto number) {
-            constexpr int j = decltype(number)::value, i = j / T;
-            acc[i][j % T] = multiply4<S>(fb[set][j % T], eb[j % T], fa[set][i], ea[i], acc[i][j % T]);
-            if constexpr (S == 3 && j == 0) meet<0>();
-            if constexpr ((j + 1) * kReads / N != j * kReads / N) {
-                read(stage, (S + 1) & 3, set ^ 1, j * kReads / N);
-                if constexpr (S == 3) read_exps(stage, j * kReads / N);
+
+    uint32_t now = 0, id = blockIdx.x;
+    Work w = work_of(id);
+    first_chunk(w, now);
+    for (;;) {
+        f32x16 acc[T][T] = {};
+        // T x T products 64 deep: S = 0 .. 3 of a chunk.  The operands of the following ones are read; S = 3: those of the next chunk, behind a barrier since when nobody needs
+        // the present one, into whose place the chunk after the next goes: one operand during S = 3, the other one and the exponents during S = 0.
+        auto deep64 = [&](auto step64, const char *stage, uint32_t to) {
+            constexpr int S = decltype(step64)::value, set = S & 1, kReads = 2 * T;
+            each<N>([&](auto number) {
+                constexpr int j = decltype(number)::value, i = j / T;
+                acc[i][j % T] = multiply4<S>(fb[set][j % T], eb[j % T], fa[set][i], ea[i], acc[i][j % T]);
+                if constexpr (S == 3 && j == 0) meet<0>();
+                if constexpr (j % (N / kReads < 1 ? 1 : N / kReads) == 0) {       // (T = 4: reads behind even products, loads behind odd ones)
+                    read(stage, (S + 1) & 3, set ^ 1, j * kReads / N);
+                    if constexpr (S == 3) read_exps(stage, j * kReads / N);
+                }
+                constexpr int load = due(j, kLoads, N);
+                if constexpr (load >= 0 && S == 3) w.a.fetch(to, wave, load);
+                if constexpr (load >= 0 && S == 0) w.b.fetch(to + kOperand, wave, load);
+                if constexpr (S == 0 && j == N - 1) w.exps.fetch(to);
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            if constexpr (S == 3) take_exps();
+        };
+        meet<0>();                                                 // the first chunk has arrived, and the sums of the tile before have left the LDS
+        start(w, 1);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) w.a.fetch(lds0 + (kStage - now), wave, i);
+#pragma unroll
+        for (int i = 0; i < 2 * T; ++i) read(lds + now, 0, 0, i), read_exps(lds + now, i);
+        take_exps();
+        for (uint32_t step = 0; step < w.steps; ++step) {
+            const uint32_t next = kStage - now;
+            deep64(std::integral_constant<int, 0>(), lds + now, lds0 + next);
+            deep64(std::integral_constant<int, 1>(), lds + now, 0);
+            deep64(std::integral_constant<int, 2>(), lds + now, 0);
+            start(w, step + 2);
+            deep64(std::integral_constant<int, 3>(), lds + next, lds0 + now);
+            now = next;
+        }
+        meet<0>();                                                 // nothing is read or fetched any more: one place takes the next tile's first chunk, the other one the sums, 32 rows of each wave at a time
+        const uint32_t split = w.split, row0 = w.row0 + wave_row * (kSide / 2), col0 = w.col0 + wave_col * (kSide / 2);
+        if constexpr (T == 4) {                                    // (two workgroups to a CU fill each other's pauses)
+            id += gridDim.x;
+            if (id < total) {
+                w = work_of(id);
+                first_chunk(w, now);
             }
-            constexpr int load = due(j, kLoads, N);
-            if constexpr (load >= 0 && S == 3) a.fetch(to, wave, load);
-            if constexpr (load >= 0 && S == 0) b.fetch(to + kOperand, wave, load);
-            if constexpr (S == 0 && j == N - 1) exps.fetch(to);
-            __builtin_amdgcn_sched_barrier(0);
-        });
-        if constexpr (S == 3) take_exps();
-    };
-    auto start = [&](uint32_t step) { a.start(step < steps), b.start(step < steps), exps.start(step < steps); };
-    auto all = [&](uint32_t to) {
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) a.fetch(to, wave, i);
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) b.fetch(to + kOperand, wave, i);
-        exps.fetch(to);
-    };
-    start(0);
-    all(lds0);
-    meet<0>();
-    start(1);
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) a.fetch(lds0 + kStage, wave, i);
-#pragma unroll
-    for (int i = 0; i < 2 * T; ++i) read(lds, 0, 0, i), read_exps(lds, i);
-    take_exps();
-    uint32_t now = 0;
-    for (uint32_t step = 0; step < steps; ++step) {
-        const uint32_t next = kStage - now;
-        deep64(std::integral_constant<int, 0>(), lds + now, lds0 + next);
-        deep64(std::integral_constant<int, 1>(), lds + now, 0);
-        deep64(std::integral_constant<int, 2>(), lds + now, 0);
-        start(step + 2);
-        deep64(std::integral_constant<int, 3>(), lds + next, lds0 + now);
-        now = next;
+        } else {
+            id = total;
+        }
+        finish_wave<OP, DTYPE, T>(p, acc, reinterpret_cast<float *>(lds + (kStage - now)) + wave * 32 * kRowFloats<T>, row0, col0, 0, lane, split);
+        if (id >= total) break;
     }
-    meet<0>();                                                     // nothing is read or fetched any more: the LDS takes the sums, 32 rows of each wave at a time
-    finish_wave<OP, DTYPE, T>(p, acc, reinterpret_cast<float *>(lds) + wave * 32 * kRowFloats<T>, row0 + wave_row * (kSide / 2), col0 + wave_col * (kSide / 2), 0, lane, split);
 }
 
 }  // namespace
 
 hipError_t launch_mx4_tiles(Op op, uint32_t dtype, const Product &p, uint32_t side, hipStream_t st) {
-    const uint32_t grid = ((p.rows + side - 1) / side) * ((p.cols + side - 1) / side) * p.splits;
+    const uint32_t tiles = ((p.rows + side - 1) / side) * ((p.cols + side - 1) / side) * p.splits, grid = side == 256 ? std::min(tiles, kResident) : tiles;
     auto typed = [&](auto o, auto t) {
         constexpr int OP = decltype(o)::value;
         constexpr uint32_t DTYPE = decltype(t)::value;

@@ -38,7 +38,7 @@ def lib():
     L = eden.lib()
     vp, u64, u32, sz, ci = ctypes.c_void_p, ctypes.c_uint64, ctypes.c_uint32, ctypes.c_size_t, ctypes.c_int
     for name, args, result in (("eden_mx4_bytes", [u64, u64], sz), ("eden_mx4_sums_bytes", [u64, u64], sz), ("eden_mx4_workspace_bytes", [u64, u64, u64, ci], sz),
-                               ("eden_mx4_quantize", [vp, u64, u64, u64, u32, ci, ctypes.POINTER(blocks.RandomArgs), vp, sz, vp, ci, vp, sz, vp], ci),
+                               ("eden_mx4_quantize", [vp, u64, u64, u64, u32, ci, ctypes.c_char_p, vp, sz, vp, ci, vp, sz, vp], ci),
                                ("eden_mx4_restore", [vp, u64, u64, u32, vp, u64, vp], ci),
                                ("eden_mx4_linear", [vp, u64, vp, vp, vp, vp, u64, vp, u64, vp, sz, u64, u64, u64, u32, u32, vp, sz, vp], ci),
                                ("eden_mx4_input_grad", [vp, vp, vp, u32, vp, u64, vp, u64, u64, u64, u64, u32, vp, sz, vp], ci),
@@ -133,7 +133,7 @@ def quantize(x, transpose: bool = False, rounding: Stochastic = None, into: Mx4 
         into.buffer, into.rows, into.cols = torch.empty(_bytes(r, c), dtype=torch.uint8, device=device), r, c
     elif (into.rows, into.cols) != (r, c) or into.buffer.device != device:
         _refuse(f"quantize: into is {into.rows} x {into.cols} on {into.buffer.device}, expected {r} x {c} on {device}")
-    random = None if rounding is None else blocks._random(rounding.seed, rounding.id, 0, device, "quantize")
+    random = None if rounding is None else blocks._RANDOM_ARGS.pack(*blocks._random(rounding.seed, rounding.id, 0, device, "quantize"))
     total, tp, ws, wsp, size = None, None, None, None, 0
     if with_sums:
         total, tp, _ = _output(None if sums is True else sums, (cols,), x, "quantize: sums", torch.float32)

@@ -4,6 +4,7 @@ import ctypes
 import os
 import re
 import shutil
+import struct
 import subprocess
 
 import pytest
@@ -44,6 +45,18 @@ def test_header_is_plain_c_and_the_binding_has_its_layout(blocks, tmp_path):
     got = [int(v) for v in subprocess.run([str(tmp_path / "c")], check=True, capture_output=True, text=True).stdout.split()]
     want = [ctypes.sizeof(s) for s in fields.values()] + [getattr(s, f[0]).offset for s in fields.values() for f in s._fields_]
     assert got == want
+    assert [blocks._JOIN_ARGS.size, blocks._JOIN_GRAD_ARGS.size, struct.calcsize(blocks._NORM), blocks._RANDOM_ARGS.size] == want[:4]
+
+
+def test_arguments_are_packed_as_the_structures_are(blocks):
+    """Every field a number of its own: the packed bytes are those of the structure."""
+    for kind, packed in ((blocks.JoinArgs, blocks._JOIN_ARGS), (blocks.JoinGradArgs, blocks._JOIN_GRAD_ARGS)):
+        a, flat = kind(), []
+        for name, field in kind._fields_:
+            for part, of in [(name, None)] if not issubclass(field, ctypes.Structure) else [(f[0], name) for f in field._fields_]:
+                flat.append(len(flat) + 1)
+                setattr(a if of is None else getattr(a, of), part, flat[-1])
+        assert packed.pack(*flat) == bytes(a)
 
 
 def test_workspace(blocks):
@@ -61,7 +74,7 @@ def test_refusals(blocks):
     L, bad = blocks.lib(), -1
 
     def dropout(x=P, ldx=8, y=P, ldy=8, rows=2, cols=8, dtype=0, threshold=5, seed_at=None):
-        return L.eden_dropout(x, ldx, y, ldy, rows, cols, dtype, blocks.RandomArgs(1, seed_at, 0, threshold), None)
+        return L.eden_dropout(x, ldx, y, ldy, rows, cols, dtype, bytes(blocks.RandomArgs(1, seed_at, 0, threshold)), None)
 
     assert dropout(rows=0) == dropout(cols=0) == 0
     for case in (dict(x=None), dict(y=None), dict(ldx=7), dict(ldy=7), dict(x=P + 2), dict(dtype=3), dict(threshold=65536), dict(seed_at=P + 4), dict(rows=2 ** 30 + 1), dict(cols=16385, ldx=16385, ldy=16385)):
@@ -80,7 +93,7 @@ def test_refusals(blocks):
     def join(**given):
         a = blocks.JoinArgs(rows=4, cols=8, x=P, f=P, r=P, h=P, ldx=8, ldf=8, ldr=8, ldh=8, gates=1, x_scale=1.0, scale=1.0)
         a.pre.kind = 1
-        return L.eden_join(fill(a, given), None)
+        return L.eden_join(bytes(fill(a, given)), None)
 
     assert join(rows=0) == join(cols=0) == 0 and L.eden_join(None, None) == bad
     inf = float("inf")
@@ -94,7 +107,7 @@ def test_refusals(blocks):
     def grad(**given):
         a = blocks.JoinGradArgs(rows=4, cols=8, dr=P, dh=P, r=P, f=P, dx=P, df=P, lddr=8, lddh=8, ldr=8, ldf=8, lddx=8, lddf=8, gates=1, x_scale=1.0, scale=1.0, branch=1)
         a.pre.kind = a.post.kind = 2
-        return L.eden_join_grad(fill(a, given), None)
+        return L.eden_join_grad(bytes(fill(a, given)), None)
 
     assert grad(cols=0) == grad(dx=None, df=None) == 0 and L.eden_join_grad(None, None) == bad
     for case in (dict(r=None), dict(f=None), dict(pre__kind=0), dict(lddr=7), dict(lddh=7), dict(ldr=7), dict(ldf=7), dict(lddx=7), dict(lddf=7), dict(dr=P + 1), dict(dx=P + 2), dict(workspace=P + 8),

@@ -85,7 +85,7 @@ def test_refusals(mx4):
     assert quantize(rows=0) == quantize(cols=0) == quantize(rows=0, transpose=1) == 0
     for case in (dict(x=None), dict(packed=None), dict(packed=P + 8), dict(ldx=7), dict(x=P + 2), dict(dtype=3), dict(sums=P), dict(transpose=1, sums=P + 2), dict(ws=P + 4, size=8),
                  dict(cols=2 ** 22 + 1, ldx=2 ** 23), dict(rows=2 ** 28 + 1), dict(rows=2 ** 22 + 1, transpose=1), dict(cols=2 ** 28 + 1, ldx=2 ** 29, transpose=1),
-                 dict(rows=2 ** 28, cols=2 ** 22, ldx=2 ** 22, capacity=2 ** 62), dict(rounding=RandomArgs(1, P + 4, 0, 0))):
+                 dict(rows=2 ** 28, cols=2 ** 22, ldx=2 ** 22, capacity=2 ** 62), dict(rounding=bytes(RandomArgs(1, P + 4, 0, 0)))):
         assert quantize(**case) == bad, case
     assert quantize(capacity=mx4.mx4_bytes(4, 8) - 1) == room and quantize(transpose=1, capacity=mx4.mx4_bytes(8, 4) - 1) == room
 
