@@ -32,11 +32,25 @@ struct Shape {
     uint32_t side;
     uint64_t splits;
 };
+// Tiles of 256 x 256, one to a CU, or of 128 x 128, two to a CU, by what a round of each takes in us.  Measured (bf16): a chunk of 256 deep 1.65 in a full round of the former (8192 x 8192: 264 us at 8192 deep, four
+// rounds), 1.2 where CUs are idle (512 x 4096 x 4096: 28); 1.0 in a full round of the latter (2048 x 4096 x 4096: 25, 1500 x 5120 x 8192: 40), 0.55 with one to a CU (512 x 4096 x 4096: 13.6,
+// 2048 x 2048 x 2048: 10.6); ends 10 and 5 a round.  That puts 4096 x 5120 x 4096 (54 us against 69) and 3000 x 3000 x 1000 (16 against 20) at the latter, 4096 x 4096 x 4096 at the former (42).
+// A sum of small tiles is split over workgroups where that is worth the join, a launch and 8 bytes a result and split at 3 TB/s: 256 x 256, 16384 deep, in 16 parts 11 us against 34; 64 x 4096 x 4096 in
+// four 11.2 against 12.2; 1024 x 1024 x 4096 not (two parts: 15.7 against 12.7; four: 20).
 Shape shape_of(uint64_t rows, uint64_t cols, uint64_t depth) {
-    const uint64_t large = tile_count(rows, cols, 256), small = tile_count(rows, cols, 128);
-    if (large >= 192) return {256, 1};
-    const uint64_t s = std::min<uint64_t>({512 / small, chunks_of(depth) / 2, 64});
-    return {128, std::max<uint64_t>(s, 1)};
+    const uint64_t large = tile_count(rows, cols, 256), small = tile_count(rows, cols, 128), chunks = std::max<uint64_t>(1, chunks_of(depth));
+    const double cost_large = (double)(large / 256) * (1.65 * (double)chunks + 10.0) + (large % 256 ? 1.2 * (double)chunks + 11.0 : 0.0);
+    auto cost_small = [&](uint64_t splits) {
+        const uint64_t tiles = small * splits, left = tiles % 512;
+        const double deep = (double)((chunks + splits - 1) / splits);
+        const double join = splits > 1 ? 4.5 + (double)splits * (double)rows * (double)cols * (8.0 / 3e6) : 0.0;
+        return (double)(tiles / 512) * (deep + 5.0) + (left > 256 ? deep + 5.0 : left ? 0.55 * deep + 1.5 : 0.0) + join;
+    };
+    Shape best = {128, 1};
+    double cost = cost_small(1);
+    for (uint64_t splits = 2; splits <= 64 && splits <= chunks && small * splits <= 512; ++splits)
+        if (cost_small(splits) < cost) cost = cost_small(splits), best.splits = splits;
+    return cost_large < cost ? Shape{256, 1} : best;
 }
 
 // Launches a product whose operands and end are set.
