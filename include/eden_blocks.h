@@ -7,7 +7,7 @@
  * Conventions are those of eden_layers.h: status codes, device pointers, row-major matrices with a distance between rows, streams,
  * no allocation, no memset, no synchronisation; a call may be captured in a HIP graph, and calls may run on any streams at once if their buffers
  * do not overlap.  Rows have up to EDEN_MOST_COLUMNS columns, there are up to 2^30 of them; either may be 0.
- * Values, statistics and sums are fp32; every result is rounded once, to nearest even.
+ * Values, statistics and sums are fp32 (a row's mean square has to be in its range); every result is rounded once, to nearest even.
  *
  * Random numbers: the words of the hash of eden.h.  Row i, column j of a matrix of c columns has bits 16 (j mod 4) .. + 15 of word
  * i ceil(c / 4) + floor(j / 4) of the stream's key for (seed, id).  Nothing is stored: the backward pass names the same seed and id.
@@ -64,7 +64,8 @@ int eden_join(const eden_join_args *args, void *stream);
 
 /* The gradients of the join from those of r (dr) and h (dh); either may be NULL for zeros, dh is if pre.kind is EDEN_NORM_NONE:
  *   d = dr + (gradient of pre at r);  dx = x_scale d;  df, gate_grad, and those of the norms' weights and biases: behind d.
- * r: the sum as eden_join wrote it, read if dh is there.  f: read if post is there or gate_grad is wanted; `branch` says whether the join had one.
+ * r: the sum as eden_join wrote it (without a branch x), read if dh is there.  f: read if post is there or gate_grad is wanted; `branch` says whether the join had one:
+ * without it there are no gate, post, dropout and df, and dh has to be there.
  * dx, df and every sum may be NULL.  Sums are fp32: gate_grad gates x cols at distance ld_gate_grad, the others cols; accumulate != 0: added
  * to what they hold.  dx may be dr, dh or r, df may be f (same pointer, same distance); outputs must not overlap anything else.
  * Sums over rows are split over workgroups as far as the workspace reaches (NULL: not at all, which is slow); the split sets the order of the

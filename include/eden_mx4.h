@@ -12,9 +12,10 @@
  * step, and what is a code's value stays.
  * Layout: r rows of 128 ceil(c / 256) bytes, two codes to a byte, the even column's in the low half, zeros behind the last column; then, for each 256 columns, eight
  * exponent bytes of each row, for an even number of rows (what those of a row too many hold does not matter).  Exponents behind the last block are 0.  Buffers
- * are 16-byte aligned; r is at most 2^28, c at most 2^22.
+ * are 16-byte aligned; r is at most 2^27, c at most 2^22.
  *
- * Products of codes are exact, sums fp32, results rounded once to nearest even.
+ * Products of codes are exact, sums fp32, results rounded once to nearest even.  Outputs must not overlap inputs, except that eden_mx4_linear's y and eden_mx4_input_grad's dx may be the
+ * residual itself (same pointer, same distance).
  */
 #ifndef EDEN_MX4_H
 #define EDEN_MX4_H

@@ -19,7 +19,6 @@ Dropout.  Calls that share seed and id drop the same places.
 from __future__ import annotations
 
 import ctypes
-import math
 import struct
 from typing import NamedTuple, Optional
 
@@ -118,7 +117,7 @@ class Norm:
             _refuse(f"Norm: unknown kind {kind!r}")
         if kind == "rms" and bias is not None:
             _refuse("Norm: an rms norm has no bias")
-        if not (eps >= 0.0 and math.isfinite(eps)):
+        if not 0.0 <= eps <= 3.4028234e38:
             _refuse(f"Norm: eps = {eps}")
 
     def _args(self, like, cols, what):
@@ -250,6 +249,8 @@ class JoinGrads(NamedTuple):
 
 def norm_grad(dh, x, pre: Norm, residual=None, into: JoinGrads = JoinGrads(), accumulate: bool = False, stream=None) -> JoinGrads:
     """The gradients of norm(x, pre) from that of its result; dx is added to `residual`, the gradient that reaches x past the norm."""
+    if dh is None or pre is None:
+        _refuse("norm_grad: dh and pre are needed")
     return _join_grad("norm_grad", residual, None, dh, x, None, 1.0, 1.0, None, None, pre, into, accumulate, False, stream)
 
 

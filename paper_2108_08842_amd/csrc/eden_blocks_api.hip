@@ -118,7 +118,7 @@ int eden_join_grad(const eden_join_grad_args *args, void *stream) {
     // what a norm or a branch that is not there would give
     if ((!normed && (a.dh || a.pre_weight_grad || a.pre_bias_grad)) || (!post && (a.post_weight_grad || a.post_bias_grad))) return EDEN_ERR_INVALID_ARG;
     if ((a.pre_bias_grad && a.pre.kind != EDEN_NORM_LAYER) || (a.post_bias_grad && a.post.kind != EDEN_NORM_LAYER)) return EDEN_ERR_INVALID_ARG;
-    if (!a.branch && (a.gate || a.gate_grad || a.df || post || a.random.threshold)) return EDEN_ERR_INVALID_ARG;
+    if (!a.branch && (a.gate || a.gate_grad || a.df || post || a.random.threshold || (a.dh == nullptr && a.rows && a.cols))) return EDEN_ERR_INVALID_ARG;
     if (a.cols == 0) return EDEN_OK;
     g.needs_f = post || a.gate_grad;
     if (a.rows != 0 && ((g.needs_f && a.f == nullptr) || (a.dh && a.r == nullptr))) return EDEN_ERR_INVALID_ARG;

@@ -8,7 +8,7 @@ using namespace eden_layers;
 
 namespace {
 
-constexpr uint64_t kMostRows = 1ull << 28, kMostDepth = 1ull << 22, kMostGroups = 0x7FFFFFFFull;
+constexpr uint64_t kMostRows = 1ull << 27, kMostDepth = 1ull << 22, kMostGroups = 0x7FFFFFFFull;
 
 bool known_type(uint32_t dtype) { return dtype <= EDEN_BF16; }
 size_t bytes_of(uint32_t dtype) { return dtype == EDEN_F32 ? 4 : 2; }

@@ -112,7 +112,7 @@ def test_refusals(blocks):
     assert grad(cols=0) == grad(dx=None, df=None) == 0 and L.eden_join_grad(None, None) == bad
     for case in (dict(r=None), dict(f=None), dict(pre__kind=0), dict(lddr=7), dict(lddh=7), dict(ldr=7), dict(ldf=7), dict(lddx=7), dict(lddf=7), dict(dr=P + 1), dict(dx=P + 2), dict(workspace=P + 8),
                  dict(gate=P, gates=3, ld_gate=8), dict(gate_grad=P, gates=2, ld_gate_grad=7), dict(gate_grad=P + 2, gates=1), dict(pre__kind=1, pre_bias_grad=P), dict(post__kind=1, post_bias_grad=P),
-                 dict(post__kind=0, post_weight_grad=P), dict(pre__kind=0, dh=None, pre_weight_grad=P), dict(pre_weight_grad=P + 2), dict(branch=0), dict(branch=0, df=None), dict(dtype=7),
+                 dict(post__kind=0, post_weight_grad=P), dict(pre__kind=0, dh=None, pre_weight_grad=P), dict(pre_weight_grad=P + 2), dict(branch=0), dict(branch=0, df=None), dict(branch=0, df=None, post__kind=0, dh=None), dict(dtype=7),
                  dict(random__threshold=70000), dict(cols=20000), dict(rows=2 ** 31), dict(scale=inf)):
         assert grad(**case) == bad, case
 
@@ -122,8 +122,8 @@ def test_calls_that_do_not_fit_are_refused(blocks):
     x = torch.ones(4, 8)
     for call in (lambda: blocks.dropout(x, blocks.Dropout(0.1, 1)), lambda: blocks.norm(x, blocks.Norm("rms")), lambda: blocks.join(x, x), lambda: blocks.join_grad(x, x), lambda: blocks.join(x, None),
                  lambda: blocks.join_grad(None), lambda: blocks.Dropout(1.0, 1), lambda: blocks.Dropout(-0.1, 1), lambda: blocks.Dropout(float("nan"), 1), lambda: blocks.Norm("batch"),
-                 lambda: blocks.Norm("rms", None, x[0]), lambda: blocks.Norm("layer", eps=-1.0), lambda: blocks.Norm("layer", eps=float("inf")),
-                 lambda: blocks.Dropout(0.1, 1, 2 ** 32)._args(None, "x"), lambda: blocks.Dropout(0.1, torch.tensor(3))._args(None, "x")):
+                 lambda: blocks.Norm("rms", None, x[0]), lambda: blocks.Norm("layer", eps=-1.0), lambda: blocks.Norm("layer", eps=float("inf")), lambda: blocks.Norm("layer", eps=1e39), lambda: blocks.norm_grad(None, x, blocks.Norm("rms"), residual=x),
+                 lambda: blocks.norm_grad(x, x, None), lambda: blocks.Dropout(0.1, 1, 2 ** 32)._args(None, "x"), lambda: blocks.Dropout(0.1, torch.tensor(3))._args(None, "x")):
         with pytest.raises(EdenError):
             call()
 

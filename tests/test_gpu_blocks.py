@@ -384,3 +384,89 @@ def test_gradients_against_differences(blocks):
             slope = (ends[0] - ends[1]) / (2 * t)
             # r, rounded to fp32, and the gradients' own roundings: 1e-5 of the sum of sizes is a hundred of them; the third derivative's t^2 is below that
             assert abs(slope - float((double(grad) * way).sum())) <= 1e-5 * float((double(grad) * way).abs().sum()) + 1e-5
+
+
+# ---- ends of the range
+
+@pytest.mark.parametrize("cols", [5, 250, 1000, 1031, 4097, 8190, 16383])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_results_in_the_place_of_operands(blocks, dtype, cols):
+    """A result over the operand it replaces, with and without the sums over a row that keep a row's waves together."""
+    t = TYPES[dtype]
+    for number in (1, 4, 5):
+        g = gen("place", dtype, cols, number)
+        kw, _ = setting(blocks, g, 40, cols, t, number)
+        x, f, dr, dh = (matrix(g, 40, cols, t, 3) for _ in range(4))
+        want = blocks.join(x, f, **kw)
+        want = (want, None) if kw["pre"] is None else want
+        for place in (x, f):
+            x2, f2 = x.clone(), f.clone()
+            out = x2 if place is x else f2
+            got = blocks.join(x2, f2, out=out, norm_out=None if kw["pre"] is None else (f2 if place is x else x2), **kw)
+            got = (got, None) if kw["pre"] is None else got
+            assert got[0] is out and torch.equal(got[0], want[0]) and (want[1] is None or torch.equal(got[1], want[1]))
+        dh = dh if kw["pre"] is not None else None
+        want = blocks.join_grad(dr, f, dh=dh, r=x, **kw)
+        for place in range(3):
+            if place and dh is None:
+                continue
+            operands = [dr.clone(), dh.clone() if dh is not None else None, x.clone()]
+            f2 = f.clone()
+            got = blocks.join_grad(operands[0], f2, dh=operands[1], r=operands[2], into=blocks.JoinGrads(dx=operands[place], df=f2), **kw)
+            for a, b in zip(want, got):
+                assert (a is None and b is None) or torch.equal(a, b)
+        y = x.clone()
+        assert torch.equal(blocks.dropout(y, blocks.Dropout(0.4, 3), out=y), blocks.dropout(x, blocks.Dropout(0.4, 3)))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_operands_that_begin_anywhere(blocks, dtype):
+    t = TYPES[dtype]
+    for cols in (64, 1000, 1031, 4096):
+        g = gen("anywhere", dtype, cols)
+        kw, _ = setting(blocks, g, 20, cols, t, 5)
+
+        def moved(v):
+            if v is None:
+                return None
+            flat = torch.full((v.numel() + 8,), float("nan"), dtype=v.dtype, device="cuda")
+            return flat[1:1 + v.numel()].view(v.shape).copy_(v)
+        x, f, dr, dh = (matrix(g, 20, cols, t) for _ in range(4))
+        kw2 = dict(kw, gate=moved(kw["gate"]), post=blocks.Norm("layer", moved(kw["post"].weight), moved(kw["post"].bias)), pre=blocks.Norm("layer", moved(kw["pre"].weight), moved(kw["pre"].bias)))
+        for a, b in zip(blocks.join(x, f, **kw), blocks.join(moved(x), moved(f), out=moved(x), norm_out=moved(x), **kw2)):
+            assert torch.equal(a, b)
+        into = blocks.JoinGrads(dx=moved(x), df=moved(x))
+        for a, b in zip(blocks.join_grad(dr, f, dh=dh, r=x, **kw), blocks.join_grad(moved(dr), moved(f), dh=moved(dh), r=moved(x), into=into, **kw2)):
+            assert torch.equal(a, b)
+        assert torch.equal(blocks.dropout(moved(x), blocks.Dropout(0.2, 1), out=moved(x)), blocks.dropout(x, blocks.Dropout(0.2, 1)))
+
+
+def test_more_rows_than_workgroups_and_elements_than_32_bits_count(blocks):
+    """The last rows of 2^32 elements and more, in more rows than the join has workgroups."""
+    rows, cols, last, t = 2 ** 18 + 2 ** 15, 16384, 8, torch.bfloat16
+    g = gen("large")
+    words = (cols + 3) // 4
+    bits = np.asarray(ref.oracle.hash_words(ref.oracle.stream_key(5, ref.STREAM_DROPOUT, 2), (rows - last) * words, last * words)).astype("<u8").view("<u2")
+    mask = torch.from_numpy(bits.reshape(last, 4 * words)[:, :cols].astype(np.int64)) >= 16384
+
+    def ending(tail):
+        x = torch.zeros(rows, cols, dtype=t, device="cuda")
+        x[-last:] = tail
+        return x
+    tails = [matrix(g, last, cols, t) for _ in range(4)]
+    x, f = ending(tails[0]), ending(tails[1])
+    drop, w = blocks.Dropout(0.25, 5, 2), vector(g, cols, t, 1.0)
+    want = ref.join(double(tails[0]), double(tails[1]), None, 1.0, 1.0, mask, 0.25, None, ("rms", double(w), None, float(np.float32(1e-5))))
+    r, h = blocks.join(x, f, dropout=drop, pre=blocks.Norm("rms", w), norm_out=f)
+    near(r[-last:], want["r"], "r")
+    near(h[-last:], want["h"], "h")
+    assert not bool(h[:-last].any())
+    y = blocks.dropout(x, drop, out=x)
+    assert torch.equal(y[-last:].cpu(), torch.where(mask, tails[0].cpu().float() * torch.tensor(65536.0 / 49152, dtype=torch.float32), torch.zeros(())).to(t))
+    dr, dh = ending(tails[2]), ending(tails[3])
+    got = blocks.join_grad(dr, dh=dh, r=r, dropout=drop, pre=blocks.Norm("rms", w), into=blocks.JoinGrads(dx=dr, df=h))
+    want = ref.join_grad(double(tails[2]), None, double(tails[3]), double(r[-last:]), None, 1.0, 1.0, mask, 0.25, None, ("rms", double(w), None, float(np.float32(1e-5))))
+    near(got.dx[-last:], want["dx"], "dx")
+    near(got.df[-last:], want["df"], "df")
+    # (the zeros in front add nothing)
+    near(got.pre_weight, (want["pre_weight"][0], want["pre_weight"][1] + 64 * ref.E * want["pre_weight"][0].abs()), "pre_weight")

@@ -360,3 +360,47 @@ def test_on_other_streams_at_once(mx4):
     torch.cuda.synchronize()
     for y in got:
         assert torch.equal(y, want)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_operands_that_begin_anywhere(mx4, dtype):
+    t = TYPES[dtype]
+    for rows, cols in ((40, 300), (257, 1000), (1, 4096), (3, 128)):
+        g = gen("anywhere", dtype, rows)
+        x, w = matrix(g, rows, cols, t), mx4.quantize(matrix(g, 90, cols, t))
+        flat = torch.full((rows * cols + 8,), float("nan"), dtype=t, device="cuda")
+        moved = flat[1:1 + rows * cols].view(rows, cols).copy_(x)
+        for transpose in (False, True):
+            for rounding in (None, mx4.Stochastic(3)):
+                a, b = (mx4.quantize(v, transpose=transpose, rounding=rounding) for v in (x, moved))
+                assert torch.equal(a.restore(torch.float32), b.restore(torch.float32))
+        out = torch.full((rows * 90 + 8,), float("nan"), dtype=t, device="cuda")[1:1 + rows * 90].view(rows, 90)
+        residual = torch.full((rows * 90 + 8,), 0.5, dtype=t, device="cuda")[3:3 + rows * 90].view(rows, 90)
+        want = mx4.linear(x, w, residual=residual)
+        assert torch.equal(mx4.linear(moved, w, residual=residual, out=out), want)
+        assert torch.equal(mx4.linear(x, w, residual=residual, out=residual), want)
+
+
+def test_transposes_beyond_two_to_the_32_elements(mx4):
+    rows, cols, last = 2 ** 18 + 2 ** 15, 16384, 32
+    g = torch.Generator(device="cuda").manual_seed(2)
+    tail = torch.randn(last, cols, generator=g, device="cuda").bfloat16()
+    x = torch.zeros(rows, cols, dtype=torch.bfloat16, device="cuda")
+    x[-last:] = tail
+    got, sums = mx4.quantize(x, transpose=True, rounding=mx4.Stochastic(9, 1), sums=True)
+    # the last block of every packed row: its words are the last eight of a row's
+    words = rows // 4
+    pick = [0, 1, 777, cols - 1]
+    back = got.restore(torch.float32, out=torch.empty(cols, rows, device="cuda"))
+    for c in pick:
+        bits = np.asarray(lref_hash(c * words + words - last // 4, last // 4)).astype("<u8").view("<u2")
+        want = ref.values(tail[:, c:c + 1].t().cpu(), torch.from_numpy(bits.astype(np.int64)).view(1, last).numpy())
+        assert torch.equal(back[c, -last:].cpu().double(), want[0])
+        assert not bool(back[c, :-last].any())
+    assert bool(((sums.double() - tail.double().sum(0)).abs() <= (last + 8) * 2.0 ** -24 * tail.double().abs().sum(0)).all())
+
+
+def lref_hash(first, count):
+    from oracle import eden_oracle as oracle
+    from tests import blocks_reference
+    return oracle.hash_words(oracle.stream_key(9, blocks_reference.STREAM_ROUNDING, 1), first, count)

@@ -42,9 +42,9 @@ def test_header_is_plain_c(tmp_path):
 
 
 def test_sizes(mx4):
-    for rows, cols in ((0, 5), (5, 0), (1, 1), (1, 256), (2, 257), (3, 33), (7, 1000), (2 ** 28, 2 ** 22)):
+    for rows, cols in ((0, 5), (5, 0), (1, 1), (1, 256), (2, 257), (3, 33), (7, 1000), (2 ** 27, 2 ** 22)):
         assert mx4.mx4_bytes(rows, cols) == ref.size(rows, cols) == mx4._bytes(rows, cols)
-    assert mx4.mx4_bytes(2 ** 28 + 1, 1) == 0 and mx4.mx4_bytes(1, 2 ** 22 + 1) == 0
+    assert mx4.mx4_bytes(2 ** 27 + 1, 1) == 0 and mx4.mx4_bytes(1, 2 ** 22 + 1) == 0
     sums, space = mx4.lib().eden_mx4_sums_bytes, mx4.lib().eden_mx4_workspace_bytes
     assert sums(256, 100) == 0 and 0 < sums(8192, 100) <= 32 * 400 and sums(0, 5) == sums(5, 0) == 0
     assert space(8192, 8192, 8192, 0) == 0 and space(0, 5, 10000, 0) == 0
@@ -84,8 +84,8 @@ def test_refusals(mx4):
 
     assert quantize(rows=0) == quantize(cols=0) == quantize(rows=0, transpose=1) == 0
     for case in (dict(x=None), dict(packed=None), dict(packed=P + 8), dict(ldx=7), dict(x=P + 2), dict(dtype=3), dict(sums=P), dict(transpose=1, sums=P + 2), dict(ws=P + 4, size=8),
-                 dict(cols=2 ** 22 + 1, ldx=2 ** 23), dict(rows=2 ** 28 + 1), dict(rows=2 ** 22 + 1, transpose=1), dict(cols=2 ** 28 + 1, ldx=2 ** 29, transpose=1),
-                 dict(rows=2 ** 28, cols=2 ** 22, ldx=2 ** 22, capacity=2 ** 62), dict(rounding=bytes(RandomArgs(1, P + 4, 0, 0)))):
+                 dict(cols=2 ** 22 + 1, ldx=2 ** 23), dict(rows=2 ** 27 + 1), dict(rows=2 ** 22 + 1, transpose=1), dict(cols=2 ** 27 + 1, ldx=2 ** 29, transpose=1),
+                 dict(rows=2 ** 27, cols=2 ** 22, ldx=2 ** 22, capacity=2 ** 62), dict(rounding=bytes(RandomArgs(1, P + 4, 0, 0)))):
         assert quantize(**case) == bad, case
     assert quantize(capacity=mx4.mx4_bytes(4, 8) - 1) == room and quantize(transpose=1, capacity=mx4.mx4_bytes(8, 4) - 1) == room
 
@@ -101,9 +101,9 @@ def test_refusals(mx4):
 
     assert linear(m=0) == linear(n=0) == 0
     for case in (dict(x=None), dict(x4=P), dict(x=None, x4=P + 8), dict(w=None), dict(w=P + 8), dict(y=None), dict(dtype=3), dict(act=5), dict(ldx=7), dict(ldy=3), dict(res=P, ldr=3), dict(x=P + 2),
-                 dict(bias=P + 2), dict(res=P + 1), dict(z=P + 8, cap=1 << 20), dict(m=2 ** 28 + 1), dict(n=2 ** 28 + 1), dict(k=2 ** 22 + 1), dict(ws=P + 4)):
+                 dict(bias=P + 2), dict(res=P + 1), dict(z=P + 8, cap=1 << 20), dict(m=2 ** 27 + 1), dict(n=2 ** 27 + 1), dict(k=2 ** 22 + 1), dict(ws=P + 4)):
         assert linear(**case) == bad, case
-    assert linear(x=None, x4=P, m=2 ** 28, n=2 ** 28, ldy=2 ** 28) == bad
+    assert linear(x=None, x4=P, m=2 ** 27, n=2 ** 27, ldy=2 ** 27) == bad
     assert linear(z=P, cap=3 * 33 - 1) == room and linear(ws=None) == room and linear(size=mx4.mx4_bytes(3, 8) - 1) == room and linear(m=1, k=2 ** 15 + 1, ldx=2 ** 16, size=64) == room
 
     def inputs(dz=P, wt=P, c=None, act=0, res=None, ldr=8, dx=P, ldx=8, m=2, n=4, k=8, dtype=1, ws=None):
@@ -118,7 +118,7 @@ def test_refusals(mx4):
         return L.eden_mx4_weight_grad(dyt, xt, dw, ldw, m, n, k, 0, ws, 0, None)
 
     assert weight(n=0) == weight(k=0) == 0
-    for case in (dict(dyt=None), dict(xt=None), dict(dw=None), dict(ldw=7), dict(dyt=P + 8), dict(xt=P + 2), dict(dw=P + 2), dict(ws=P + 8), dict(m=2 ** 22 + 1), dict(n=2 ** 28 + 1)):
+    for case in (dict(dyt=None), dict(xt=None), dict(dw=None), dict(ldw=7), dict(dyt=P + 8), dict(xt=P + 2), dict(dw=P + 2), dict(ws=P + 8), dict(m=2 ** 22 + 1), dict(n=2 ** 27 + 1)):
         assert weight(**case) == bad, case
 
 
@@ -126,6 +126,6 @@ def test_calls_that_do_not_fit_are_refused(mx4):
     from paper_2108_08842_amd.eden import EdenError
     x = torch.ones(4, 8)
     for call in (lambda: mx4.quantize(x), lambda: mx4.linear(x, None), lambda: mx4.linear_input_grad(x, x), lambda: mx4.linear_weight_grad(x, x),
-                 lambda: mx4.Mx4(torch.zeros(10 ** 4, dtype=torch.uint8), 4, 8), lambda: mx4.Mx4(torch.zeros(1, dtype=torch.uint8), 2 ** 28 + 1, 8)):
+                 lambda: mx4.Mx4(torch.zeros(10 ** 4, dtype=torch.uint8), 4, 8), lambda: mx4.Mx4(torch.zeros(1, dtype=torch.uint8), 2 ** 27 + 1, 8)):
         with pytest.raises(EdenError):
             call()
