@@ -118,12 +118,13 @@ template <uint32_t DTYPE> struct Eight {
         __builtin_memcpy(&raw, w, sizeof(raw));
     }
 };
-template <uint32_t DTYPE> __device__ inline void store_eight(void *row, uint32_t col, const float (&v)[8], int valid) {
+template <uint32_t DTYPE, bool STREAM = false> __device__ inline void store_eight(void *row, uint32_t col, const float (&v)[8], int valid) {
     using T = typename Elem<DTYPE>::type;
     Vec<T, 8> to;
 #pragma unroll
     for (int i = 0; i < 8; ++i) to.v[i] = (T)v[i];
-    store_some<T, 8>(static_cast<T *>(row) + col, to, valid);
+    if constexpr (STREAM) stream_some<T, 8>(static_cast<T *>(row) + col, to, valid);
+    else store_some<T, 8>(static_cast<T *>(row) + col, to, valid);
 }
 
 // A lane's columns in a row that LANES lanes share, eight at a time.  Loads take no branch.  RAGGED (rows that are no multiple of eight): a lane whose eight columns end behind the
@@ -159,9 +160,9 @@ template <uint32_t DTYPE, int LANES, int CHUNKS, bool RAGGED> struct RowPlace {
             if constexpr (LANES < 64) v.keep(has);
         }
     }
-    __device__ void store(void *row, int c, const float (&v)[8]) const {
+    template <bool STREAM> __device__ void store(void *row, int c, const float (&v)[8]) const {
         if constexpr (RAGGED) {
-            if (valid[c]) store_eight<DTYPE>(row, col[c], v, valid[c]);
+            if (valid[c]) store_eight<DTYPE, STREAM>(row, col[c], v, valid[c]);
         } else if (valid[c]) {
             Vec<T, 8> to;
 #pragma unroll
@@ -169,7 +170,11 @@ template <uint32_t DTYPE, int LANES, int CHUNKS, bool RAGGED> struct RowPlace {
             u32x4 words[sizeof(T) / 2];
             __builtin_memcpy(words, &to, sizeof(to));
 #pragma unroll
-            for (int i = 0; i < (int)sizeof(T) / 2; ++i) *(piece_to_memory)(reinterpret_cast<uintptr_t>(row) + col[c] * (uint32_t)sizeof(T) + 16 * i) = words[i];
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+                const piece_to_memory to_piece = (piece_to_memory)(reinterpret_cast<uintptr_t>(row) + col[c] * (uint32_t)sizeof(T) + 16 * i);
+                if constexpr (STREAM && sizeof(T) == 2) __builtin_nontemporal_store(words[i], to_piece);
+                else *to_piece = words[i];
+            }
         }
     }
 };

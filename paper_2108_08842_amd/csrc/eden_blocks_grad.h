@@ -212,7 +212,7 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) __attribute__((amdgpu_wave
                     float to8[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) to8[i] = k->a.x_scale * d[c][i];
-                    if (has) place.store(row_of<DTYPE, LANES>(k->a.dx, row, k->a.lddx), c, to8);
+                    if (has) place.template store<(LANES >= 64)>(row_of<DTYPE, LANES>(k->a.dx, row, k->a.lddx), c, to8);
                 }
             }
             if constexpr (kBranch) {
@@ -264,7 +264,7 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) __attribute__((amdgpu_wave
                     }
 #pragma unroll
                     for (int c = 0; c < CHUNKS; ++c)
-                        if (has) place.store(row_of<DTYPE, LANES>(k->a.df, row, k->a.lddf), c, d[c]);
+                        if (has) place.template store<(LANES >= 64)>(row_of<DTYPE, LANES>(k->a.df, row, k->a.lddf), c, d[c]);
                 }
             }
             if constexpr (kHeld) now = next;

@@ -22,7 +22,7 @@ __global__ __launch_bounds__(kSpreadThreads) void k_dropout(const typename Elem<
     float to[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) to[i] = bits.of(i) >= random.threshold ? v[i] * scale : 0.0f;
-    store_eight<DTYPE>(y + (size_t)at.row * ldy, at.col, to, valid);
+    store_eight<DTYPE, true>(y + (size_t)at.row * ldy, at.col, to, valid);
 }
 
 // Takes the mean (layer) and the size out of a row.  Behind the row's end its values are zeros, and stay so.
@@ -150,7 +150,7 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 256) __attribute__((amdgpu_wav
                 place.settle(x8[c], c, has);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) r[c][i] = __builtin_fmaf(scale, f[c][i], a.x_scale * x8[c][i]);
-                if (a.r && has) place.store(row_of<DTYPE, LANES>(a.r, row, a.ldr), c, r[c]);
+                if (a.r && has) place.template store<true>(row_of<DTYPE, LANES>(a.r, row, a.ldr), c, r[c]);
             }
         }
         if (!BRANCH || pre) {
@@ -158,7 +158,7 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 256) __attribute__((amdgpu_wav
             weights.apply(r, a.pre, place);
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c)
-                if (has) place.store(row_of<DTYPE, LANES>(a.h, row, a.ldh), c, r[c]);
+                if (has) place.template store<true>(row_of<DTYPE, LANES>(a.h, row, a.ldh), c, r[c]);
         }
     }
 }

@@ -69,6 +69,20 @@ template <class T, int N> __device__ inline void store_some(T *p, const Vec<T, N
     }
 }
 
+// The same past the caches where it is 16 bytes, for results larger than they are.  Neighbouring lanes have to have neighbouring pieces: 32 bytes a lane in two such stores write every line twice.
+template <class T, int N> __device__ inline void stream_some(T *p, const Vec<T, N> &r, int valid) {
+    if constexpr (sizeof(r) == 16) {
+        if (valid >= N) {
+            typedef u32x4 anywhere __attribute__((aligned(2)));
+            u32x4 words;
+            __builtin_memcpy(&words, &r, sizeof(r));
+            __builtin_nontemporal_store(words, reinterpret_cast<anywhere *>(p));
+            return;
+        }
+    }
+    store_some<T, N>(p, r, valid);
+}
+
 // ---- 8-bit checkpoint
 
 // Exponent byte of a block from the bits of its largest |x| (as whole numbers: NaN above infinity above all else).
@@ -267,8 +281,8 @@ __device__ inline void finish_store(const Finish &f, uint32_t row, uint32_t col,
 // The whole end of eight neighbouring columns from `col` on of ROWS rows STEP apart; four lanes side by side have a checkpoint's block.  The rows go
 // through it side by side, so that their reads and exponentials overlap, and the activation is chosen once for all of them (once for each value: 301 x 2056
 // bf16, 64 deep, 9.1 us in place of 5.9).
-// Unless INSIDE, the result has `valid` of the columns (none or less: the lane only takes part in its block's largest value) and `rows` rows.
-template <bool INSIDE, int OP, uint32_t DTYPE, int ROWS, int STEP>
+// STREAM: the result goes past the caches.  Unless INSIDE, the result has `valid` of the columns (none or less: the lane only takes part in its block's largest value) and `rows` rows.
+template <bool INSIDE, int OP, uint32_t DTYPE, int ROWS, int STEP, bool STREAM = false>
 __device__ inline void finish_eight(const Finish &f, uint32_t row, uint32_t rows, uint32_t col, int valid, float (&v)[ROWS][8]) {
     auto has = [&](int r) { return INSIDE || (valid > 0 && row + r * STEP < rows); };
     const int n = INSIDE ? 8 : valid;
@@ -352,7 +366,9 @@ __device__ inline void finish_eight(const Finish &f, uint32_t row, uint32_t rows
                 Vec<T, 8> to;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) to.v[i] = (T)(f.residual ? v[r][i] + (float)added[r].v[i] : v[r][i]);
-                store_some<T, 8>(static_cast<T *>(f.out) + (size_t)(row + r * STEP) * f.ld_out + col, to, n);
+                T *place = static_cast<T *>(f.out) + (size_t)(row + r * STEP) * f.ld_out + col;
+                if constexpr (STREAM) stream_some<T, 8>(place, to, n);
+                else store_some<T, 8>(place, to, n);
             }
     }
 }

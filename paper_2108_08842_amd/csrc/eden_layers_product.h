@@ -90,7 +90,7 @@ __device__ inline void wave_fence() {
 // The end of 32 x 32 T sums that a wave has left in the LDS: eight columns a lane, so that four lanes have a checkpoint's block and a row's
 // results leave in pieces of 16 bytes side by side; up to four rows at a time.
 template <int T> constexpr int kRowFloats = 32 * T + 4;            // the four: neighbouring rows begin in different banks
-template <int OP, uint32_t DTYPE, int T>
+template <int OP, uint32_t DTYPE, int T, bool STREAM = false>
 __device__ inline void finish_rows(const Product &p, const float *sums, uint32_t row0, uint32_t col0, int lane, uint32_t split) {
     constexpr int kLanes = 4 * T, kStep = 64 / kLanes;             // lanes of a row; rows side by side
     constexpr int kRows = 32 / kStep < 4 ? 32 / kStep : 4;
@@ -114,16 +114,16 @@ __device__ inline void finish_rows(const Product &p, const float *sums, uint32_t
                 if (valid > 4) *reinterpret_cast<f32x4 *>(out + (size_t)(kStep * i) * p.partial_ld + 4) = *reinterpret_cast<f32x4 *>(v[i] + 4);
             }
         } else if (inside) {
-            finish_eight<true, OP, DTYPE, kRows, kStep>(p.finish, row, p.rows, col, 8, v);
+            finish_eight<true, OP, DTYPE, kRows, kStep, STREAM>(p.finish, row, p.rows, col, 8, v);
         } else {
-            finish_eight<false, OP, DTYPE, kRows, kStep>(p.finish, row, p.rows, col, valid, v);
+            finish_eight<false, OP, DTYPE, kRows, kStep, STREAM>(p.finish, row, p.rows, col, valid, v);
         }
     }
 }
 
 // The end of a wave's T x T tiles of 32 x 32 through `mine`, its own 32 * kRowFloats<T> floats of the LDS (that nobody else uses any more); row tile i is
 // number i ^ swap from row0 on.
-template <int OP, uint32_t DTYPE, int T>
+template <int OP, uint32_t DTYPE, int T, bool STREAM = false>
 __device__ inline void finish_wave(const Product &p, const f32x16 (&acc)[T][T], float *mine, uint32_t row0, uint32_t col0, int swap, int lane, uint32_t split) {
     for (int i = 0; i < T; ++i) {
         wave_fence();
@@ -140,7 +140,7 @@ __device__ inline void finish_wave(const Product &p, const f32x16 (&acc)[T][T], 
         else if (i == 2) put(acc[T / 2]);
         else put(acc[T - 1]);
         wave_fence();
-        finish_rows<OP, DTYPE, T>(p, mine, row0 + (i ^ swap) * 32, col0, lane, split);
+        finish_rows<OP, DTYPE, T, STREAM>(p, mine, row0 + (i ^ swap) * 32, col0, lane, split);
     }
 }
 

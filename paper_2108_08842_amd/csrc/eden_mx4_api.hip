@@ -32,32 +32,40 @@ struct Shape {
     uint32_t side;
     uint64_t splits;
 };
-// Tiles of 256 x 256, one to a CU, or of 128 x 128, two to a CU, by what a round of each takes in us.  Measured (bf16): a chunk of 256 deep 1.65 in a full round of the former (8192 x 8192: 264 us at 8192 deep, four
+// What an end takes longer than a bare one, us a round of large and of small tiles: the two workgroups of a CU hide some of each other's (8192 x 16384, 4096 deep, in large and in small tiles: bare 312
+// and 317 us, gelu 371 and 361, its slope 439 and 375, gelu and checkpoint 414 and 460, residual 399 and 423, fp32 results 331 and 424; 4096 x 16384, 2048 deep: 94 and 95, 135 and 126, 171 and 131, 154 and 135, 117 and 116).
+struct End {
+    double large, small;
+    End(double l, double s) : large(l), small(s) {}
+    End(const Finish &f, bool fp32)
+        : large((f.codes_in ? 17.0 : f.codes_out ? 14.0 : f.activation ? 8.5 : 0.0) + (f.residual ? 11.0 : 0.0) + (fp32 ? 2.5 : 0.0)),
+          small((f.codes_in ? 4.0 : f.codes_out ? 6.0 : f.activation ? 3.3 : 0.0) + (f.residual ? 6.0 : 0.0) + (fp32 ? 6.5 : 0.0)) {}
+};
+// Tiles of 256 x 256, one to a CU, or of 128 x 128, two to a CU, by what a round of each takes in us.  Measured (bf16): a chunk of 256 deep 1.65 in a full round of the former (8192 x 8192: 250 us at 8192 deep, four
 // rounds), 1.2 where CUs are idle (512 x 4096 x 4096: 28); 1.0 in a full round of the latter (2048 x 4096 x 4096: 25, 1500 x 5120 x 8192: 40), 0.55 with one to a CU (512 x 4096 x 4096: 13.6,
-// 2048 x 2048 x 2048: 10.6); ends 10 and 5 a round.  That puts 4096 x 5120 x 4096 (54 us against 69) and 3000 x 3000 x 1000 (16 against 20) at the latter, 4096 x 4096 x 4096 at the former (42).
+// 2048 x 2048 x 2048: 10.6); bare ends 10 and 4 a round.  That puts 4096 x 5120 x 4096 (54 us against 69) and 3000 x 3000 x 1000 (16 against 20) at the latter, 4096 x 4096 x 4096 at the former (38 against 42).
 // A sum of small tiles is split over workgroups where that is worth the join, a launch and 8 bytes a result and split at 3 TB/s: 256 x 256, 16384 deep, in 16 parts 11 us against 34; 64 x 4096 x 4096 in
-// four 11.2 against 12.2; 1024 x 1024 x 4096 not (two parts: 15.7 against 12.7; four: 20).
-Shape shape_of(uint64_t rows, uint64_t cols, uint64_t depth) {
+// four 11.2 against 12.2; 1024 x 1024 x 4096 not (two parts: 15.7 against 12.7; four: 20).  (The end is not looked at for that: the workspace is asked for without knowing it.)
+Shape shape_of(uint64_t rows, uint64_t cols, uint64_t depth, const End &end) {
     const uint64_t large = tile_count(rows, cols, 256), small = tile_count(rows, cols, 128), chunks = std::max<uint64_t>(1, chunks_of(depth));
-    const double cost_large = (double)(large / 256) * (1.65 * (double)chunks + 10.0) + (large % 256 ? 1.2 * (double)chunks + 11.0 : 0.0);
-    auto cost_small = [&](uint64_t splits) {
+    const double cost_large = (double)(large / 256) * (1.65 * (double)chunks + 10.0 + end.large) + (large % 256 ? 1.2 * (double)chunks + 11.0 + end.large : 0.0);
+    auto cost_small = [&](uint64_t splits, double more) {
         const uint64_t tiles = small * splits, left = tiles % 512;
         const double deep = (double)((chunks + splits - 1) / splits);
         const double join = splits > 1 ? 4.5 + (double)splits * (double)rows * (double)cols * (8.0 / 3e6) : 0.0;
-        return (double)(tiles / 512) * (deep + 5.0) + (left > 256 ? deep + 5.0 : left ? 0.55 * deep + 1.5 : 0.0) + join;
+        return (double)(tiles / 512) * (deep + 4.0 + more) + (left > 256 ? deep + 4.0 + more : left ? 0.55 * deep + 1.5 + more : 0.0) + join;
     };
     Shape best = {128, 1};
-    double cost = cost_small(1);
     for (uint64_t splits = 2; splits <= 64 && splits <= chunks && small * splits <= 512; ++splits)
-        if (cost_small(splits) < cost) cost = cost_small(splits), best.splits = splits;
-    return cost_large < cost ? Shape{256, 1} : best;
+        if (cost_small(splits, 0.0) < cost_small(best.splits, 0.0)) best.splits = splits;
+    return cost_large < cost_small(best.splits, end.small) ? Shape{256, 1} : best;
 }
 
 // Launches a product whose operands and end are set.
 int run(Op op, uint32_t dtype, Product &p, void *workspace, size_t workspace_bytes, void *stream) {
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (workspace == nullptr) workspace_bytes = 0;
-    const Shape shape = shape_of(p.rows, p.cols, p.depth);
+    const Shape shape = shape_of(p.rows, p.cols, p.depth, End(p.finish, op == kWeightGrad || dtype == EDEN_F32));
     if (tile_count(p.rows, p.cols, shape.side) * shape.splits > most_groups(256)) return EDEN_ERR_INVALID_ARG;
     uint64_t splits = shape.splits;
     while (splits > 1 && partial_bytes(p.rows, p.cols, splits) > workspace_bytes) --splits;
@@ -127,7 +135,7 @@ int eden_mx4_restore(const void *packed, uint64_t rows, uint64_t cols, uint32_t 
 
 size_t eden_mx4_workspace_bytes(uint64_t rows, uint64_t cols, uint64_t depth, int quantize) {
     if (!operand_sizes_ok(rows, depth) || !operand_sizes_ok(cols, depth) || rows == 0 || cols == 0) return 0;
-    const uint64_t splits = shape_of(rows, cols, depth).splits;
+    const uint64_t splits = shape_of(rows, cols, depth, End(1e9, 0.0)).splits;       // (those of small tiles, if any end takes them)
     return (splits > 1 ? partial_bytes(rows, cols, splits) : 0) + (quantize ? (mx4_bytes(rows, depth) + 15) / 16 * 16 : 0);
 }
 

@@ -140,7 +140,7 @@ __global__ __launch_bounds__(kThreads) void k_mx4_restore(const uint8_t *packed,
     const uint8_t t = packed[(size_t)rows * chunks * kChunkBytes + exps_at(rows, row, chunk) + within / 4];
     float v[8];
     mx4_values(codes, mx4_unit(t), v);
-    store_eight<DTYPE>(x + row * ldx, col, v, valid_of(col, cols));
+    store_eight<DTYPE, true>(x + row * ldx, col, v, valid_of(col, cols));
 }
 
 // f(workgroups before a launch, workgroups of it, shift, workgroups along a row) until all are launched

@@ -191,7 +191,7 @@ template <int OP, uint32_t DTYPE, int T> __global__ __launch_bounds__(kThreads) 
         } else {
             id = total;
         }
-        finish_wave<OP, DTYPE, T>(p, acc, reinterpret_cast<float *>(lds + (kStage - now)) + wave * 32 * kRowFloats<T>, row0, col0, 0, lane, split);
+        finish_wave<OP, DTYPE, T, true>(p, acc, reinterpret_cast<float *>(lds + (kStage - now)) + wave * 32 * kRowFloats<T>, row0, col0, 0, lane, split);
         if (id >= total) break;
     }
 }
