@@ -122,21 +122,33 @@ class Norm:
 
     def _args(self, like, cols, what):
         weight, bias = self.weight, self.bias
-        return self.code, self.eps, 0 if weight is None else _vector(weight, like, cols, what, "weight"), 0 if bias is None else _vector(bias, like, cols, what, "bias")
+        return (self.code, self.eps, 0 if weight is None else _vector(weight, like, cols, what, "a norm's weight"),
+                0 if bias is None else _vector(bias, like, cols, what, "a norm's bias"))
 
 
 _NO_NORM, _NO_RANDOM = (0, 0.0, 0, 0), (0, 0, 0, 0)
 
 
+# The checks of operands: first the one that nearly all pass, then what is wrong or another layout.  `what` and `name` are put together only for a message.
+
+def _fits(t, like, shape):
+    return t.dtype is like.dtype and t.shape == shape and t.is_contiguous() and not t.requires_grad and t.device == like.device
+
+
 def _vector(v, like, cols, what, name):
-    _same(v, like, what)
+    if _fits(v, like, (cols,)):
+        return v.data_ptr()
+    _same(v, like, f"{what}: {name}")
     if v.dim() != 1 or v.shape[0] != cols or (cols > 1 and v.stride(0) != 1):
         _refuse(f"{what}: {name} is {tuple(v.shape)} with stride {v.stride()}, expected {cols} neighbours")
     return v.data_ptr()
 
 
-def _matrix(t, like, shape, what):
+def _matrix(t, like, shape, what, name):
     """(address, distance between rows) of an operand of that shape."""
+    if _fits(t, like, shape):
+        return t.data_ptr(), shape[-1]
+    what = f"{what}: {name}"
     _same(t, like, what)
     if t.shape != shape:
         _refuse(f"{what} is {tuple(t.shape)}, expected {tuple(shape)}")
@@ -147,11 +159,19 @@ def _gate(gate, like, rows, cols, what):
     """(address, distance between rows, rows) of a gate."""
     if gate.dim() == 1:
         return _vector(gate, like, cols, what, "gate"), cols, 1
-    _same(gate, like, what)
-    address, ld, groups, width = _rows(gate, what)
+    _same(gate, like, f"{what}: gate")
+    address, ld, groups, width = _rows(gate, f"{what}: gate")
     if width != cols or groups < 1 or rows % groups:
         _refuse(f"{what}: gate is {tuple(gate.shape)}, expected {cols} columns and a number of rows that divides {rows}")
     return address, ld, groups
+
+
+def _result(out, shape, like, what, name):
+    """(tensor, address, distance between rows) of `out`, or of a new tensor."""
+    if out is None:
+        out = like.new_empty(shape)
+        return out, out.data_ptr(), shape[-1]
+    return _output(out, shape, like, f"{what}: {name}")
 
 
 def _narrow(cols, what):
@@ -214,17 +234,17 @@ def _join(what, x, f, gate, scale, x_scale, drop, post, pre, out, norm_out, stre
     ldf = ldg = ldr = ldh = cols
     gates, random, post_args = 1, _NO_RANDOM, _NO_NORM
     if f is not None:
-        fp, ldf = _matrix(f, x, shape, f"{what}: f")
+        fp, ldf = _matrix(f, x, shape, what, "f")
         if gate is not None:
-            gp, ldg, gates = _gate(gate, x, rows, cols, f"{what}: gate")
+            gp, ldg, gates = _gate(gate, x, rows, cols, what)
         if drop is not None:
             random = drop._args(device, what)
         if post is not None:
-            post_args = post._args(x, cols, f"{what}: post")
-        r, rp, ldr = _output(out, shape, x, f"{what}: out")
+            post_args = post._args(x, cols, what)
+        r, rp, ldr = _result(out, shape, x, what, "out")
     if pre is not None:
-        pre_args = pre._args(x, cols, f"{what}: pre")
-        h, hp, ldh = _output(norm_out, shape, x, f"{what}: norm_out" if f is not None else f"{what}: out")
+        pre_args = pre._args(x, cols, what)
+        h, hp, ldh = _result(norm_out, shape, x, what, "out" if f is None else "norm_out")
     elif f is None:
         _refuse("norm: without a norm")
     elif norm_out is not None:
@@ -281,53 +301,54 @@ def _join_grad(what, dr, f, dh, r, gate, scale, x_scale, drop, post, pre, into, 
     lddr = lddh = ldr = ldf = ldg = lddf = cols
     gates, random, post_args, pre_args = 1, _NO_RANDOM, _NO_NORM, _NO_NORM
     if dr is not None:
-        drp, lddr = _matrix(dr, like, shape, f"{what}: dr")
+        drp, lddr = _matrix(dr, like, shape, what, "dr")
     if pre is not None:
-        pre_args = pre._args(like, cols, f"{what}: pre")
+        pre_args = pre._args(like, cols, what)
         if dh is not None:
             if r is None:
                 _refuse(f"{what}: dh without r")
-            dhp, lddh = _matrix(dh, like, shape, f"{what}: dh")
-            rp, ldr = _matrix(r, like, shape, f"{what}: r")
+            dhp, lddh = _matrix(dh, like, shape, what, "dh")
+            rp, ldr = _matrix(r, like, shape, what, "r")
     elif dh is not None:
         _refuse(f"{what}: dh without pre")
     if gate is not None:
-        gp, ldg, gates = _gate(gate, like, rows, cols, f"{what}: gate")
+        gp, ldg, gates = _gate(gate, like, rows, cols, what)
     if drop is not None:
         random = drop._args(device, what)
     if post is not None:
-        post_args = post._args(like, cols, f"{what}: post")
+        post_args = post._args(like, cols, what)
     if gate is not None or post is not None:
         if f is None:
             _refuse(f"{what}: f is needed with a gate or post")
-        fp, ldf = _matrix(f, like, shape, f"{what}: f")
-    dx, dxp, lddx = _output(into.dx, shape, like, f"{what}: into.dx")
+        fp, ldf = _matrix(f, like, shape, what, "f")
+    dx, dxp, lddx = _result(into.dx, shape, like, what, "into.dx")
     if branch:
-        df, dfp, lddf = _output(into.df, shape, like, f"{what}: into.df")
+        df, dfp, lddf = _result(into.df, shape, like, what, "into.df")
     elif into.df is not None:
         _refuse(f"{what}: into.df without a branch")
-    sums, addresses, ld_gate_grad, fresh = [None] * 5, [0] * 5, cols, []
-    for i, (name, there) in enumerate((("gate", gate is not None), ("post_weight", post is not None and post.weight is not None), ("post_bias", post is not None and post.bias is not None),
-                                       ("pre_weight", pre is not None and pre.weight is not None), ("pre_bias", pre is not None and pre.bias is not None))):
+    sums, addresses, ld_gate_grad, fresh, sizes = [None] * 5, [0] * 5, cols, [], []
+    there = (gate is not None, post is not None and post.weight is not None, post is not None and post.bias is not None, pre is not None and pre.weight is not None,
+             pre is not None and pre.bias is not None)
+    for i in range(5):
         given = into[2 + i]
-        if not there:
+        if not there[i]:
             if given is not None:
-                _refuse(f"{what}: into.{name} without one")
+                _refuse(f"{what}: into.{into._fields[2 + i]} without one")
         elif given is not None:
-            sums[i], addresses[i], ld = _output(given, gate.shape if i == 0 else (cols,), like, f"{what}: into.{name}", torch.float32)
+            sums[i], addresses[i], ld = _output(given, gate.shape if i == 0 else (cols,), like, f"{what}: into.{into._fields[2 + i]}", torch.float32)
             if i == 0:
                 ld_gate_grad = ld
         elif accumulate:
-            _refuse(f"{what}: nothing to accumulate in for {name}")
+            _refuse(f"{what}: nothing to accumulate in for {into._fields[2 + i]}")
         else:
             fresh.append(i)
+            sizes.append(gates * cols if i == 0 else cols)
     if fresh:
-        # new ones are parts of one allocation, each of whole 64-byte pieces
-        sizes = [gates * cols if i == 0 else cols for i in fresh]
-        parts = like.new_empty(sum((n + 15) // 16 * 16 for n in sizes), dtype=torch.float32).split([(n + 15) // 16 * 16 for n in sizes]) if len(fresh) > 1 else [like.new_empty(sizes[0], dtype=torch.float32)]
-        for i, n, part in zip(fresh, sizes, parts):
-            part = part if part.shape[0] == n else part[:n]
-            sums[i], addresses[i] = part if i or gate.dim() == 1 else part.view(gate.shape), part.data_ptr()
+        # new ones are parts of one allocation
+        flat = like.new_empty(sum(sizes), dtype=torch.float32)
+        for i, part in zip(fresh, flat.split(sizes) if len(fresh) > 1 else (flat,)):
+            addresses[i] = part.data_ptr()
+            sums[i] = part if i or gate.dim() == 1 else part.view(gate.shape)
     ws, size = None, 0
     if any(addresses):
         size = L.eden_join_workspace_bytes(rows, cols, gates, dtype)
