@@ -53,8 +53,8 @@ size_t eden_mx4_workspace_bytes(uint64_t rows, uint64_t cols, uint64_t depth, in
  *   at most EDEN_MX4_ROWS and m k at most EDEN_MX4_VALUES (EDEN_ERR_CAPACITY)
  *   w_packed n x k, bias n or NULL, residual m x n or NULL, y m x n of dtype
  *   z_checkpoint   NULL, or a buffer of eden_checkpoint_bytes(m, n) that gets the 8-bit checkpoint of z */
-#define EDEN_MX4_ROWS 2
-#define EDEN_MX4_VALUES 32768
+#define EDEN_MX4_ROWS 16
+#define EDEN_MX4_VALUES 16384
 int eden_mx4_linear(const void *x, uint64_t ldx, const void *x_packed, const void *w_packed, const void *bias, const void *residual, uint64_t ldr, void *y,
                     uint64_t ldy, void *z_checkpoint, size_t z_capacity, uint64_t m, uint64_t n, uint64_t k, uint32_t dtype, uint32_t activation,
                     void *workspace, size_t workspace_bytes, void *stream);

@@ -2,7 +2,10 @@
 //
 // A workgroup has 32 columns of the result and all rows; its eight waves go through the chunks of 256 in turn, from memory to the matrix cores' registers without the LDS: lane l holds
 // row l % 16 of either operand and blocks 2 (l / 16), + 1 of the chunk, so a load takes whole lines of 16 rows.  The waves' sums meet in the LDS, in the order of the waves.
-// One or two rows that come as values are rounded by every workgroup itself, into the LDS: the weights' first loads are on their way meanwhile.
+// Up to 16384 values are rounded by every workgroup itself, into the LDS: the weights' first loads are on their way meanwhile.
+//
+// In a captured graph, bf16 next to 16384 x 4096 (35.7 MB): one row 8.4 us = 4.2 TB/s, four 10.6, sixteen (rounded by a launch before) 12.6; next to 1024 x 1024 4.0, four 4.1, sixteen 5.4.  With a launch of their
+// own to round x: four rows of 4096 11.6, four of 1024 5.5, sixteen 6.1; eight rows of 4096 rounded by every workgroup 13.4 against 11.9.
 #include "eden_layers_product.h"
 #include "eden_mx4_kernels.h"
 

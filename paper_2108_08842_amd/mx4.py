@@ -26,7 +26,7 @@ from .layers import _act, _check, _dtype, _DTYPES, _elsewhere, _gradient_lost, _
 EXPORTS = ["eden_mx4_bytes", "eden_mx4_quantize", "eden_mx4_sums_bytes", "eden_mx4_restore", "eden_mx4_workspace_bytes", "eden_mx4_linear", "eden_mx4_input_grad", "eden_mx4_weight_grad"]
 CHUNK = 256                                                       # columns of a row's 128 bytes of codes and 8 exponents
 MOST_ROWS, MOST_COLUMNS = 2 ** 27, 2 ** 22
-OWN_ROWS, OWN_VALUES = 2, 32768                                   # up to here linear rounds x without a workspace
+OWN_ROWS, OWN_VALUES = 16, 16384                                 # up to here linear rounds x without a workspace
 _lib = None
 
 

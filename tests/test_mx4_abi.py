@@ -104,7 +104,7 @@ def test_refusals(mx4):
                  dict(bias=P + 2), dict(res=P + 1), dict(z=P + 8, cap=1 << 20), dict(m=2 ** 27 + 1), dict(n=2 ** 27 + 1), dict(k=2 ** 22 + 1), dict(ws=P + 4)):
         assert linear(**case) == bad, case
     assert linear(x=None, x4=P, m=2 ** 27, n=2 ** 27, ldy=2 ** 27) == bad
-    assert linear(z=P, cap=3 * 33 - 1) == room and linear(ws=None) == room and linear(size=mx4.mx4_bytes(3, 8) - 1) == room and linear(m=1, k=2 ** 15 + 1, ldx=2 ** 16, size=64) == room
+    assert linear(z=P, cap=3 * 33 - 1) == room and linear(m=17, ws=None) == room and linear(m=17, size=mx4.mx4_bytes(17, 8) - 1) == room and linear(m=1, k=2 ** 14 + 1, ldx=2 ** 16, size=64) == room
 
     def inputs(dz=P, wt=P, c=None, act=0, res=None, ldr=8, dx=P, ldx=8, m=2, n=4, k=8, dtype=1, ws=None):
         return L.eden_mx4_input_grad(dz, wt, c, act, res, ldr, dx, ldx, m, n, k, dtype, ws, 0, None)
