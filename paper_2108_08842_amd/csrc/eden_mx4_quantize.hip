@@ -61,7 +61,7 @@ __device__ inline uint32_t largest_of_four(uint32_t v) {
 }
 
 template <uint32_t DTYPE, bool STOCHASTIC>
-__global__ __launch_bounds__(kWaves * 64) void k_mx4_columns(const typename Elem<DTYPE>::type *x, size_t ldx, uint32_t rows, uint32_t cols, uint32_t chunks, eden_random random, uint8_t *packed,
+__global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(4))) void k_mx4_columns(const typename Elem<DTYPE>::type *x, size_t ldx, uint32_t rows, uint32_t cols, uint32_t chunks, eden_random random, uint8_t *packed,
                                                              float *sums, uint64_t ld_sums, uint32_t accumulate, uint32_t chunks_each, uint32_t wide) {
     __shared__ uint32_t codes[kWide * 32];                         // column c, block b, word g at 32 c + 4 (b ^ (c / 8 mod 8)) + g
     __shared__ __attribute__((aligned(8))) uint8_t exps[kWide * 8];
