@@ -16,40 +16,48 @@ constexpr int kThreads = 256;
 // neighbouring rows share lines).
 struct ChunkPlace {
     uint32_t row, chunk, within;
-    __device__ ChunkPlace(uint32_t chunks, uint32_t shift, uint32_t before, uint32_t groups) {
-        const uint32_t xcd = blockIdx.x & 7u, each = gridDim.x >> 3, more = gridDim.x & 7u, number = before + xcd * each + min(xcd, more) + (blockIdx.x >> 3);
+    // each: such rows one after the other
+    __device__ ChunkPlace(uint32_t shift, uint32_t before, uint32_t groups, uint32_t each = 1) {
+        const uint32_t xcd = blockIdx.x & 7u, run = gridDim.x >> 3, more = gridDim.x & 7u, number = before + xcd * run + min(xcd, more) + (blockIdx.x >> 3);
         const uint32_t group = number / groups, unit = threadIdx.x / 32;
-        row = group * (8u >> shift) + (unit >> shift);
+        row = group * each * (8u >> shift) + (unit >> shift);
         chunk = ((number - group * groups) << shift) + (unit & ((1u << shift) - 1));
         within = threadIdx.x % 32;
     }
 };
 
 template <uint32_t DTYPE, bool STOCHASTIC>
-__global__ __launch_bounds__(kThreads) void k_mx4_rows(const typename Elem<DTYPE>::type *x, size_t ldx, uint32_t rows, uint32_t cols, uint32_t chunks, eden_random random, uint8_t *packed, uint32_t before, uint32_t shift, uint32_t groups) {
-    const ChunkPlace place(chunks, shift, before, groups);
-    const uint32_t row = place.row, chunk = place.chunk, within = place.within, col = chunk * kChunk + within * 8;
-    const bool has = row < rows && chunk < chunks;                                   // (all lanes take part in the exchanges)
-    Eight<DTYPE> in;
-    in.load(x + (has ? row : 0) * ldx, col, has ? valid_of(col, cols) : 0);
-    float v[8];
-    uint32_t largest = 0;
+__global__ __launch_bounds__(kThreads) void k_mx4_rows(const typename Elem<DTYPE>::type *x, size_t ldx, uint32_t rows, uint32_t cols, uint32_t chunks, eden_random random, uint8_t *packed, uint32_t before, uint32_t shift,
+                                                       uint32_t groups, uint32_t each) {
+    const ChunkPlace place(shift, before, groups, each);
+    const uint32_t chunk = place.chunk, within = place.within, col = chunk * kChunk + within * 8, step = 8u >> shift;
+    const int valid = chunk < chunks ? valid_of(col, cols) : 0;
+    uint64_t state = 0;
+    const uint64_t words = words_of(cols);
+    if constexpr (STOCHASTIC) state = state_of(key_of(random, eden::kStreamRounding), place.row * words + col / 4);
+    for (uint32_t row = place.row, i = 0; i < each; ++i, row += step, state += eden::kPhi * words * step) {
+        const bool has = row < rows && chunk < chunks;             // (all lanes take part in the exchanges)
+        Eight<DTYPE> in;
+        in.load(x + (has ? row : 0) * ldx, col, has ? valid : 0);
+        float v[8];
+        uint32_t largest = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        v[i] = in[i];
-        largest = max(largest, magnitude_bits(v[i]));
+        for (int e = 0; e < 8; ++e) {
+            v[e] = in[e];
+            largest = max(largest, magnitude_bits(v[e]));
+        }
+        const uint32_t t = mx4_exponent(largest_of_quad(largest));
+        uint32_t codes;
+        if constexpr (STOCHASTIC) codes = mx4_codes(v, t, bits_of(state));
+        else codes = mx4_codes(v, t);
+        // the exponents of four blocks, one in each lane's byte, come together
+        uint32_t four = t << (8 * ((within >> 2) & 3));
+        four |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)four, 0x141, 0xF, 0xF, false);
+        four |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)four, 0x140, 0xF, 0xF, false);
+        if (!has) continue;
+        *reinterpret_cast<uint32_t *>(packed + (size_t)(row * (uint64_t)chunks + chunk) * kChunkBytes + within * 4) = codes;
+        if (within % 16 == 0) *reinterpret_cast<uint32_t *>(packed + (size_t)rows * chunks * kChunkBytes + exps_at(rows, row, chunk) + within / 4) = four;
     }
-    const uint32_t t = mx4_exponent(largest_of_quad(largest));
-    uint32_t codes;
-    if constexpr (STOCHASTIC) codes = mx4_codes(v, t, bits_of(key_of(random, eden::kStreamRounding), row * words_of(cols) + col / 4));
-    else codes = mx4_codes(v, t);
-    // the exponents of four blocks, one in each lane's byte, come together
-    uint32_t four = t << (8 * ((within >> 2) & 3));
-    four |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)four, 0x141, 0xF, 0xF, false);
-    four |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)four, 0x140, 0xF, 0xF, false);
-    if (!has) return;
-    *reinterpret_cast<uint32_t *>(packed + (size_t)(row * (uint64_t)chunks + chunk) * kChunkBytes + within * 4) = codes;
-    if (within % 16 == 0) *reinterpret_cast<uint32_t *>(packed + (size_t)rows * chunks * kChunkBytes + exps_at(rows, row, chunk) + within / 4) = four;
 }
 
 constexpr int kWide = 128, kWaves = 8;                             // columns of a workgroup
@@ -133,7 +141,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(4))
 
 template <uint32_t DTYPE>
 __global__ __launch_bounds__(kThreads) void k_mx4_restore(const uint8_t *packed, uint32_t rows, uint32_t cols, uint32_t chunks, typename Elem<DTYPE>::type *x, size_t ldx, uint32_t before, uint32_t shift, uint32_t groups) {
-    const ChunkPlace place(chunks, shift, before, groups);
+    const ChunkPlace place(shift, before, groups);
     const uint32_t row = place.row, chunk = place.chunk, within = place.within, col = chunk * kChunk + within * 8;
     if (row >= rows || col >= cols) return;
     const uint32_t codes = *reinterpret_cast<const uint32_t *>(packed + (size_t)(row * (uint64_t)chunks + chunk) * kChunkBytes + within * 4);
@@ -144,8 +152,8 @@ __global__ __launch_bounds__(kThreads) void k_mx4_restore(const uint8_t *packed,
 }
 
 // f(workgroups before a launch, workgroups of it, shift, workgroups along a row) until all are launched
-template <class F> hipError_t by_chunks(uint32_t rows, uint32_t chunks, F f) {
-    const uint32_t shift = chunks >= 4 ? 2 : chunks >= 2 ? 1 : 0, along = (chunks + (1u << shift) - 1) >> shift, rows_each = 8u >> shift;
+template <class F> hipError_t by_chunks(uint32_t rows, uint32_t chunks, uint32_t each, F f) {
+    const uint32_t shift = chunks >= 4 ? 2 : chunks >= 2 ? 1 : 0, along = (chunks + (1u << shift) - 1) >> shift, rows_each = each * (8u >> shift);
     Spread s = {};
     s.groups = (uint64_t)((rows + rows_each - 1) / rows_each) * along;
     return launches(s, [&](uint32_t before, uint32_t groups) { f(before, groups, shift, along); });
@@ -154,12 +162,13 @@ template <class F> hipError_t by_chunks(uint32_t rows, uint32_t chunks, F f) {
 }  // namespace
 
 hipError_t launch_mx4_rows(uint32_t dtype, const void *x, size_t ldx, uint32_t rows, uint32_t cols, const Rounding &rounding, uint8_t *packed, hipStream_t st) {
-    const uint32_t chunks = chunks_of(cols);
-    return by_chunks(rows, chunks, [&](uint32_t before, uint32_t groups, uint32_t shift, uint32_t along) {
+    // four rows a thread where there is more than the device holds at once: the key of the random numbers is made once for them
+    const uint32_t chunks = chunks_of(cols), each = (uint64_t)rows * chunks >= (1u << 16) ? 4 : 1;
+    return by_chunks(rows, chunks, each, [&](uint32_t before, uint32_t groups, uint32_t shift, uint32_t along) {
         for_type(dtype, [&](auto t) {
             using T = typename Elem<decltype(t)::value>::type;
-            if (rounding.stochastic) k_mx4_rows<decltype(t)::value, true><<<groups, kThreads, 0, st>>>(static_cast<const T *>(x), ldx, rows, cols, chunks, rounding.random, packed, before, shift, along);
-            else k_mx4_rows<decltype(t)::value, false><<<groups, kThreads, 0, st>>>(static_cast<const T *>(x), ldx, rows, cols, chunks, rounding.random, packed, before, shift, along);
+            if (rounding.stochastic) k_mx4_rows<decltype(t)::value, true><<<groups, kThreads, 0, st>>>(static_cast<const T *>(x), ldx, rows, cols, chunks, rounding.random, packed, before, shift, along, each);
+            else k_mx4_rows<decltype(t)::value, false><<<groups, kThreads, 0, st>>>(static_cast<const T *>(x), ldx, rows, cols, chunks, rounding.random, packed, before, shift, along, each);
         });
     });
 }
@@ -181,7 +190,7 @@ hipError_t launch_mx4_columns(uint32_t dtype, const void *x, size_t ldx, uint32_
 
 hipError_t launch_mx4_restore(uint32_t dtype, const uint8_t *packed, uint32_t rows, uint32_t cols, void *x, size_t ldx, hipStream_t st) {
     const uint32_t chunks = chunks_of(cols);
-    return by_chunks(rows, chunks, [&](uint32_t before, uint32_t groups, uint32_t shift, uint32_t along) {
+    return by_chunks(rows, chunks, 1, [&](uint32_t before, uint32_t groups, uint32_t shift, uint32_t along) {
         for_type(dtype, [&](auto t) {
             using T = typename Elem<decltype(t)::value>::type;
             k_mx4_restore<decltype(t)::value><<<groups, kThreads, 0, st>>>(packed, rows, cols, chunks, static_cast<T *>(x), ldx, before, shift, along);

@@ -106,6 +106,15 @@ def test_rounding_is_bit_exact(mx4, dtype, rows, cols, pad):
             assert np.array_equal(out[:, :c].cpu().double().numpy(), ref.values(like, bits).numpy()) and bool((out[:, c:] == 7.0).all())
 
 
+@pytest.mark.parametrize("rows,cols", [(65539, 40), (32779, 300), (16391, 777)])
+def test_rounding_of_many_rows_is_bit_exact(mx4, rows, cols):                    # threads that have several rows, the last ones behind the matrix
+    x = matrix(gen("many", rows, cols), rows, cols, torch.bfloat16, 8)
+    same(mx4.quantize(x), x)
+    into = mx4.Mx4(torch.full((mx4.mx4_bytes(rows, cols) + 64,), 0xA5, dtype=torch.uint8, device="cuda"), rows, cols)
+    same(mx4.quantize(x, rounding=mx4.Stochastic(8, 1), into=into), x, ref.draws(8, 1, rows, cols))
+    assert bool((into.buffer[mx4.mx4_bytes(rows, cols):] == 0xA5).all())
+
+
 @pytest.mark.parametrize("transpose", [False, True])
 def test_stochastic_rounding_keeps_the_expectation(mx4, transpose):
     x = torch.linspace(-6.0, 6.0, 256, device="cuda").repeat(4096, 1)            # 4096 draws of each value, in blocks whose unit is at most 1
