@@ -19,6 +19,7 @@ Dropout.  Calls that share seed and id drop the same places.
 from __future__ import annotations
 
 import ctypes
+import operator
 import struct
 from typing import NamedTuple, Optional
 
@@ -85,7 +86,10 @@ def _random(seed, number, threshold, device, what):
     if not 0 <= number < 2 ** 32:
         _refuse(f"{what}: id {number} is not in 0 .. 2^32 - 1")
     if not isinstance(seed, torch.Tensor):
-        return seed & (2 ** 64 - 1), 0, number, threshold
+        try:
+            return operator.index(seed) & (2 ** 64 - 1), 0, number, threshold
+        except TypeError:
+            _refuse(f"{what}: a seed is a whole number or a tensor, got {type(seed).__name__}")
     if seed.dtype is not torch.int64 or seed.numel() != 1 or (device is not None and seed.device != device) or not seed.is_cuda:
         _refuse(f"{what}: a seed tensor is one int64 on the operands' device, got {seed.numel()} of {seed.dtype} on {seed.device}")
     return 0, seed.data_ptr(), number, threshold

@@ -37,7 +37,7 @@ uint64_t sums_distance(uint64_t cols) { return (cols + 7) / 8 * 8; }
 Share share_of(uint64_t rows, uint64_t cols, uint64_t gates, bool full, bool post, uint64_t most) {
     const int lanes = full ? FullGradShape((uint32_t)cols).lanes : GradShape((uint32_t)cols).lanes, threads = std::max(64, lanes);
     const uint64_t rows_each = 2 * (uint64_t)(threads / lanes);
-    const uint64_t wanted = std::min<uint64_t>(256 * (full && (post || cols > 4096) ? lanes == 512 ? 512 : 768 : 1024) / threads, most);
+    const uint64_t wanted = std::min<uint64_t>(256 * (full && (post || cols > 4096) ? lanes == 512 ? 512 : lanes < 512 ? 768 : 1024 : 1024) / threads, most);
     Share s = {(uint32_t)gates, (uint32_t)(rows / gates), 1, 1, 1};
     if (gates >= wanted || s.group_rows == 0) {
         s.groups_each = (uint32_t)((gates + wanted - 1) / std::max<uint64_t>(wanted, 1));

@@ -15,7 +15,7 @@ namespace eden_layers {
 namespace {
 
 // waves of a SIMD that the registers are shared out to
-constexpr int waves_of(int lanes, int chunks, int post) { return post < 0 || (post == 0 && chunks == 1) ? 4 : lanes == 512 ? 2 : 3; }
+constexpr int waves_of(int lanes, int chunks, int post) { return lanes == 1024 || post < 0 || (post == 0 && chunks == 1) ? 4 : lanes == 512 ? 2 : 3; }
 
 // The operands of a row as they lie in memory
 template <uint32_t DTYPE, int CHUNKS> struct RowOperands {
@@ -26,11 +26,40 @@ template <uint32_t DTYPE, int CHUNKS> struct RowOperands {
 template <uint32_t DTYPE, int LANES, int CHUNKS, bool RAGGED, int PRE, int POST>
 __global__ __launch_bounds__(LANES > 64 ? LANES : 64) __attribute__((amdgpu_waves_per_eu(waves_of(LANES, CHUNKS, POST)))) void k_block_grad(const GradArgs args) {
     constexpr int kThreads = LANES > 64 ? LANES : 64, kRows = kThreads / LANES;
-    constexpr bool kHeld = CHUNKS * sizeof(typename Elem<DTYPE>::type) <= (POST == EDEN_NORM_LAYER ? 2 : 4);       // weights stay in registers, and the next row's operands come while one is worked on
+    constexpr bool kHeld = (POST < 0 || LANES < 1024) && CHUNKS * sizeof(typename Elem<DTYPE>::type) <= (POST == EDEN_NORM_LAYER ? 2 : 4);       // weights stay in registers, and the next row's operands come while one is worked on
     constexpr bool kPacked = sizeof(typename Elem<DTYPE>::type) == 2 && (waves_of(LANES, CHUNKS, POST) == 4 || (CHUNKS == 2 && POST == EDEN_NORM_LAYER));
     constexpr bool kPre = PRE != EDEN_NORM_NONE, kPreLayer = PRE == EDEN_NORM_LAYER, kBranch = POST >= 0, kPost = POST > 0, kPostLayer = POST == EDEN_NORM_LAYER;
     constexpr bool kHas[kAllSums] = {kBranch, kPost, kPostLayer, kPre, kPreLayer};
     __shared__ float shared[kSumFloats<LANES>];
+    // Sums of the gate and of the norm's weights behind the branch, of rows so long that the registers have no place for them: in the LDS, each read and written by its own thread only
+    constexpr bool kFar = kBranch && LANES == 1024;
+    constexpr int kFarSums = kPost ? 2 : 1;
+    __shared__ f32x4 far[kFar ? kFarSums * CHUNKS * 2 : 1][kFar ? LANES : 1];
+    auto far_at = [] {                                             // (made anew each time: kept, the addresses would take a register for every 64 KB)
+        uint32_t at = threadIdx.x;
+        asm volatile("" : "+v"(at));
+        return at;
+    };
+    auto far_load = [&](int s, int c, float (&v)[8]) {
+        const uint32_t at = far_at();
+        const f32x4 low = far[(s * CHUNKS + c) * 2][at], high = far[(s * CHUNKS + c) * 2 + 1][at];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = low[i], v[4 + i] = high[i];
+    };
+    auto far_store = [&](int s, int c, const float (&v)[8]) {
+        const uint32_t at = far_at();
+        far[(s * CHUNKS + c) * 2][at] = f32x4{v[0], v[1], v[2], v[3]};
+        far[(s * CHUNKS + c) * 2 + 1][at] = f32x4{v[4], v[5], v[6], v[7]};
+    };
+    auto far_clear = [&](int s) {
+        const float zeros[8] = {};
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) far_store(s, c, zeros);
+    };
+    if constexpr (kFar) {
+#pragma unroll
+        for (int s = 0; s < kFarSums; ++s) far_clear(s);
+    }
     int turn = 0;
     const eden_join_grad_args &a = args.a;
     typedef const __attribute__((address_space(4))) GradArgs *Arguments;
@@ -59,26 +88,31 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) __attribute__((amdgpu_wave
         if constexpr (kHeld && kPost) held_post[c] = weights_of(a.post.weight, c, 1.0f);
         if constexpr (kHeld && kPostLayer) held_post_bias[c] = weights_of(a.post.bias, c, 0.0f);
     }
-    auto pre_weight = [&](int c) { return kHeld ? held_pre[c] : weights_of(a.pre.weight, c, 1.0f); };
-    auto post_weight = [&](int c) { return kHeld ? held_post[c] : weights_of(a.post.weight, c, 1.0f); };
-    auto post_bias = [&](int c) { return kHeld ? held_post_bias[c] : weights_of(a.post.bias, c, 0.0f); };
+    auto pre_weight = [&](int c) { return kHeld ? held_pre[c] : weights_of(again()->a.pre.weight, c, 1.0f); };
+    auto post_weight = [&](int c) { return kHeld ? held_post[c] : weights_of(again()->a.post.weight, c, 1.0f); };
+    auto post_bias = [&](int c) { return kHeld ? held_post_bias[c] : weights_of(again()->a.post.bias, c, 0.0f); };
     float sums[kAllSums][CHUNKS][8] = {};
 
     // one result's or one part's sums
-    auto put = [&](float (&v)[CHUNKS][8], float *to, bool add) {
+    auto put = [&](int s, float *to, bool add) {
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
+            float v[8];
+            if (kFar && s < kFarSums) far_load(s, c, v);
+            else
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = sums[s][c][i];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
 #pragma unroll
-                for (int d = LANES; d < 64; d *= 2) v[c][i] += __shfl_xor(v[c][i], d);
+                for (int d = LANES; d < 64; d *= 2) v[i] += __shfl_xor(v[i], d);
             }
             if (threadIdx.x < LANES && place.valid[c]) {
                 float *at = to + place.col[c];
                 Vec<float, 8> out;
                 if (add) out = load_some<float, 8>(at, place.valid[c]);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) out.v[i] = add ? out.v[i] + v[c][i] : v[c][i];
+                for (int i = 0; i < 8; ++i) out.v[i] = add ? out.v[i] + v[i] : v[i];
                 store_some<float, 8>(at, out, place.valid[c]);
             }
         }
@@ -91,7 +125,11 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) __attribute__((amdgpu_wave
     for (uint32_t group = first_group; group < end_group; ++group) {
         const uint64_t group_row = (uint64_t)group * share.group_rows;
         auto gate_of = [&](int c) { return weights_of(a.gate ? row_of<DTYPE, LANES>(a.gate, group, a.ld_gate) : nullptr, c, 1.0f); };
-        auto gate = [&](int c) { return kHeld ? held_gate[c] : gate_of(c); };
+        auto gate = [&](int c) {
+            if constexpr (kHeld) return held_gate[c];
+            const Arguments k = again();
+            return weights_of(k->a.gate ? row_of<DTYPE, LANES>(k->a.gate, group, k->a.ld_gate) : nullptr, c, 1.0f);
+        };
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c)
             if constexpr (kHeld && kBranch) held_gate[c] = gate_of(c);
@@ -115,6 +153,7 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) __attribute__((amdgpu_wave
             if constexpr (kHeld) {
                 if (at + kRows < to) load(next, at + kRows);
             } else {
+                now = {};                                          // (what is not there would be carried from row to row)
                 load(now, at);
             }
             const bool has = kRows == 1 || at + sub < to;
@@ -154,6 +193,7 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) __attribute__((amdgpu_wave
                         if constexpr (kPreLayer) three[0] += now.r[c][i], three[2] = __builtin_fmaf(now.dh[c][i], w[i], three[2]);
                         if constexpr (kPostLayer) three[1] += now.f[c][i];
                     }
+                    if constexpr (kFar) __builtin_amdgcn_sched_barrier(0);
                 }
                 stay_packed();
                 sum_in_row<LANES>(three, shared, turn);
@@ -179,6 +219,7 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) __attribute__((amdgpu_wave
                             three[1] = __builtin_fmaf(u, u, three[1]);
                         }
                     }
+                    if constexpr (kFar) __builtin_amdgcn_sched_barrier(0);
                 }
                 stay_packed();
                 sum_in_row<LANES>(three, shared, turn);
@@ -227,6 +268,10 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) __attribute__((amdgpu_wave
                         if constexpr (kPost) w = post_weight(c);
                         if constexpr (kPostLayer) b = post_bias(c);
                         const Eight<DTYPE> g = gate(c);
+                        float far_gate[8], far_weight[8];
+                        if constexpr (kFar) far_load(kGateSum, c, far_gate);
+                        if constexpr (kFar && kPost) far_load(kPostWeight, c, far_weight);
+                        float(&gate_sum)[8] = kFar ? far_gate : sums[kGateSum][c], (&weight_sum)[8] = kFar ? far_weight : sums[kPostWeight][c];
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
                             // behind a row's end d is what a layer norm took out; what is dropped may be anything
@@ -234,10 +279,10 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) __attribute__((amdgpu_wave
                             const float u = kPost ? (now.f[c][i] - mean_f) * rho_f : now.f[c][i];
                             const float v = kPostLayer ? __builtin_fmaf(u, w[i], b[i]) : kPost ? u * w[i] : u;
                             const float back = !DROP && !kPreLayer ? scale * d[c][i] : keep ? scale * d[c][i] : 0.0f;
-                            sums[kGateSum][c][i] = __builtin_fmaf(back, DROP && !keep ? 0.0f : v, sums[kGateSum][c][i]);
+                            gate_sum[i] = __builtin_fmaf(back, DROP && !keep ? 0.0f : v, gate_sum[i]);
                             const float du = DROP && !keep ? 0.0f : back * g[i];
                             if constexpr (kPost) {
-                                sums[kPostWeight][c][i] = __builtin_fmaf(du, u, sums[kPostWeight][c][i]);
+                                weight_sum[i] = __builtin_fmaf(du, u, weight_sum[i]);
                                 if constexpr (kPostLayer) sums[kPostBias][c][i] += du;
                                 d[c][i] = du * w[i];
                                 if constexpr (kPostLayer) two[0] += d[c][i];
@@ -247,6 +292,8 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) __attribute__((amdgpu_wave
                             }
                             if (kPacked && i % 2 == 1) __builtin_amdgcn_sched_barrier(0);       // (all eight side by side would take too many registers)
                         }
+                        if constexpr (kFar) far_store(kGateSum, c, far_gate);
+                        if constexpr (kFar && kPost) far_store(kPostWeight, c, far_weight);
                     }
                 }
                 if (k->a.df) {
@@ -271,7 +318,8 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) __attribute__((amdgpu_wave
         }
         if constexpr (kBranch)
             if (args.sums[kGateSum] && share.splits == 1) {
-                put(sums[kGateSum], args.sums[kGateSum] + group * a.ld_gate_grad, a.accumulate);
+                put(kGateSum, args.sums[kGateSum] + group * a.ld_gate_grad, a.accumulate);
+                if constexpr (kFar) far_clear(kGateSum);
 #pragma unroll
                 for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
@@ -282,7 +330,7 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) __attribute__((amdgpu_wave
 #pragma unroll
     for (int s = 0; s < kAllSums; ++s) {
         if (!kHas[s] || !args.sums[s] || (s == kGateSum && share.splits == 1)) continue;
-        put(sums[s], args.sums[s] + (parts ? worker * args.ld_sums : 0), !parts && a.accumulate);
+        put(s, args.sums[s] + (parts ? worker * args.ld_sums : 0), !parts && a.accumulate);
     }
 }
 

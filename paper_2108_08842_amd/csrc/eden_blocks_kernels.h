@@ -39,13 +39,13 @@ template <int WIDE, int FROM> struct RowShape {
         one(std::integral_constant<int, 128>()), one(std::integral_constant<int, 256>()), one(std::integral_constant<int, 512>()), one(std::integral_constant<int, 1024>());
         two(std::integral_constant<int, 64>()), two(std::integral_constant<int, 128>()), two(std::integral_constant<int, 256>()), two(std::integral_constant<int, 512>());
         two(std::integral_constant<int, 1024>());
-        if constexpr (WIDE < 1024) with(std::integral_constant<int, WIDE>(), std::integral_constant<int, 4>());
     }
 };
 using JoinShape = RowShape<1024, 64>;
-// A gradient with the sums of the gate and of two norms takes more registers than 1024 lanes have (128 each).
+// A gradient with the sums of the gate and of two norms takes more registers than 1024 lanes have (128 each): up to 8192 columns it has 512 lanes at most; beyond, two of its sums are
+// in the LDS (4096 x 16384 bf16, both norms rms, gate, dropout: 461 -> 327 us against 512 lanes with four chunks each and all sums in registers, which spilled; layer norms 890 -> 530).
 using GradShape = RowShape<1024, 1024>;
-using FullGradShape = RowShape<512, 512>;
+using FullGradShape = RowShape<1024, 512>;
 
 // How the rows of a gradient are shared out: `gates` groups of `group_rows` rows.  Either splits workgroups share a group, or a workgroup has
 // `groups_each` whole ones.

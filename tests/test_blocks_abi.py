@@ -123,9 +123,16 @@ def test_calls_that_do_not_fit_are_refused(blocks):
     for call in (lambda: blocks.dropout(x, blocks.Dropout(0.1, 1)), lambda: blocks.norm(x, blocks.Norm("rms")), lambda: blocks.join(x, x), lambda: blocks.join_grad(x, x), lambda: blocks.join(x, None),
                  lambda: blocks.join_grad(None), lambda: blocks.Dropout(1.0, 1), lambda: blocks.Dropout(-0.1, 1), lambda: blocks.Dropout(float("nan"), 1), lambda: blocks.Norm("batch"),
                  lambda: blocks.Norm("rms", None, x[0]), lambda: blocks.Norm("layer", eps=-1.0), lambda: blocks.Norm("layer", eps=float("inf")), lambda: blocks.Norm("layer", eps=1e39), lambda: blocks.norm_grad(None, x, blocks.Norm("rms"), residual=x),
-                 lambda: blocks.norm_grad(x, x, None), lambda: blocks.Dropout(0.1, 1, 2 ** 32)._args(None, "x"), lambda: blocks.Dropout(0.1, torch.tensor(3))._args(None, "x")):
+                 lambda: blocks.norm_grad(x, x, None), lambda: blocks.Dropout(0.1, 1, 2 ** 32)._args(None, "x"), lambda: blocks.Dropout(0.1, torch.tensor(3))._args(None, "x"),
+                 lambda: blocks.Dropout(0.1, 1.5)._args(None, "x")):
         with pytest.raises(EdenError):
             call()
+
+
+def test_seeds_are_whole_numbers_of_any_kind(blocks):
+    import numpy as np
+    for seed, want in ((0, 0), (-1, 2 ** 64 - 1), (2 ** 64 + 5, 5), (np.int64(-3), 2 ** 64 - 3), (np.uint64(2 ** 64 - 1), 2 ** 64 - 1)):
+        assert blocks.Dropout(0.5, seed, 7)._args(None, "x") == (want, 0, 7, 32768)
 
 
 def test_the_reference_gradients_against_autograd():
