@@ -34,6 +34,7 @@ bool gates_ok(const void *gate, const void *gate_grad, uint64_t gates, uint64_t 
 
 uint64_t sums_distance(uint64_t cols) { return (cols + 7) / 8 * 8; }
 // Workgroups that share the rows of a gradient: at most `most`, those that the device holds together, and each with some rows.  full: with a branch, post: and a norm behind it.
+// Two rows each at least: with one, 77 x 1000 writes and reads as many sums again as it has operands (16.8 us against 12.1).
 Share share_of(uint64_t rows, uint64_t cols, uint64_t gates, bool full, bool post, uint64_t most) {
     const int lanes = full ? FullGradShape((uint32_t)cols).lanes : GradShape((uint32_t)cols).lanes, threads = std::max(64, lanes);
     const uint64_t rows_each = 2 * (uint64_t)(threads / lanes);

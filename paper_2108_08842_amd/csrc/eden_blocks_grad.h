@@ -9,12 +9,17 @@
 // Bound by memory: dr, dh, r, f are read once, dx, df written once; statistics are taken again from r and f, which costs a sum over a row that is in
 // registers and keeps no memory.  The sums over rows stay in registers of the workgroups, each of which goes through many rows; a second launch adds what they
 // have.  No atomics: the same bits every time.
+//
+// What counts is registers: sums, operands of this row and of the next (on their way meanwhile, or each row would wait for its loads), weights.  Hence operands stay packed, kinds of norms are compiled in, and the arguments
+// are read again for each row.  bf16, dropout, gate: 8192 x 4096 with rms norms 81 us and 5 for the second launch (403 MB at 4.7 TB/s together), layer norms 103, 32768 x 1024 81 and 91, 8192 x 8192 169 and 248; without a
+// branch 43 and 52.  Above 8192 columns nothing is fetched ahead and some registers go to memory: 4096 x 16384 327 and 530 (a floor of 158).  Rows of 128 columns 35 to 53 us at 131072 of
+// them, 2.7 to 4 TB/s: four rows a wave, and a loop that waits.
 #include "eden_blocks_kernels.h"
 
 namespace eden_layers {
 namespace {
 
-// waves of a SIMD that the registers are shared out to
+// Waves of a SIMD that the registers are shared out to: 512 registers of a lane by the sums and operands of each kind
 constexpr int waves_of(int lanes, int chunks, int post) { return lanes == 1024 || post < 0 || (post == 0 && chunks == 1) ? 4 : lanes == 512 ? 2 : 3; }
 
 // The operands of a row as they lie in memory

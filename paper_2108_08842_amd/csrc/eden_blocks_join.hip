@@ -3,6 +3,10 @@
 // Bound by memory: x and f are read once, r and h written once.  LANES threads share a row and keep it in registers, eight neighbouring columns (16 bytes of a
 // two-byte type) at a time, so the statistics of both norms take no second pass over memory: a sum over the row is a few lane
 // exchanges, for rows of several waves one barrier.  The mean square of a layer norm is taken around the mean, which is known by then: no digits cancel.
+//
+// bf16: 8192 x 4096 with dropout, gate and both norms rms 44 to 47 us (268 MB at 5.7 to 6.1 TB/s, vector instructions in 68% of the cycles), a norm alone 22 (6.1 TB/s), 4096 x 16384 115 and 42; a single token 3,
+// a launch and two trips to memory.  Dropout of 8192 x 8192 45 (6.0 TB/s, vector 59%).  A copy of 1 GiB moves 5.1 TB/s: results of two bytes are stored past the caches, in which they would
+// displace operands (8192 x 16384 dropout 128 -> 100 us).  fp32 results are not: a lane's 32 bytes leave in two stores, so each would write part of a line.
 #include "eden_blocks_kernels.h"
 #include "eden_layers_spread.h"
 
@@ -82,7 +86,7 @@ template <uint32_t DTYPE, int CHUNKS> struct Weights {
     }
 };
 
-// Waves of a SIMD: rows of up to a wave's eights need few registers, and nothing but other waves hides their loads
+// Waves of a SIMD: rows of up to a wave's eights need few registers, and nothing but other waves hides their loads.  (Two chunks a lane: half as many, or the compiler puts operands into memory.)
 template <uint32_t DTYPE> constexpr int waves_of(int lanes, int chunks, bool branch) {
     return lanes == 1024 ? 4 : (DTYPE == EDEN_F32 ? 4 : branch ? 6 : 8) / (chunks == 2 ? 2 : 1);
 }
