@@ -40,29 +40,35 @@ __device__ inline uint32_t mx4_codes(const float (&x)[8], uint32_t t) {
     w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6] * inverse, x[7] * inverse, 1.0f, 3);
     return t == 255u ? 0u : w;
 }
-// 2 times a half of w more than v
-template <bool UPPER> __device__ inline uint32_t add_half_twice(uint32_t w, uint32_t v) {
+// factor times a half of w more than v
+template <bool UPPER> __device__ inline uint32_t add_half_times(uint32_t w, uint32_t factor, uint32_t v) {
     uint32_t r;
-    if constexpr (UPPER) asm("v_mad_u32_u16 %0, %1, 2, %2 op_sel:[1,0,0,0]" : "=v"(r) : "v"(w), "v"(v));
-    else asm("v_mad_u32_u16 %0, %1, 2, %2" : "=v"(r) : "v"(w), "v"(v));
+    if constexpr (UPPER) asm("v_mad_u32_u16 %0, %1, %2, %3 op_sel:[1,0,0,0]" : "=v"(r) : "v"(w), "s"(factor), "v"(v));
+    else asm("v_mad_u32_u16 %0, %1, %2, %3" : "=v"(r) : "v"(w), "s"(factor), "v"(v));
+    return r;
+}
+// The largest whole number up to -v
+__device__ inline uint32_t floor_of_negative(float v) {
+    uint32_t r;
+    asm("v_cvt_flr_i32_f32_e64 %0, -%1" : "=v"(r) : "v"(v));
     return r;
 }
 // Eight values' codes, stochastically.  v = |x| 2^(127 - t) lies between codes 2 e + floor(f) and the next, f = v 2^(1 - e), e = max(exponent of v, 0).  Its share is
-// f - floor(f), and d + 1/2 < 65536 share iff ceil(2^17 f) + 2 (65535 - d) reaches the next multiple of 2^17: whole numbers, so nothing is rounded on the way.  With e at 2^18 (127 more,
-// which makes 254 = -2 mod 256 codes) the code is three bits of one sum.
+// f - floor(f), and d + 1/2 < 65536 share iff ceil(2^28 f) + 4096 (65535 - d) + 2047 reaches the next multiple of 2^28: whole numbers, so nothing is rounded on the way.  With e at 2^29
+// the code is bits 28 to 30 of one sum T; what is added up is -T - 1, whose bits are the inverted ones: -ceil is one instruction, and 156 - (e + 127), the distance that v is moved by, adds -e at 2^29 and
+// otherwise nothing below bit 31, where x's sign goes.  The four topmost bits move into the word from below, the last value's first.
 __device__ inline uint32_t mx4_codes(const float (&x)[8], uint32_t t, const Bits8 &bits) {
     const float inverse = mx4_inverse(t);
     uint32_t w = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 7; i >= 0; --i) {
         const float v = fabsf(x[i]) * inverse;
-        const uint32_t e = __float_as_uint(fmaxf(v, 1.0f)) >> 23;
-        const uint32_t steps = (uint32_t)ceilf(__builtin_amdgcn_ldexpf(v, 145 - (int)e));
-        const uint32_t others = ~bits.pair[i >> 1], sum = (e << 18) + steps;
-        const uint32_t code = ((i & 1 ? add_half_twice<true>(others, sum) : add_half_twice<false>(others, sum)) + (2u << 17)) >> 17 & 7u;
-        w |= (code | ((__float_as_uint(x[i]) >> 28) & 8u)) << (4 * i);
+        const uint32_t by = 156u - (__float_as_uint(fmaxf(v, 1.0f)) >> 23);
+        const uint32_t sum = (by << 29) + floor_of_negative(__builtin_amdgcn_ldexpf(v, (int)by)), d = bits.pair[i >> 1];
+        const uint32_t all = (i & 1 ? add_half_times<true>(d, 4096u, sum) : add_half_times<false>(d, 4096u, sum)) + (2048u - (3u << 28));
+        w = __builtin_amdgcn_alignbit(w, (all & 0x7FFFFFFFu) | (__float_as_uint(x[i]) & 0x80000000u), 28);
     }
-    return t == 255u ? 0u : w;
+    return t == 255u ? 0u : w ^ 0x77777777u;
 }
 __device__ inline void mx4_values(uint32_t codes, float unit, float (&x)[8]) {
     const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.0f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.0f, 1);
