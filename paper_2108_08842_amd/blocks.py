@@ -136,7 +136,7 @@ _NO_NORM, _NO_RANDOM = (0, 0.0, 0, 0), (0, 0, 0, 0)
 # The checks of operands: first the one that nearly all pass, then what is wrong or another layout.  `what` and `name` are put together only for a message.
 
 def _fits(t, like, shape):
-    return t.dtype is like.dtype and t.shape == shape and t.is_contiguous() and not t.requires_grad and t.device == like.device
+    return t.dtype is like.dtype and t.shape == shape and t.is_contiguous() and not t.requires_grad and t.get_device() == like.get_device()
 
 
 def _vector(v, like, cols, what, name):
@@ -350,7 +350,7 @@ def _join_grad(what, dr, f, dh, r, gate, scale, x_scale, drop, post, pre, into, 
     if fresh:
         # new ones are parts of one allocation
         flat = like.new_empty(sum(sizes), dtype=torch.float32)
-        for i, part in zip(fresh, flat.split(sizes) if len(fresh) > 1 else (flat,)):
+        for i, part in zip(fresh, flat.split_with_sizes(sizes) if len(fresh) > 1 else (flat,)):
             addresses[i] = part.data_ptr()
             sums[i] = part if i or gate.dim() == 1 else part.view(gate.shape)
     ws, size = None, 0
