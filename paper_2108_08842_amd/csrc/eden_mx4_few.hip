@@ -1,18 +1,20 @@
 // eden_mx4_linear for up to 16 rows (single tokens, a few tokens at a time): the weights are read once and everything else is small.  Bound by memory: w's bytes.
 //
-// A workgroup has 32 columns of the result and all rows; its eight waves go through the chunks of 256 in turn, from memory to the matrix cores' registers without the LDS: lane l holds
+// A workgroup has 32 columns of the result (16 of a narrow one) and all rows; its eight waves go through the chunks of 256 in turn, from memory to the matrix cores' registers without the LDS: lane l holds
 // row l % 16 of either operand and blocks 2 (l / 16), + 1 of the chunk, so a load takes whole lines of 16 rows.  The waves' sums meet in the LDS, in the order of the waves.
 // Up to 16384 values are rounded by every workgroup itself, into the LDS: the weights' first loads are on their way meanwhile.
 //
 // In a captured graph, bf16 next to 16384 x 4096 (35.7 MB): one row 8.4 us = 4.2 TB/s, four 10.6, sixteen (rounded by a launch before) 12.6; next to 1024 x 1024 4.0, four 4.1, sixteen 5.4.  With a launch of their
 // own to round x: four rows of 4096 11.6, four of 1024 5.5, sixteen 6.1; eight rows of 4096 rounded by every workgroup 13.4 against 11.9.
 #include "eden_layers_product.h"
+#include "eden_layers_spread.h"
 #include "eden_mx4_kernels.h"
 
 namespace eden_layers {
 namespace {
 
-constexpr int kWaves = 8, kCols = 2, kRun = 2;                     // sixteens of columns; chunks on their way at a time
+constexpr int kWaves = 8;
+constexpr uint32_t kNarrow = 16 * 256;                             // columns that 256 CUs have in sixteens
 
 struct Piece4 {
     u32x4 code[2];
@@ -29,8 +31,9 @@ __device__ inline f32x4 multiply4(const Piece4 &a, const Piece4 &b, f32x4 c) {
     return c;
 }
 
-// OWN: x comes as values
-template <uint32_t DTYPE, bool OWN> __global__ __launch_bounds__(kWaves * 64) void k_mx4_few(const Product p, const typename Elem<DTYPE>::type *x, size_t ldx) {
+// OWN: x comes as values; kCols: sixteens of columns
+template <uint32_t DTYPE, bool OWN, int kCols> __global__ __launch_bounds__(kWaves * 64) void k_mx4_few(const Product p, const typename Elem<DTYPE>::type *x, size_t ldx) {
+    constexpr int kRun = 4 / kCols;                                // chunks on their way at a time
     __shared__ f32x4 sums[kWaves][kCols][64];
     __shared__ __attribute__((aligned(16))) uint8_t mine[OWN ? EDEN_MX4_VALUES / 2 + EDEN_MX4_ROWS * kChunkBytes : 16];
     __shared__ __attribute__((aligned(16))) uint8_t my_exps[OWN ? EDEN_MX4_VALUES / kBlock + EDEN_MX4_ROWS * kChunkBlocks : 16];
@@ -129,7 +132,7 @@ template <uint32_t DTYPE, bool OWN> __global__ __launch_bounds__(kWaves * 64) vo
         const uint32_t at = col0 + quad * 4;
         const int valid = (uint32_t)r < p.rows && at < p.cols ? (int)min(4u, p.cols - at) : 0;
         float v[4] = {sum[0], sum[1], sum[2], sum[3]};
-        finish_quad<true, DTYPE>(p, r, col0, at, valid, v);
+        finish_quad<(kCols == 2), DTYPE>(p, r, col0, at, valid, v);
     }
 }
 
@@ -137,19 +140,24 @@ template <uint32_t DTYPE, bool OWN> __global__ __launch_bounds__(kWaves * 64) vo
 
 hipError_t launch_mx4_few(uint32_t dtype, const Product &product, const void *x, size_t ldx, hipStream_t st) {
     Product p = product;
-    const uint32_t groups = (p.cols + 16 * kCols - 1) / (16 * kCols);
+    // 16 columns a workgroup where each CU has one of them at most (a checkpoint's block is 32): one row next to 4096 x 16384 9.5 us against 13.5, 4096 x 4096 4.4 and 5.1, 1024 x 8192 4.8 and 6.9.  With more,
+    // 5000 x 2048 takes 5.0 against 4.1, 8192 x 4096 6.8 against 5.7: the second workgroup of a CU waits as long as the first.
+    const uint32_t wide = p.cols <= kNarrow && p.finish.codes_out == nullptr ? 16 : 32;
+    const uint32_t groups = (p.cols + wide - 1) / wide;
     hipError_t e = hipSuccess;
     for (p.before = 0; p.before < groups && e == hipSuccess; p.before += (uint32_t)most_groups(kWaves * 64)) {
         const uint32_t now = min(groups - p.before, (uint32_t)most_groups(kWaves * 64));
-        auto typed = [&](auto t) {
+        auto typed = [&](auto t, auto cols) {
             constexpr uint32_t DTYPE = decltype(t)::value;
+            constexpr int COLS = decltype(cols)::value;
             using T = typename Elem<DTYPE>::type;
-            if (x) k_mx4_few<DTYPE, true><<<now, kWaves * 64, 0, st>>>(p, static_cast<const T *>(x), ldx);
-            else k_mx4_few<DTYPE, false><<<now, kWaves * 64, 0, st>>>(p, nullptr, 0);
+            if (x) k_mx4_few<DTYPE, true, COLS><<<now, kWaves * 64, 0, st>>>(p, static_cast<const T *>(x), ldx);
+            else k_mx4_few<DTYPE, false, COLS><<<now, kWaves * 64, 0, st>>>(p, nullptr, 0);
         };
-        if (dtype == EDEN_F32) typed(std::integral_constant<uint32_t, EDEN_F32>());
-        else if (dtype == EDEN_F16) typed(std::integral_constant<uint32_t, EDEN_F16>());
-        else typed(std::integral_constant<uint32_t, EDEN_BF16>());
+        for_type(dtype, [&](auto t) {
+            if (wide == 16) typed(t, std::integral_constant<int, 1>());
+            else typed(t, std::integral_constant<int, 2>());
+        });
         e = hipGetLastError();
     }
     return e;
