@@ -61,6 +61,12 @@ Shape shape_of(uint64_t rows, uint64_t cols, uint64_t depth, const End &end) {
     return cost_large < cost_small(best.splits, end.small) ? Shape{256, 1} : best;
 }
 
+// Products by few rows.  Above sixteen of them each workgroup reads as much of x as of w and more: those of a short sum and of a result that is no more than one round of workgroups (two to a CU up to
+// 32 rows).  Both sides' times stand at the kernel.
+bool few(uint64_t rows, uint64_t cols, uint64_t depth) {
+    return rows <= kFewRows || (rows * depth <= 1u << 18 && (rows <= 32 ? cols <= 16384 : rows <= kFewMx4 && cols <= 8192));
+}
+
 // Launches a product whose operands and end are set.
 int run(Op op, uint32_t dtype, Product &p, void *workspace, size_t workspace_bytes, void *stream) {
     const hipStream_t st = static_cast<hipStream_t>(stream);
@@ -168,7 +174,7 @@ int eden_mx4_linear(const void *x, uint64_t ldx, const void *x_packed, const voi
         p.a = to;
         workspace = to + need, workspace_bytes -= need;
     }
-    if (m <= kFewRows) return status(launch_mx4_few(dtype, p, nullptr, 0, st));
+    if (few(m, n, k)) return status(launch_mx4_few(dtype, p, nullptr, 0, st));
     return run(kForward, dtype, p, workspace, workspace_bytes, stream);
 }
 

@@ -19,7 +19,8 @@ hipError_t launch_mx4_restore(uint32_t dtype, const uint8_t *packed, uint32_t ro
 
 // Products: a is rows x depth, b is cols x depth, both packed (Product::a, b); lda, ldb and the widths are not used.  side: of the tiles, 128 or 256
 hipError_t launch_mx4_tiles(Op op, uint32_t dtype, const Product &p, uint32_t side, hipStream_t st);
-// up to kFewRows rows; x: NULL, or the matrix (dtype) that the kernel rounds itself: up to EDEN_MX4_ROWS rows, EDEN_MX4_VALUES values
+constexpr uint32_t kFewMx4 = 64;
+// up to kFewMx4 rows; x: NULL, or the matrix (dtype) that the kernel rounds itself: up to EDEN_MX4_ROWS rows, EDEN_MX4_VALUES values
 hipError_t launch_mx4_few(uint32_t dtype, const Product &p, const void *x, size_t ldx, hipStream_t st);
 
 }  // namespace eden_layers

@@ -5,8 +5,8 @@
 // Transpose: a workgroup has 256 rows of 128 columns, a wave 32 rows of them and a lane eight columns of eight rows: loads of 16 bytes, four lanes to a block, whose codes are a word
 // each; codes and exponents go through the LDS and leave in whole lines.
 //
-// 8192 x 16384 bf16 (268 MB of values, 71 of 4 bits): rows to the nearest 59 us = 5.8 TB/s, stochastically 115 to 125; the transpose to the nearest 68 = 5.0 TB/s, stochastically 106 to 110 with vector
-// instructions in 82% of the cycles, with sums of columns 118 in two launches; restored 45 in a loop (part of it from the last cache), 60 with other work between.
+// 8192 x 16384 bf16 (268 MB of values, 71 of 4 bits): rows to the nearest 58 us = 5.8 TB/s, stochastically 101 to 107; the transpose to the nearest 68 to 71 = 4.9 TB/s, stochastically 103 to 105 with vector
+// instructions in four fifths of the cycles, with sums of columns 109 in two launches; restored 45 in a loop (part of it from the last cache), 60 with other work between.
 // Restoring stores past the caches: 109 -> 47 us.  The transpose by loads of 16 bytes: 166 -> 68 (of single columns by neighbouring lanes before).
 #include "eden_layers_spread.h"
 #include "eden_mx4_kernels.h"
@@ -167,8 +167,8 @@ template <class F> hipError_t by_chunks(uint32_t rows, uint32_t chunks, uint32_t
 }  // namespace
 
 hipError_t launch_mx4_rows(uint32_t dtype, const void *x, size_t ldx, uint32_t rows, uint32_t cols, const Rounding &rounding, uint8_t *packed, hipStream_t st) {
-    // Four rows a thread where there is more than the device holds at once: the key of the random numbers and the first row's word are made once for them (8192 x 16384 stochastically 140 us against 115 to 125,
-    // 8192 x 4096 31 against 28, to the nearest 15.6 against 14.3; 1024 x 4096 is below and takes 6.7 either way)
+    // Four rows a thread where there is more than the device holds at once: the key of the random numbers and the first row's word are made once for them (8192 x 16384 stochastically 140 us against 120,
+    // 8192 x 4096 31 against 28, to the nearest 15.6 against 14.3, with the codes made in more instructions than now; 1024 x 4096 is below and takes 6.7 either way)
     const uint32_t chunks = chunks_of(cols), each = (uint64_t)rows * chunks >= (1u << 16) ? 4 : 1;
     return by_chunks(rows, chunks, each, [&](uint32_t before, uint32_t groups, uint32_t shift, uint32_t along) {
         for_type(dtype, [&](auto t) {
