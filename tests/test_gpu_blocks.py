@@ -206,10 +206,29 @@ def test_join_grad(blocks, dtype, cols):
             check_grad(blocks, dtype, rows, cols, number, (0, 3, 8)[number % 3])
 
 
-@pytest.mark.parametrize("rows,cols", [(5000, 40), (3001, 129), (2100, 1000), (600, 8192)])
+@pytest.mark.parametrize("rows,cols", [(5000, 40), (3001, 129), (2100, 1000), (600, 8192), (600, 8200), (300, 12001)])
 @pytest.mark.parametrize("number", [2, 4, 5, 6])
 def test_join_grad_of_many_rows(blocks, rows, cols, number):
     check_grad(blocks, "bf16", rows, cols, number, 0)
+
+
+@pytest.mark.parametrize("rows,gates,cols", [(600, 300, 8200), (1200, 600, 40), (1030, 515, 1001), (9, 9, 16384)])
+@pytest.mark.parametrize("kind", [None, "rms", "layer"])
+def test_more_gates_than_workgroups(blocks, rows, gates, cols, kind):          # workgroups that have several gates one after the other
+    g = gen("gates", rows, cols, kind)
+    f, dr = (matrix(g, rows, cols, torch.float32) for _ in range(2))
+    gate = matrix(g, gates, cols, torch.float32, 0, 0.5)
+    w = vector(g, cols, torch.float32, 1.0)
+    post = blocks.Norm(kind, w) if kind else None
+    got = blocks.join_grad(dr, f, gate=gate, post=post)
+    want = ref.join_grad(double(dr), double(f), None, None, double(gate), 1.0, 1.0, None, 0.0, (kind, double(w), None, float(np.float32(1e-5))) if kind else None, None)
+    near(got.gate, want["gate"], (kind, cols))
+    near(got.df, want["df"], (kind, cols))
+    if kind:
+        near(got.post_weight, want["post_weight"], (kind, cols))
+    held = torch.full_like(got.gate, 3.0)
+    added = blocks.join_grad(dr, f, gate=gate, into=blocks.JoinGrads(gate=held), accumulate=True) if not kind else None
+    assert added is None or bool(((held - 3.0 - got.gate).abs() <= 2.0 ** -23 * (3.0 + got.gate.abs())).all())
 
 
 @pytest.mark.parametrize("kind", ["rms", "layer"])
