@@ -88,3 +88,40 @@ def test_training_runs(options):
     losses = train.train(senders=2, rows=128, width=64, hidden=128, budget=1, steps=4, **options)
     again = train.train(senders=2, rows=128, width=64, hidden=128, budget=1, steps=4, **options)
     assert len(losses) == 4 and all(0.0 < v < float("inf") for v in losses) and losses == again
+
+
+@pytest.mark.parametrize("norm,dropout", [("rms", 0.0), ("layer", 0.1), ("rms", 0.3)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_four_bit_block_with_a_norm(norm, dropout, dtype):
+    """What the norm, the gate and the residual do with the 4-bit products' results, against 64 bits: the gradient of x, and those of the gate and of the norm's weight and bias."""
+    import numpy as np
+    from paper_2108_08842_amd import blocks, mx4
+    from tests.test_gpu_blocks import near
+    block, weights, x, dy, y, kept, gradient, dx = made(norm, dropout, True, dtype)
+    pre, gate, drop = block._around(weights, SEED)
+    f, threshold = kept[4], drop.threshold if drop else 0
+    mask, p = (bref.kept(SEED, 0, threshold, ROWS, WIDTH), threshold / 65536) if drop else (None, 0.0)
+
+    def double(t):
+        return None if t is None else t.cpu().double()
+    joined = bref.join(double(x), double(f), double(gate), 1.0, 1.0, mask, p, None, None)
+    near(y, joined["r"], "y")
+    split = bref.join_grad(double(dy), double(f), None, None, double(gate), 1.0, 1.0, mask, p, None, None)
+    parts = block.parts(gradient)
+    near(parts[4], split["gate"], "gate")
+    # the gradient that reaches the norm: both layers' products of what was rounded, each held against 64 bits by itself
+    df = blocks.join_grad(dy, f, gate=gate, dropout=drop).df
+    near(df, split["df"], "df")
+    off = 1.5 * mref.norm_bound(WIDTH, dtype) + 2.0 ** -20
+
+    def rounded(v, number):
+        return mref.values(v, mref.draws(SEED, number, *v.shape))
+    dz = mx4.linear_input_grad(mx4.quantize(df, rounding=mx4.Stochastic(SEED, 1)), weights[-1], activation="gelu", checkpoint=kept[1], dtype=dtype)
+    dn = mx4.linear_input_grad(mx4.quantize(dz, rounding=mx4.Stochastic(SEED, 3)), weights[-3], dtype=dtype)
+    assert lref.rel(dn.cpu(), rounded(dz, 3) @ mref.values(weights[0].t().contiguous()).t()) <= off
+    want = bref.join_grad(double(dy), None, double(dn), double(x), None, 1.0, 1.0, None, 0.0, None, (norm, double(pre.weight), double(pre.bias), float(np.float32(1e-5))))
+    near(dx, want["dx"], "dx")
+    near(parts[5], want["pre_weight"], "norm's weight")
+    if norm == "layer":
+        near(parts[6], want["pre_bias"], "norm's bias")
+    assert len(parts) == (7 if norm == "layer" else 6)
