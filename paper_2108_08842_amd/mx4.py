@@ -12,7 +12,7 @@ A block of 32 values has a power of two, the smallest that reaches its largest v
 rows of what is rounded, products sum along them: hence the transposes.  Both operands of a product are Mx4 of (rows, depth).
 
 Tensors, streams, errors and autograd are as in layers.py: float32, float16 or bfloat16 on the GPU, dimensions in front of the last are rows at one distance, what
-does not fit raises EdenError before anything is launched.
+does not fit raises EdenError before anything is launched.  Where autograd records, quantize refuses what requires a gradient, weights among it (torch.no_grad() or detach()).
 """
 from __future__ import annotations
 
@@ -113,13 +113,15 @@ class Mx4:
 
 def quantize(x, transpose: bool = False, rounding: Stochastic = None, into: Mx4 = None, sums=False, accumulate: bool = False, stream=None):
     """The 4 bits of x, or of its transpose.  `rounding`: None for the nearest; `into`: an Mx4 of the same size that is overwritten.  With `sums` (transpose only; True, or a
-    float32 tensor that is written or, with `accumulate`, added to) also the sums of x's columns: (Mx4, sums)."""
+    float32 tensor that is written or, with `accumulate`, added to) also the sums of x's columns: (Mx4, sums).  x is refused where it requires a gradient and autograd records."""
     dtype = _dtype(x, "quantize: x")
     device = x.device
     if _elsewhere(device, stream):
         with _On(device, stream):
             return quantize(x, transpose, rounding, into, sums, accumulate)
     L = _lib or lib()
+    if x.requires_grad:
+        _gradient_lost("quantize: x")                              # (here, since an Mx4 no longer says where it comes from)
     p, ld, rows, cols = _rows(x, "quantize: x")
     r, c = (cols, rows) if transpose else (rows, cols)
     _sizes(r, c, "quantize")
