@@ -83,6 +83,10 @@ def lib():
 
 def _random(seed, number, threshold, device, what):
     """The fields of RandomArgs for a seed that is a number, or an int64 tensor on the device."""
+    try:
+        number = operator.index(number)
+    except TypeError:
+        _refuse(f"{what}: an id is a whole number, got {number!r}")
     if not 0 <= number < 2 ** 32:
         _refuse(f"{what}: id {number} is not in 0 .. 2^32 - 1")
     if not isinstance(seed, torch.Tensor):

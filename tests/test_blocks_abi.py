@@ -135,6 +135,23 @@ def test_seeds_are_whole_numbers_of_any_kind(blocks):
         assert blocks.Dropout(0.5, seed, 7)._args(None, "x") == (want, 0, 7, 32768)
 
 
+def test_ids_are_whole_numbers_of_any_kind(blocks):
+    import numpy as np
+    from paper_2108_08842_amd import mx4
+    from paper_2108_08842_amd.eden import EdenError
+
+    def args(number):
+        rounding = mx4.Stochastic(5, number)                       # as mx4.quantize reads it
+        assert blocks._random(rounding.seed, rounding.id, 0, None, "x")[2] == number
+        return blocks.Dropout(0.5, 5, number)._args(None, "x")
+    for number in (0, 2 ** 32 - 1, np.int32(7), np.uint64(9), torch.tensor(3)):
+        assert args(number) == (5, 0, int(number), 32768) and len(blocks._RANDOM_ARGS.pack(*args(number))) == 24
+    for bad in (1.5, 2.0, "3", None, torch.tensor(1.5), -1, 2 ** 32, np.int64(-1), float("nan")):
+        for call in (lambda: blocks.Dropout(0.5, 5, bad)._args(None, "x"), lambda: blocks._random(5, bad, 0, None, "quantize")):
+            with pytest.raises(EdenError):
+                call()
+
+
 def test_the_reference_gradients_against_autograd():
     """The formulas of the tests' reference, in 64 bits, against torch's own differentiation of the forward formulas."""
     g = torch.Generator().manual_seed(4)
