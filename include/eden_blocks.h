@@ -57,7 +57,7 @@ typedef struct eden_join_args {
     uint64_t gates;
     eden_norm post, pre;
     eden_random random;
-    float x_scale, scale;          /* finite */
+    float x_scale, scale;          /* finite, scale 65536 / (65536 - threshold) too */
     uint32_t dtype;
 } eden_join_args;
 int eden_join(const eden_join_args *args, void *stream);

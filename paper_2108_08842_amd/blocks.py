@@ -217,7 +217,8 @@ def norm(x, pre: Norm, out=None, stream=None):
 
 def join(x, f, gate=None, scale: float = 1.0, x_scale: float = 1.0, dropout: Optional[Dropout] = None, post: Optional[Norm] = None, pre: Optional[Norm] = None, out=None,
          norm_out=None, stream=None):
-    """r = x_scale x + scale gate * dropout(post(f)); with `pre` (r, pre(r)).  `out` may be x or f, `norm_out` may be x or f."""
+    """r = x_scale x + scale gate * dropout(post(f)); with `pre` (r, pre(r)).  `out` may be x or f, `norm_out` may be x or f.  Both scales, and scale / (1 - p), are finite in
+    float32."""
     if f is None:
         _refuse("join: f is missing")
     r, h = _join("join", x, f, gate, scale, x_scale, dropout, post, pre, out, norm_out, stream)

@@ -23,6 +23,8 @@ bool matrix_ok(const void *p, uint64_t ld, uint64_t rows, uint64_t cols, size_t 
 }
 bool optional_ok(const void *p, uint64_t ld, uint64_t rows, uint64_t cols, size_t element) { return p == nullptr || matrix_ok(p, ld, rows, cols, element); }
 bool random_ok(const eden_random &r) { return r.threshold <= 65535 && aligned(r.seed_at, 8); }
+// scale times what kept values are multiplied by is one factor of the kernels: infinite, it would make NaN of zeros
+bool scales_ok(float scale, float x_scale, const eden_random &r) { return std::isfinite(scale * kept_scale(r.threshold)) && std::isfinite(x_scale); }
 bool norm_ok(const eden_norm &n, size_t element) {
     if (n.kind > EDEN_NORM_LAYER) return false;
     if (n.kind == EDEN_NORM_NONE) return n.weight == nullptr && n.bias == nullptr;
@@ -76,7 +78,7 @@ int eden_join(const eden_join_args *args, void *stream) {
     if (args == nullptr || !known_type(args->dtype) || !sizes_ok(args->rows, args->cols)) return EDEN_ERR_INVALID_ARG;
     eden_join_args a = *args;
     const size_t e = bytes_of(a.dtype);
-    if (!random_ok(a.random) || !norm_ok(a.post, e) || !norm_ok(a.pre, e) || !std::isfinite(a.scale) || !std::isfinite(a.x_scale)) return EDEN_ERR_INVALID_ARG;
+    if (!random_ok(a.random) || !norm_ok(a.post, e) || !norm_ok(a.pre, e) || !scales_ok(a.scale, a.x_scale, a.random)) return EDEN_ERR_INVALID_ARG;
     const bool empty = a.rows == 0 || a.cols == 0, normed = a.pre.kind != EDEN_NORM_NONE;
     if (!matrix_ok(a.x, a.ldx, a.rows, a.cols, e) || !optional_ok(a.f, a.ldf, a.rows, a.cols, e) || !optional_ok(a.r, a.ldr, a.rows, a.cols, e) ||
         !optional_ok(a.h, a.ldh, a.rows, a.cols, e) || !gates_ok(a.gate, nullptr, a.gates, a.rows) || !optional_ok(a.gate, a.ld_gate, a.gates, a.cols, e))
@@ -102,7 +104,7 @@ int eden_join_grad(const eden_join_grad_args *args, void *stream) {
     eden_join_grad_args &a = g.a;
     const size_t e = bytes_of(a.dtype);
     const bool normed = a.pre.kind != EDEN_NORM_NONE, post = a.post.kind != EDEN_NORM_NONE;
-    if (!random_ok(a.random) || !norm_ok(a.post, e) || !norm_ok(a.pre, e) || !std::isfinite(a.scale) || !std::isfinite(a.x_scale) || !aligned(a.workspace, 16))
+    if (!random_ok(a.random) || !norm_ok(a.post, e) || !norm_ok(a.pre, e) || !scales_ok(a.scale, a.x_scale, a.random) || !aligned(a.workspace, 16))
         return EDEN_ERR_INVALID_ARG;
     const void *mats[] = {a.dr, a.dh, a.r, a.f, a.dx, a.df};
     const uint64_t lds[] = {a.lddr, a.lddh, a.ldr, a.ldf, a.lddx, a.lddf};

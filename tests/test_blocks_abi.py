@@ -152,6 +152,18 @@ def test_ids_are_whole_numbers_of_any_kind(blocks):
                 call()
 
 
+def test_scales_that_leave_the_range_with_dropout_are_refused(blocks):
+    """scale 65536 / (65536 - threshold) multiplies what is kept: infinite, it would make NaN of the zeros of what is dropped."""
+    L, most, half = blocks.lib(), 3.4028234e38, 32768
+    for rows, scale, threshold, want in ((0, most, 0, 0), (0, most / 2.01, half, 0), (4, most / 1.9, half, -1), (4, -most, 1, -1), (0, 1e33, 65535, 0), (4, 1e34, 65535, -1)):
+        a = blocks.JoinArgs(rows=rows, cols=8, x=P, f=P, r=P, ldx=8, ldf=8, ldr=8, gates=1, x_scale=1.0, scale=scale)
+        a.random.threshold = threshold
+        assert L.eden_join(bytes(a), None) == want, (scale, threshold)
+        a = blocks.JoinGradArgs(rows=rows, cols=8, dr=P, f=P, dx=None if rows == 0 else P, lddr=8, ldf=8, lddx=8, lddf=8, gates=1, x_scale=1.0, scale=scale, branch=1)
+        a.random.threshold = threshold
+        assert L.eden_join_grad(bytes(a), None) == want, (scale, threshold)
+
+
 def test_the_reference_gradients_against_autograd():
     """The formulas of the tests' reference, in 64 bits, against torch's own differentiation of the forward formulas."""
     g = torch.Generator().manual_seed(4)
