@@ -252,6 +252,16 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) __attribute__((amdgpu_wave
                     }
                 }
             }
+            if constexpr (kPre && !kPreLayer && kPost) {
+                // Behind a row's end d is 0, or NaN where the row's statistics are: the norm behind the branch would add it up.  (Full rows go past it here; as one more
+                // condition of `keep` below 8192 x 4096 bf16 takes 76 to 83 us in place of 74 to 77.)
+                if (place.partial) {
+#pragma unroll
+                    for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) d[c][i] = place.inside(c, i) ? d[c][i] : 0.0f;
+                }
+            }
             if (k->a.dx) {
 #pragma unroll
                 for (int c = 0; c < CHUNKS; ++c) {
