@@ -7,7 +7,7 @@
  * Conventions are those of eden_layers.h: status codes, device pointers, row-major matrices with a distance between rows, streams,
  * no allocation, no memset, no synchronisation; a call may be captured in a HIP graph, and calls may run on any streams at once if their buffers
  * do not overlap.  Rows have up to EDEN_MOST_COLUMNS columns, there are up to 2^30 of them; either may be 0.
- * Values, statistics and sums are fp32 (a row's mean square has to be in its range); every result is rounded once, to nearest even.
+ * Values, statistics and sums are fp32; a row's mean square has to be in its range, the sum of its squares need not.  Every result is rounded once, to nearest even.
  *
  * Random numbers: the words of the hash of eden.h.  Row i, column j of a matrix of c columns has bits 16 (j mod 4) .. + 15 of word
  * i ceil(c / 4) + floor(j / 4) of the stream's key for (seed, id).  Nothing is stored: the backward pass names the same seed and id.

@@ -63,6 +63,22 @@ template <int LANES, int N> __device__ inline void sum_in_row(float (&v)[N], flo
 }
 template <int LANES> constexpr int kSumFloats = LANES > 64 ? 6 * (LANES / 64) : 1;       // N up to 3
 
+// What a norm multiplies a row by: 1 / sqrt(sum / cols + eps), each = 1 / cols, `sum` that of the squares.  The mean of the squares may be in fp32's range where their sum, or one of them, is
+// not (rows of 16384 values of 2^57): then it is taken once more of values 2^-72 times as large, behind a branch that a whole wave takes or does not.  squares(by): the lane's part of the sum for
+// values times `by`.
+constexpr float kMostFinite = 3.402823466e+38f;
+template <int LANES, class F> __device__ inline float rho_of(float sum, float each, float eps, float *shared, int turn, F squares) {
+    float rho = rsqrtf(sum * each + eps);
+    const bool past = sum > kMostFinite;
+    if (__builtin_expect(__builtin_amdgcn_readfirstlane((int)(LANES >= 64 ? past : __any(past))), 0)) {
+        float again[1] = {squares(0x1p-72f)};
+        sum_in_row<LANES>(again, shared, turn);
+        if constexpr (LANES > 64) __syncthreads();                 // (the caller's next sum has the same turn)
+        if (past) rho = 0x1p-72f * rsqrtf(again[0] * each + 0x1p-144f * eps);
+    }
+    return rho;
+}
+
 // ---- eight values of a row, as they lie in memory
 
 // 16 bytes of memory at any multiple of two (what the part asks for at most), in its own address space: a flat address would wait for the LDS as well

@@ -19,8 +19,9 @@
 namespace eden_layers {
 namespace {
 
-// Waves of a SIMD that the registers are shared out to: 512 registers of a lane by the sums and operands of each kind
-constexpr int waves_of(int lanes, int chunks, int post) { return lanes == 1024 || post < 0 || (post == 0 && chunks == 1) ? 4 : lanes == 512 ? 2 : 3; }
+// Waves of a SIMD that the registers are shared out to: 512 registers of a lane by the sums and operands of each kind.  wide: operands of four bytes next to a norm in front (512 lanes without a norm behind
+// the branch, 8192 x 4096 fp32: two waves, nothing in memory, 175 us rms and 177 layer; four, 8 to 31 registers in memory, 190 and 200)
+constexpr int waves_of(int lanes, int chunks, int post, bool wide) { return lanes == 1024 || post < 0 || (post == 0 && chunks == 1 && !(wide && lanes == 512)) ? 4 : lanes == 512 ? 2 : 3; }
 
 // The operands of a row as they lie in memory
 template <uint32_t DTYPE, int CHUNKS> struct RowOperands {
@@ -29,10 +30,10 @@ template <uint32_t DTYPE, int CHUNKS> struct RowOperands {
 
 // PRE, POST: kinds of the norms; POST -1: no branch
 template <uint32_t DTYPE, int LANES, int CHUNKS, bool RAGGED, int PRE, int POST>
-__global__ __launch_bounds__(LANES > 64 ? LANES : 64) __attribute__((amdgpu_waves_per_eu(waves_of(LANES, CHUNKS, POST)))) void k_block_grad(const GradArgs args) {
+__global__ __launch_bounds__(LANES > 64 ? LANES : 64) __attribute__((amdgpu_waves_per_eu(waves_of(LANES, CHUNKS, POST, DTYPE == EDEN_F32 && PRE != EDEN_NORM_NONE)))) void k_block_grad(const GradArgs args) {
     constexpr int kThreads = LANES > 64 ? LANES : 64, kRows = kThreads / LANES;
     constexpr bool kHeld = (POST < 0 || LANES < 1024) && CHUNKS * sizeof(typename Elem<DTYPE>::type) <= (POST == EDEN_NORM_LAYER ? 2 : 4);       // weights stay in registers, and the next row's operands come while one is worked on
-    constexpr bool kPacked = sizeof(typename Elem<DTYPE>::type) == 2 && (waves_of(LANES, CHUNKS, POST) == 4 || (CHUNKS == 2 && POST == EDEN_NORM_LAYER));
+    constexpr bool kPacked = sizeof(typename Elem<DTYPE>::type) == 2 && (waves_of(LANES, CHUNKS, POST, false) == 4 || (CHUNKS == 2 && POST == EDEN_NORM_LAYER));
     constexpr bool kPre = PRE != EDEN_NORM_NONE, kPreLayer = PRE == EDEN_NORM_LAYER, kBranch = POST >= 0, kPost = POST > 0, kPostLayer = POST == EDEN_NORM_LAYER;
     constexpr bool kHas[kAllSums] = {kBranch, kPost, kPostLayer, kPre, kPreLayer};
     __shared__ float shared[kSumFloats<LANES>];
@@ -228,7 +229,31 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) __attribute__((amdgpu_wave
                 }
                 stay_packed();
                 sum_in_row<LANES>(three, shared, turn);
-                if (has) rho_r = rsqrtf(three[0] * each + k->a.pre.eps), rho_f = rsqrtf(three[1] * each + k->a.post.eps);       // (of rows that are none, 0 times 0 and not times 1 / 0)
+                if constexpr (kPre)
+                    rho_r = rho_of<LANES>(three[0], each, k->a.pre.eps, shared, turn, [&](float by) {
+                        float sum = 0.0f;
+#pragma unroll
+                        for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                const float n = kPreLayer && !inside(c, i) ? 0.0f : (now.r[c][i] - mean_r) * by;
+                                sum = __builtin_fmaf(n, n, sum);
+                            }
+                        return sum;
+                    });
+                if constexpr (kPost)
+                    rho_f = rho_of<LANES>(three[1], each, k->a.post.eps, shared, turn, [&](float by) {
+                        float sum = 0.0f;
+#pragma unroll
+                        for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                const float u = kPostLayer && !inside(c, i) ? 0.0f : (now.f[c][i] - mean_f) * by;
+                                sum = __builtin_fmaf(u, u, sum);
+                            }
+                        return sum;
+                    });
+                if (!has) rho_r = rho_f = 0.0f;                    // (of rows that are none, 0 times 0 and not times 1 / 0)
                 inner = three[2] * rho_r * each;
             }
             float d[CHUNKS][8];
@@ -237,8 +262,8 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) __attribute__((amdgpu_wave
 #pragma unroll
                 for (int i = 0; i < 8; ++i) d[c][i] = now.dr[c][i];
             if constexpr (kPre) {
-                // rho (g - mean_g - n rho inner), n = r - mean_r
-                const float c0 = -rho_r * mean_g, c1 = -rho_r * rho_r * inner;
+                // rho (g - mean_g - n rho inner), n = r - mean_r: in this order, for rho^2 may be below the range where rho n is not
+                const float c1 = -rho_r * inner;
 #pragma unroll
                 for (int c = 0; c < CHUNKS; ++c) {
                     const Eight<DTYPE> w = pre_weight(c);
@@ -247,7 +272,7 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) __attribute__((amdgpu_wave
                         const float dh = now.dh[c][i], n = now.r[c][i] - mean_r;
                         sums[kPreWeight][c][i] = __builtin_fmaf(dh, n * rho_r, sums[kPreWeight][c][i]);
                         if constexpr (kPreLayer) sums[kPreBias][c][i] += dh;
-                        d[c][i] += __builtin_fmaf(rho_r, dh * w[i], kPreLayer ? __builtin_fmaf(c1, n, c0) : c1 * n);
+                        d[c][i] = __builtin_fmaf(rho_r, __builtin_fmaf(c1, n, kPreLayer ? __builtin_fmaf(dh, w[i], -mean_g) : dh * w[i]), d[c][i]);
                         if (kPacked && i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
                     }
                 }
@@ -315,13 +340,14 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) __attribute__((amdgpu_wave
                     if constexpr (kPost) {
                         stay_packed();
                         sum_in_row<LANES>(two, shared, turn);
-                        const float c0 = -rho_f * (two[0] * each), c1 = -rho_f * rho_f * (two[1] * each);
+                        const float c0 = -rho_f * (two[0] * each), c1 = -rho_f * (two[1] * each);
 #pragma unroll
                         for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
                             for (int i = 0; i < 8; ++i) {
                                 const float u = now.f[c][i] - mean_f;
-                                d[c][i] = __builtin_fmaf(rho_f, d[c][i], kPostLayer ? __builtin_fmaf(c1, u, c0) : c1 * u);
+                                const float v = __builtin_fmaf(c1, u, d[c][i]);
+                                d[c][i] = kPostLayer ? __builtin_fmaf(rho_f, v, c0) : rho_f * v;
                             }
                     }
 #pragma unroll

@@ -52,7 +52,14 @@ __device__ inline void standardise(float (&v)[CHUNKS][8], const eden_norm &norm,
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum[0] = __builtin_fmaf(v[c][i], v[c][i], sum[0]);
     sum_in_row<LANES>(sum, shared, turn);
-    const float scale = rsqrtf(sum[0] * each + norm.eps);
+    const float scale = rho_of<LANES>(sum[0], each, norm.eps, shared, turn, [&](float by) {
+        float s = 0.0f;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s = __builtin_fmaf(v[c][i] * by, v[c][i] * by, s);
+        return s;
+    });
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
