@@ -298,43 +298,40 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 64) __attribute__((amdgpu_wave
             }
             if constexpr (kBranch) {
                 float two[2] = {0.0f, 0.0f};
-                {
-                    constexpr bool DROP = true;
 #pragma unroll
-                    for (int c = 0; c < CHUNKS; ++c) {
-                        Bits8 bits = {};
-                        if (k->a.random.threshold) bits = bits_of(key, row * words_of(cols) + place.col[c] / 4);
-                        Eight<DTYPE> w, b;
-                        if constexpr (kPost) w = post_weight(c);
-                        if constexpr (kPostLayer) b = post_bias(c);
-                        const Eight<DTYPE> g = gate(c);
-                        float far_gate[8], far_weight[8];
-                        if constexpr (kFar) far_load(kGateSum, c, far_gate);
-                        if constexpr (kFar && kPost) far_load(kPostWeight, c, far_weight);
-                        float(&gate_sum)[8] = kFar ? far_gate : sums[kGateSum][c], (&weight_sum)[8] = kFar ? far_weight : sums[kPostWeight][c];
+                for (int c = 0; c < CHUNKS; ++c) {
+                    Bits8 bits = {};
+                    if (k->a.random.threshold) bits = bits_of(key, row * words_of(cols) + place.col[c] / 4);
+                    Eight<DTYPE> w, b;
+                    if constexpr (kPost) w = post_weight(c);
+                    if constexpr (kPostLayer) b = post_bias(c);
+                    const Eight<DTYPE> g = gate(c);
+                    float far_gate[8], far_weight[8];
+                    if constexpr (kFar) far_load(kGateSum, c, far_gate);
+                    if constexpr (kFar && kPost) far_load(kPostWeight, c, far_weight);
+                    float(&gate_sum)[8] = kFar ? far_gate : sums[kGateSum][c], (&weight_sum)[8] = kFar ? far_weight : sums[kPostWeight][c];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            // behind a row's end d is what a layer norm took out; what is dropped may be anything
-                            const bool keep = (!kPreLayer || inside(c, i)) && (!DROP || bits.of(i) >= k->a.random.threshold);
-                            const float u = kPost ? (now.f[c][i] - mean_f) * rho_f : now.f[c][i];
-                            const float v = kPostLayer ? __builtin_fmaf(u, w[i], b[i]) : kPost ? u * w[i] : u;
-                            const float back = !DROP && !kPreLayer ? scale * d[c][i] : keep ? scale * d[c][i] : 0.0f;
-                            gate_sum[i] = __builtin_fmaf(back, DROP && !keep ? 0.0f : v, gate_sum[i]);
-                            const float du = DROP && !keep ? 0.0f : back * g[i];
-                            if constexpr (kPost) {
-                                weight_sum[i] = __builtin_fmaf(du, u, weight_sum[i]);
-                                if constexpr (kPostLayer) sums[kPostBias][c][i] += du;
-                                d[c][i] = du * w[i];
-                                if constexpr (kPostLayer) two[0] += d[c][i];
-                                two[1] = __builtin_fmaf(d[c][i], u, two[1]);
-                            } else {
-                                d[c][i] = du;
-                            }
-                            if (kPacked && i % 2 == 1) __builtin_amdgcn_sched_barrier(0);       // (all eight side by side would take too many registers)
+                    for (int i = 0; i < 8; ++i) {
+                        // behind a row's end d is what a layer norm took out; what is dropped may be anything
+                        const bool keep = (!kPreLayer || inside(c, i)) && bits.of(i) >= k->a.random.threshold;
+                        const float u = kPost ? (now.f[c][i] - mean_f) * rho_f : now.f[c][i];
+                        const float v = kPostLayer ? __builtin_fmaf(u, w[i], b[i]) : kPost ? u * w[i] : u;
+                        const float back = keep ? scale * d[c][i] : 0.0f;
+                        gate_sum[i] = __builtin_fmaf(back, keep ? v : 0.0f, gate_sum[i]);
+                        const float du = keep ? back * g[i] : 0.0f;
+                        if constexpr (kPost) {
+                            weight_sum[i] = __builtin_fmaf(du, u, weight_sum[i]);
+                            if constexpr (kPostLayer) sums[kPostBias][c][i] += du;
+                            d[c][i] = du * w[i];
+                            if constexpr (kPostLayer) two[0] += d[c][i];
+                            two[1] = __builtin_fmaf(d[c][i], u, two[1]);
+                        } else {
+                            d[c][i] = du;
                         }
-                        if constexpr (kFar) far_store(kGateSum, c, far_gate);
-                        if constexpr (kFar && kPost) far_store(kPostWeight, c, far_weight);
+                        if (kPacked && i % 2 == 1) __builtin_amdgcn_sched_barrier(0);       // (all eight side by side would take too many registers)
                     }
+                    if constexpr (kFar) far_store(kGateSum, c, far_gate);
+                    if constexpr (kFar && kPost) far_store(kPostWeight, c, far_weight);
                 }
                 if (k->a.df) {
                     if constexpr (kPost) {
