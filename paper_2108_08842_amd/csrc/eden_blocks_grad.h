@@ -11,9 +11,12 @@
 // have.  No atomics: the same bits every time.
 //
 // What counts is registers: sums, operands of this row and of the next (on their way meanwhile, or each row would wait for its loads), weights.  Hence operands stay packed, kinds of norms are compiled in, and the arguments
-// are read again for each row.  bf16, dropout, gate: 8192 x 4096 with rms norms 81 us and 5 for the second launch (403 MB at 4.7 TB/s together), layer norms 103, 32768 x 1024 81 and 91, 8192 x 8192 169 and 248; without a
-// branch 43 and 52.  Above 8192 columns nothing is fetched ahead and some registers go to memory: 4096 x 16384 327 and 530 (a floor of 158).  Rows of 128 columns 35 to 53 us at 131072 of
-// them, 2.7 to 4 TB/s: four rows a wave, and a loop that waits.
+// are read again for each row.  Dropout, gate, both norms rms / both layer, us with the second launch: bf16 8192 x 4096 77 to 88 / 96 to 103 (403 MB at 4.7 TB/s), 32768 x 1024 80 / 93, 8192 x 8192 172 / 244, 4096 x 16384 320 / 525
+// (floor 158), without a branch 8192 x 4096 41 / 49; fp32 8192 x 4096 172 / 190 (floor 158), 8192 x 8192 348 / 378 (316), 4096 x 16384 466 / 715, without a branch 88 / 94 (79).  131072 x 128 bf16 50 / 53, fp32 101 / 108: four rows a
+// wave, and a loop that waits.
+// What does not fit (the compiler's resource records; a lane's registers that go to memory): above 8192 columns with both norms 33 to 98, with one up to 35; two-byte types: both norms layer up to 2048 columns 2 to 10, rms
+// behind the branch and any norm in front from 4097 to 8192 columns 2 to 26; fp32 up to 2048 columns: a norm in front alone 2 to 24, rms behind and layer in front 4 to 7.  Nothing is fetched ahead, and weights are read again for each
+// row, where kHeld is false: with a branch above 8192 columns, fp32 above 4096 (without a branch 8192), with a layer norm behind the branch two-byte types above 4096 and fp32 always.
 #include "eden_blocks_kernels.h"
 
 namespace eden_layers {

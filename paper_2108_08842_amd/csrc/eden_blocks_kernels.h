@@ -43,7 +43,7 @@ template <int WIDE, int FROM> struct RowShape {
 };
 using JoinShape = RowShape<1024, 64>;
 // A gradient with the sums of the gate and of two norms takes more registers than 1024 lanes have (128 each): up to 8192 columns it has 512 lanes at most; beyond, two of its sums are
-// in the LDS (4096 x 16384 bf16, both norms rms, gate, dropout: 461 -> 327 us against 512 lanes with four chunks each and all sums in registers, which spilled; layer norms 890 -> 530).
+// in the LDS (4096 x 16384 bf16, both norms rms, gate, dropout: 461 -> 320 us against 512 lanes with four chunks each and all sums in registers, which spilled; layer norms 890 -> 525).
 using GradShape = RowShape<1024, 1024>;
 using FullGradShape = RowShape<1024, 512>;
 

@@ -69,7 +69,7 @@ template <class T, int N> __device__ inline void store_some(T *p, const Vec<T, N
     }
 }
 
-// The same past the caches where it is 16 bytes, for results larger than they are.  Neighbouring lanes have to have neighbouring pieces: 32 bytes a lane in two such stores write every line twice.
+// The same past the caches where it is 16 bytes.  Measured on results that the caches could not hold; a short result goes the same way, and what its next reader pays for that has not been measured.  Neighbouring lanes have to have neighbouring pieces: 32 bytes a lane in two such stores write every line twice.
 template <class T, int N> __device__ inline void stream_some(T *p, const Vec<T, N> &r, int valid) {
     if constexpr (sizeof(r) == 16) {
         if (valid >= N) {
